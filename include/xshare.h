@@ -556,6 +556,163 @@ xshare_status xshare_probe_stream_read(const void* buf, size_t bytes, int32_t bl
 xshare_status xshare_block_times(uint64_t* gate_up, uint64_t* down, uint64_t* down_units,
                                  int32_t clear, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------------------- *
+ * Routing by scores, bias and groups, and FP8 products with a scale for each block of 128.  *
+ * The layer form of checkpoints that hold E4M3FN weights with one scale per 128 x 128 block *
+ * and route by sigmoid scores: xshare_gate -> xshare_block_experts, with xshare_block_linear*
+ * for the products outside the routed experts.  Limits of these calls: T and T * k at most  *
+ * 2^20, every other size at most 2^20 (XSHARE_EUNSUPPORTED beyond).                         *
+ * ---------------------------------------------------------------------------------------- */
+
+/* Element type of the logits of xshare_gate.                                               */
+enum { XSHARE_F32 = 0, XSHARE_BF16 = 1 };
+
+/* Scores s_j of a token's logits.                                                          */
+enum {
+  XSHARE_GATE_SOFTMAX = 0,  /* s = exp(h_j - max h) / sum over all N experts                 */
+  XSHARE_GATE_SIGMOID = 1   /* s = 1 / (1 + exp(-h_j))                                       */
+};
+
+/* Score of a group of experts.                                                             */
+enum {
+  XSHARE_GROUP_MAX = 0,     /* its best expert's                                             */
+  XSHARE_GROUP_TOP2 = 1     /* the sum of its two best experts' s (+ bias)                   */
+};
+
+typedef struct {
+  int32_t n_experts;        /* N <= 1024                                                     */
+  int32_t top_k;            /* k <= 32, k <= top_groups * N / n_groups                       */
+  int32_t score;            /* XSHARE_GATE_*                                                 */
+  int32_t n_groups;         /* G <= 64 groups of N / G consecutive experts; G divides N      */
+  int32_t top_groups;       /* 1 <= top_groups <= G groups that a token may choose from      */
+  int32_t group_score;      /* XSHARE_GROUP_*; TOP2 needs N / G >= 2 where groups are left out */
+  int32_t renormalize;      /* nonzero: the k weights are divided by their sum               */
+  float scale;              /* then multiplied by this (finite)                              */
+} xshare_gate_params;
+
+/*
+ * xshare_gate -- a router's choice of experts for each token by itself.
+ *
+ *   logits  [T, N] fp32 or bf16 (`dtype`), rows `ld` elements apart (ld >= N).
+ *   bias    nullable [N] fp32, finite: added to the scores for the choice only, not to the
+ *           weights (a load-balancing bias).
+ *   ids     out [T, k] int32, best first.      w  out [T, k] fp32.
+ *
+ * The experts rank by c_j = s_j + bias_j, or by the logits where there is no bias (the same
+ * order); the groups by their score; ties go to the lower index.  Of the top_groups best
+ * groups the k best experts are taken, and w_r = s_{id_r}, renormalised and scaled as asked.
+ * Scores, sums and weights are fp32.  One kernel, no workspace.
+ */
+xshare_status xshare_gate(const void* logits, int32_t dtype, int32_t T, int64_t ld,
+                          const float* bias, const xshare_gate_params* params, int32_t* ids,
+                          float* w, hipStream_t stream);
+
+/*
+ * xshare_gate_backward -- the gradient of the logits from the gradient of xshare_gate's
+ * weights.  The choice is a constant, so the bias and the groups have no part in it.
+ *
+ *   ids      [T, k] the choice; distinct in a row.  An id outside [0, N) is no choice: it
+ *            has no weight and its dw is not read.
+ *   dw       [T, k] fp32.        dlogits  out [T, N] fp32, every element written.
+ *   n_groups, top_groups and group_score of `params` are not read.
+ */
+xshare_status xshare_gate_backward(const void* logits, int32_t dtype, int32_t T, int64_t ld,
+                                   const xshare_gate_params* params, const int32_t* ids,
+                                   const float* dw, float* dlogits, hipStream_t stream);
+
+/*
+ * xshare_block_quantize -- bf16 to E4M3FN codes with one fp32 scale for each block of
+ * block_rows x 128 elements (block_rows 1: activations, 128: weights).
+ *
+ *   x       [rows, cols] bf16, rows `ld` elements apart; 16-byte aligned, cols a multiple of
+ *           16, ld >= cols a multiple of 8.
+ *   q       out [rows, cols] codes, 16-byte aligned; decode(code) * scale stands for x.
+ *   scales  out [ceil(rows / block_rows), ceil(cols / 128)]: a / 448, a = max |x| of the block,
+ *           at least 448 * 2^-126.
+ *
+ * A code is 448 x / a rounded to the nearest E4M3 value (ties to even), the quotient correctly
+ * rounded in fp32: for bf16 inputs that is the code of exact arithmetic.  A NaN in a block
+ * makes its scale NaN, else an infinity makes it infinite (every product with it is NaN).
+ */
+xshare_status xshare_block_quantize(const uint16_t* x, int32_t rows, int32_t cols, int64_t ld,
+                                    int32_t block_rows, uint8_t* q, float* scales,
+                                    hipStream_t stream);
+
+/* Workspace of xshare_block_linear (bytes, 256-aligned); 0 for invalid sizes.             */
+size_t xshare_block_linear_workspace_bytes(int32_t T, int32_t n, int32_t k);
+
+/*
+ * xshare_block_linear -- y = x W^T in FP8 with block scales.
+ *
+ *   x        [T, k] bf16, rows ldx elements apart (as xshare_block_quantize's x), quantized
+ *            here in 1 x 128 blocks; or NULL, with
+ *   xq, xs   the codes [T, k] (16-byte aligned) and scales [T, ceil(k / 128)] of it.
+ *   wq       [n, k] E4M3FN codes, 16-byte aligned, k a multiple of 16, n any.
+ *   wscale   [ceil(n / 128), ceil(k / 128)] fp32.
+ *   y        out [T, n] bf16, rows ldy >= n elements apart.
+ *
+ * y_tn = sum over blocks b of k of xs_tb wscale_{n/128,b} sum_{i in b} xq_ti wq_ni, summed in
+ * fp32 and rounded once.  Inside a block the FP8 matrix instruction aligns the products of
+ * eight neighbouring i to the largest of them (about 13 bits below it are kept), which is why
+ * no fp32 output is offered.
+ *
+ * The input's gradient, dy W, is the same call with the transposed codes [k, n] and scales
+ * [ceil(k / 128), ceil(n / 128)] (128 x 128 blocks transpose to such blocks; n a multiple of
+ * 16 then).  Weights are frozen codes here: there is no gradient of them.
+ */
+xshare_status xshare_block_linear(const uint16_t* x, int64_t ldx, const uint8_t* xq,
+                                  const float* xs, int32_t T, int32_t n, int32_t k,
+                                  const uint8_t* wq, const float* wscale, uint16_t* y,
+                                  int64_t ldy, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Arguments of xshare_block_experts.  Zero-initialise, set struct_size, fill.
+ *
+ *   x           [T, d] bf16, rows ldx elements apart (as xshare_block_quantize's x).
+ *   ids, w      [T, top_k] int32 and fp32: each token's experts and weights, from xshare_gate or a
+ *               set selection (xshare_route, ...) or elsewhere.  A pair whose id lies outside
+ *               [0, n_experts) is left out (an expert of another GPU): no weight is read for it.
+ *   w1, w3      [n_experts, f, d] codes; w2 [n_experts, d, f]; 16-byte aligned.
+ *   w1_scale, w3_scale  [n_experts, ceil(f / 128), ceil(d / 128)] fp32;
+ *   w2_scale    [n_experts, ceil(d / 128), ceil(f / 128)].
+ *   d, f        multiples of 16.    n_experts <= 1024, top_k <= 32.
+ *   y           out [T, d] bf16, rows ldy >= d elements apart, ldy a multiple of 8, 16-byte
+ *               aligned; a token without pairs gets zeros.
+ *   ws          of xshare_block_experts_workspace_bytes.
+ */
+typedef struct {
+  size_t struct_size;
+  int32_t T, top_k, n_experts, d, f;
+  const uint16_t* x;
+  int64_t ldx;
+  const int32_t* ids;
+  const float* w;
+  const uint8_t* w1;
+  const uint8_t* w3;
+  const uint8_t* w2;
+  const float* w1_scale;
+  const float* w3_scale;
+  const float* w2_scale;
+  uint16_t* y;
+  int64_t ldy;
+  void* ws;
+  size_t ws_bytes;
+  hipStream_t stream;
+} xshare_block_experts_args;
+
+/* Workspace of xshare_block_experts (bytes, 256-aligned); 0 for invalid sizes.            */
+size_t xshare_block_experts_workspace_bytes(int32_t T, int32_t top_k, int32_t n_experts,
+                                            int32_t d, int32_t f);
+
+/*
+ * xshare_block_experts -- the routed SwiGLU experts of given (token, expert, weight) triples:
+ * y_i = sum_r w_ir E_{id_ir}(x_i) in rank order, E(x) = W2 q(silu(W1 q(x)) * (W3 q(x))), q the
+ * quantisation in 1 x 128 blocks, products and sums as xshare_block_linear, SwiGLU, the
+ * experts' outputs and their sum in fp32, rounded to bf16 once.  From one token to prefill
+ * chunks; only weights of experts with a pair are read.
+ */
+xshare_status xshare_block_experts(const xshare_block_experts_args* args);
+
 /* Static description of a status code (never NULL).                                      */
 const char* xshare_status_string(int32_t status);
 

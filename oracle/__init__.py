@@ -13,7 +13,9 @@ Modules:
   fixed-budget greedy of Algorithm 1, refinement; Section 3.4), and
   Algorithms 3 + 4 (per-request then batch selection; Section 4.1);
 * ``ffn``      -- the MoE layer output of Section 2.1 with SwiGLU experts,
-  in float64.
+  in float64;
+* ``gate``     -- routing by scores, bias and groups, and its gradient, in float64;
+* ``blocks``   -- FP8 products with a scale for each block of 128, in float64.
 
 Parity status: every function here is pinned by the CPU tests (closed form
 of Section 1, brute-force optimum of Eq. (2) per Corollary 3.2, invariants,

@@ -7,6 +7,9 @@ Translation units:
                the gate arithmetic is exactly the documented sequence of fp32 operations;
 * ffn.hip   -- expert GEMMs (bf16 MFMA) and the combine (ffn_wide.h: those of large batches);
 * abi.hip   -- the extern "C" entry points declared in include/xshare.h;
+* gate.hip  -- routing by scores, bias and groups, and its backward pass; -ffp-contract=off;
+* blocks.hip -- FP8 products with a scale for each block of 128: quantiser, linear, experts;
+* abi_blocks.hip -- their extern "C" entry points;
 * probe.hip -- the streaming-read probe (measurement of the HBM read ceiling).
 Every HIP compile disables packed-fp32 instruction selection.  The same sources built with
 XS_BLOCK_TIMES=1 give libxshare_timeline.so, the profiling build whose expert GEMMs stamp
@@ -38,6 +41,10 @@ UNITS = {
                   "-fno-fast-math"],
     "ffn.hip": [],
     "abi.hip": [],
+    "gate.hip": ["-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt",
+                 "-fno-fast-math"],
+    "blocks.hip": ["-fhip-fp32-correctly-rounded-divide-sqrt"],
+    "abi_blocks.hip": [],
     "probe.hip": [],
 }
 

@@ -1,0 +1,126 @@
+// Launchers of the routing by scores (gate.hip) and of the FP8 products with a scale for each
+// block of 128 (blocks.hip), and the workspace layout of the latter.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "internal.h"
+
+namespace xs {
+
+constexpr int kMaxGateGroups = 64;
+constexpr int kMaxBlockSize = 1 << 20;   // every size of the block calls
+constexpr int kQuantBlock = 128;         // inputs (and weight rows) that share a scale
+
+inline int quant_blocks(int n) { return (n + kQuantBlock - 1) / kQuantBlock; }
+
+struct GateArgs {
+  const void* logits;
+  int bf16;                    // 0: fp32 logits
+  int T, N, k;
+  long ld;
+  const float* bias;           // nullable [N]
+  int sigmoid;                 // 0: softmax
+  int G, top_groups, top2;
+  int renormalize;
+  float scale;
+  int32_t* ids;                // [T, k], written by the forward pass
+  float* w;
+  const float* dw;             // backward: [T, k]
+  float* dlogits;              // [T, N]
+};
+
+hipError_t launch_gate(const GateArgs& a, hipStream_t stream);
+hipError_t launch_gate_backward(const GateArgs& a, hipStream_t stream);
+
+// x [rows, cols] bf16 -> codes and scales; block_rows 1 or 128.
+hipError_t launch_block_quantize(const uint16_t* x, int rows, int cols, long ld, int block_rows,
+                                 uint8_t* q, float* scales, hipStream_t stream);
+
+// Rows of a token tile of the grouped products.
+constexpr int kTileRows = 32;
+
+struct BlockLinearLayout {
+  size_t xq;                   // uint8 [T, k]  codes of x
+  size_t xs;                   // fp32 [T, ceil(k / 128)]
+  size_t total;
+};
+inline BlockLinearLayout block_linear_layout(int T, int k) {
+  BlockLinearLayout L{};
+  size_t o = 0;
+  L.xq = o; o += align256(size_t(T) * k);
+  L.xs = o; o += align256(sizeof(float) * size_t(T) * quant_blocks(k));
+  L.total = o > 0 ? o : 256;
+  return L;
+}
+
+struct BlockLinearArgs {
+  int T, n, k;
+  const uint8_t* xq;
+  const float* xs;
+  const uint8_t* wq;
+  const float* wscale;
+  uint16_t* y;
+  long ldy;
+};
+hipError_t launch_block_linear(const BlockLinearArgs& a, hipStream_t stream);
+
+// Tiles of the (token, expert) pairs in expert order: at most one partly filled tile for each
+// expert with a pair, the rest full.
+inline int pair_tiles(int pairs, int E, int tile_rows) {
+  const int some = pairs < E ? pairs : E;
+  return some + (pairs - some) / tile_rows;
+}
+
+struct BlockExpertsLayout {
+  size_t xq, xs;               // as BlockLinearLayout, of x [T, d]
+  size_t counts;               // int32 [4]: pairs, tiles
+  size_t perm;                 // int32 [T * k] pair (t * k + r) of each row in expert order
+  size_t tiles;                // int4 [pair_tiles] {expert, first row, rows, 0}
+  size_t h;                    // fp32 [T * k, f] hidden rows in expert order
+  size_t hq, hs;               // their codes [T * k, f] and scales [T * k, ceil(f / 128)]
+  size_t o;                    // fp32 [T * k, d] the pairs' outputs, by pair
+  size_t total;
+};
+inline BlockExpertsLayout block_experts_layout(int T, int k, int E, int d, int f) {
+  BlockExpertsLayout L{};
+  const size_t rows = size_t(T) * k;
+  size_t o = 0;
+  L.xq = o;     o += align256(size_t(T) * d);
+  L.xs = o;     o += align256(sizeof(float) * size_t(T) * quant_blocks(d));
+  L.counts = o; o += 256;
+  L.perm = o;   o += align256(sizeof(int32_t) * rows);
+  L.tiles = o;  o += align256(sizeof(int32_t) * 4 * size_t(pair_tiles(int(rows), E, kTileRows)));
+  L.h = o;      o += align256(sizeof(float) * rows * f);
+  L.hq = o;     o += align256(rows * f);
+  L.hs = o;     o += align256(sizeof(float) * rows * quant_blocks(f));
+  L.o = o;      o += align256(sizeof(float) * rows * d);
+  L.total = o;
+  return L;
+}
+
+struct BlockExpertsArgs {
+  int T, k, E, d, f;
+  const uint16_t* x;
+  long ldx;
+  const int32_t* ids;
+  const float* w;
+  const uint8_t *w1, *w3, *w2;
+  const float *s1, *s3, *s2;
+  uint16_t* y;
+  long ldy;
+  uint8_t* xq;
+  float* xs;
+  int32_t* counts;
+  int32_t* perm;
+  int4* tiles;
+  float* h;
+  uint8_t* hq;
+  float* hs;
+  float* o;
+};
+hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream);
+
+}  // namespace xs

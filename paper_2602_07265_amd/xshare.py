@@ -80,7 +80,37 @@ class LayerArgs(ctypes.Structure):
     ]
 
 
+class GateParams(ctypes.Structure):
+    """xshare_gate_params (include/xshare.h)."""
+    _fields_ = [
+        ("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("score", ctypes.c_int32),
+        ("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+        ("group_score", ctypes.c_int32), ("renormalize", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class BlockExpertsArgs(ctypes.Structure):
+    """xshare_block_experts_args (include/xshare.h)."""
+    _fields_ = [
+        ("struct_size", ctypes.c_size_t),
+        ("T", ctypes.c_int32), ("top_k", ctypes.c_int32), ("n_experts", ctypes.c_int32),
+        ("d", ctypes.c_int32), ("f", ctypes.c_int32),
+        ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+        ("ids", ctypes.c_void_p), ("w", ctypes.c_void_p),
+        ("w1", ctypes.c_void_p), ("w3", ctypes.c_void_p), ("w2", ctypes.c_void_p),
+        ("w1_scale", ctypes.c_void_p), ("w3_scale", ctypes.c_void_p),
+        ("w2_scale", ctypes.c_void_p),
+        ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64),
+        ("ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
 WEIGHTS = {"bf16": 0, "fp8": 1, "mxfp4": 2}
+GATE = {"softmax": 0, "sigmoid": 1}
+GROUP = {"max": 0, "top2": 1}
+LOGITS = {torch.float32: 0, torch.bfloat16: 1}
 
 STATS_FIELDS = ("n_selected", "n_active", "n_vanilla_union", "n_warmup", "n_start",
                 "budget_eff", "max_group_load")
@@ -95,6 +125,7 @@ class XShareError(RuntimeError):
 _lib = None
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
+_I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
 
 
@@ -163,6 +194,23 @@ def lib() -> ctypes.CDLL:
         L.xshare_moe_forward_v2.restype = ctypes.c_int
         L.xshare_moe_forward_v2_workspace_bytes.argtypes = [ctypes.POINTER(LayerArgs)]
         L.xshare_moe_forward_v2_workspace_bytes.restype = _SZ
+        L.xshare_gate.argtypes = [_P, _I32, _I32, _I64, _P, ctypes.POINTER(GateParams), _P, _P,
+                                  _P]
+        L.xshare_gate.restype = ctypes.c_int
+        L.xshare_gate_backward.argtypes = [_P, _I32, _I32, _I64, ctypes.POINTER(GateParams), _P,
+                                           _P, _P, _P]
+        L.xshare_gate_backward.restype = ctypes.c_int
+        L.xshare_block_quantize.argtypes = [_P, _I32, _I32, _I64, _I32, _P, _P, _P]
+        L.xshare_block_quantize.restype = ctypes.c_int
+        L.xshare_block_linear_workspace_bytes.argtypes = [_I32, _I32, _I32]
+        L.xshare_block_linear_workspace_bytes.restype = _SZ
+        L.xshare_block_linear.argtypes = [_P, _I64, _P, _P, _I32, _I32, _I32, _P, _P, _P, _I64,
+                                          _P, _SZ, _P]
+        L.xshare_block_linear.restype = ctypes.c_int
+        L.xshare_block_experts_workspace_bytes.argtypes = [_I32, _I32, _I32, _I32, _I32]
+        L.xshare_block_experts_workspace_bytes.restype = _SZ
+        L.xshare_block_experts.argtypes = [ctypes.POINTER(BlockExpertsArgs)]
+        L.xshare_block_experts.restype = ctypes.c_int
         L.xshare_probe_stream_read.argtypes = [_P, _SZ, _I32, _I32, _P, _P]
         L.xshare_probe_stream_read.restype = ctypes.c_int
         L.xshare_block_times.argtypes = [_P, _P, _P, _I32, _P]
@@ -837,6 +885,199 @@ def moe_forward_v2(x: torch.Tensor, top_k: int, warmup_k0: int, budget: int,
     a.ws, a.ws_bytes = workspace.data_ptr(), workspace.numel()
     _check(lib().xshare_moe_forward_v2(ctypes.byref(a)), "xshare_moe_forward_v2")
     return res
+
+
+# ------------------------------------------- routing by scores, FP8 products in blocks of 128
+
+def _rows(t, dtype, name, cols=None):
+    """A GPU matrix of dtype whose rows may lie apart (its columns do not); its row stride."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{name} must be a matrix" + ("" if cols is None else f" of {cols} columns")
+                         + f", got {tuple(t.shape)}")
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be neighbours")
+    return ld
+
+
+def _same_device(x, *others):
+    for t in others:
+        if t is not None and t.device != x.device:
+            raise ValueError(f"tensors on {x.device} and {t.device}")
+
+
+def _gate_params(N, top_k, score, n_groups, top_groups, group_score, renormalize, scale):
+    return GateParams(N, int(top_k), GATE[score] if isinstance(score, str) else int(score),
+                      int(n_groups), int(top_groups),
+                      GROUP[group_score] if isinstance(group_score, str) else int(group_score),
+                      int(bool(renormalize)), float(scale))
+
+
+def _logits(logits):
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in LOGITS:
+        raise ValueError("logits must be a float32 or bfloat16 GPU tensor")
+    return LOGITS[logits.dtype], _rows(logits, logits.dtype, "logits")
+
+
+def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_groups: int = 1,
+         top_groups: int = 1, group_score="max", renormalize: bool = True, scale: float = 1.0,
+         out=None, stream=None) -> dict:
+    """A router's choice for each token of logits [T, N] (fp32 or bf16): dict(ids int32 [T, k],
+    w fp32 [T, k]).  ``bias`` (fp32 [N]) enters the choice only; with ``n_groups`` the experts
+    come from the ``top_groups`` best groups (group_score "max" or "top2")."""
+    dtype, ld = _logits(logits)
+    T, N = logits.shape
+    k = int(top_k)
+    if bias is not None:
+        _dev(bias, torch.float32, (N,), "bias")
+    out = {} if out is None else out
+    ids, w = out.get("ids"), out.get("w")
+    if ids is None:
+        ids = torch.empty((T, max(k, 0)), dtype=torch.int32, device=logits.device)
+    if w is None:
+        w = torch.empty((T, max(k, 0)), dtype=torch.float32, device=logits.device)
+    _dev(ids, torch.int32, (T, k), "ids")
+    _dev(w, torch.float32, (T, k), "w")
+    _same_device(logits, bias, ids, w)
+    p = _gate_params(N, k, score, n_groups, top_groups, group_score, renormalize, scale)
+    st = lib().xshare_gate(_ptr(logits), dtype, T, ld, _ptr(bias), ctypes.byref(p), _ptr(ids),
+                           _ptr(w), _stream(stream))
+    _check(st, "xshare_gate")
+    return dict(ids=ids, w=w)
+
+
+def gate_backward(logits: torch.Tensor, ids: torch.Tensor, dw: torch.Tensor, *, score="softmax",
+                  renormalize: bool = True, scale: float = 1.0, out=None,
+                  stream=None) -> torch.Tensor:
+    """The gradient of the logits (fp32 [T, N]) from dw, the gradient of ``gate``'s weights, for
+    its choice ids; score, renormalize and scale as given to ``gate``."""
+    dtype, ld = _logits(logits)
+    T, N = logits.shape
+    k = ids.shape[1] if ids.dim() == 2 else -1
+    _dev(ids, torch.int32, (T, k), "ids")
+    _dev(dw, torch.float32, (T, k), "dw")
+    if out is None:
+        out = torch.empty((T, N), dtype=torch.float32, device=logits.device)
+    _dev(out, torch.float32, (T, N), "out")
+    _same_device(logits, ids, dw, out)
+    p = _gate_params(N, k, score, 1, 1, "max", renormalize, scale)
+    st = lib().xshare_gate_backward(_ptr(logits), dtype, T, ld, ctypes.byref(p), _ptr(ids),
+                                    _ptr(dw), _ptr(out), _stream(stream))
+    _check(st, "xshare_gate_backward")
+    return out
+
+
+def _blocks(n):
+    return (n + 127) // 128
+
+
+def block_quantize(x: torch.Tensor, block_rows: int = 1, *, out=None, stream=None) -> tuple:
+    """(codes uint8 [rows, cols], scales fp32) of a bf16 matrix: E4M3FN with one scale for each
+    block of block_rows x 128 (1: activations, 128: weights).  ``out``: the two to write."""
+    ld = _rows(x, torch.bfloat16, "x")
+    rows, cols = x.shape
+    step = max(int(block_rows), 1)
+    shape = (-(-rows // step), _blocks(cols))
+    q, s = (None, None) if out is None else out
+    if q is None:
+        q = torch.empty((rows, cols), dtype=torch.uint8, device=x.device)
+    if s is None:
+        s = torch.empty(shape, dtype=torch.float32, device=x.device)
+    _dev(q, torch.uint8, (rows, cols), "codes")
+    _dev(s, torch.float32, shape, "scales")
+    _same_device(x, q, s)
+    st = lib().xshare_block_quantize(_ptr(x), rows, cols, ld, int(block_rows), _ptr(q), _ptr(s),
+                                     _stream(stream))
+    _check(st, "xshare_block_quantize")
+    return q, s
+
+
+def block_linear_workspace_bytes(T: int, n: int, k: int) -> int:
+    return int(lib().xshare_block_linear_workspace_bytes(int(T), int(n), int(k)))
+
+
+def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale=None, y=None,
+                 workspace=None, stream=None) -> torch.Tensor:
+    """y = x W^T (bf16 [T, n]) with W as codes wq uint8 [n, k] and scales ws of its 128 x 128
+    blocks.  x is bf16, quantized here in 1 x 128 blocks, or with ``x_scale`` its codes
+    (``block_quantize``).  The input's gradient is this call on dy with ``wq.t().contiguous()``
+    and ``ws.t().contiguous()``."""
+    if wq.dim() != 2:
+        raise ValueError("wq must be a matrix of codes")
+    n, k = wq.shape
+    _dev(wq, torch.uint8, (n, k), "wq")
+    _dev(ws, torch.float32, (_blocks(n), _blocks(k)), "ws")
+    if x_scale is None:
+        ldx = _rows(x, torch.bfloat16, "x", k)
+    else:
+        ldx = k
+        _dev(x, torch.uint8, (x.shape[0], k), "x codes")
+        _dev(x_scale, torch.float32, (x.shape[0], _blocks(k)), "x_scale")
+    T = x.shape[0]
+    if y is None:
+        y = torch.empty((T, n), dtype=torch.bfloat16, device=x.device)
+    ldy = _rows(y, torch.bfloat16, "y", n)
+    if y.shape[0] != T:
+        raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
+    _same_device(x, wq, ws, x_scale, y, workspace)
+    need = 0 if x_scale is not None else block_linear_workspace_bytes(T, n, k)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    own = x_scale is None
+    st = lib().xshare_block_linear(_ptr(x) if own else None, ldx, None if own else _ptr(x),
+                                   _ptr(x_scale), T, n, k, _ptr(wq), _ptr(ws), _ptr(y), ldy,
+                                   _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                   _stream(stream))
+    _check(st, "xshare_block_linear")
+    return y
+
+
+def block_experts_workspace_bytes(T: int, top_k: int, n_experts: int, d: int, f: int) -> int:
+    return int(lib().xshare_block_experts_workspace_bytes(int(T), int(top_k), int(n_experts),
+                                                          int(d), int(f)))
+
+
+def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch.Tensor,
+                  q3: torch.Tensor, q2: torch.Tensor, s1: torch.Tensor, s3: torch.Tensor,
+                  s2: torch.Tensor, *, y=None, workspace=None, stream=None) -> torch.Tensor:
+    """The routed SwiGLU experts of given pairs: y_i = sum_r w_ir E_{ids_ir}(x_i) (bf16 [T, d]),
+    FP8 weights (codes uint8 [N, f, d], [N, f, d], [N, d, f]) with a scale for each 128 x 128
+    block, activations quantized in 1 x 128 blocks.  ids and w [T, k] as ``gate`` or the set
+    selections return them; a pair whose id is not in [0, N) is left out."""
+    ldx = _rows(x, torch.bfloat16, "x")
+    T, d = x.shape
+    if q1.dim() != 3 or ids.dim() != 2:
+        raise ValueError("weights are [N, f, d], ids [T, k]")
+    N, f = q1.shape[0], q1.shape[1]
+    k = ids.shape[1]
+    _dev(ids, torch.int32, (T, k), "ids")
+    _dev(w, torch.float32, (T, k), "w")
+    _dev(q1, torch.uint8, (N, f, d), "w1 codes")
+    _dev(q3, torch.uint8, (N, f, d), "w3 codes")
+    _dev(q2, torch.uint8, (N, d, f), "w2 codes")
+    _dev(s1, torch.float32, (N, _blocks(f), _blocks(d)), "w1 scales")
+    _dev(s3, torch.float32, (N, _blocks(f), _blocks(d)), "w3 scales")
+    _dev(s2, torch.float32, (N, _blocks(d), _blocks(f)), "w2 scales")
+    if y is None:
+        y = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
+    ldy = _rows(y, torch.bfloat16, "y", d)
+    if y.shape[0] != T:
+        raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
+    _same_device(x, ids, w, q1, q3, q2, s1, s3, s2, y, workspace)
+    if workspace is None:
+        workspace = torch.empty(max(block_experts_workspace_bytes(T, k, N, d, f), 256),
+                                dtype=torch.uint8, device=x.device)
+    a = BlockExpertsArgs(ctypes.sizeof(BlockExpertsArgs), T, k, N, d, f, x.data_ptr(), ldx,
+                         ids.data_ptr(), w.data_ptr(), q1.data_ptr(), q3.data_ptr(),
+                         q2.data_ptr(), s1.data_ptr(), s3.data_ptr(), s2.data_ptr(),
+                         y.data_ptr(), ldy, workspace.data_ptr(), workspace.numel(),
+                         _stream(stream))
+    _check(lib().xshare_block_experts(ctypes.byref(a)), "xshare_block_experts")
+    return y
 
 
 def probe_stream_read(buf: torch.Tensor, blocks: int = 2048, mode: int = 0, sink=None,
