@@ -193,6 +193,8 @@ struct Product {
   const int32_t* counts;       // [1]: tiles
   const int32_t* perm;         // pair of each row in expert order
   float* out;                  // kGateUp: h [row, N]; kDown: o [pair, N]
+  uint8_t* hq;                 // kGateUp of the tiled kernel: the codes and scales of h
+  float* hs;
   uint16_t* y;                 // kLinear
   long ldy;
 };
@@ -315,6 +317,277 @@ __global__ __launch_bounds__(256) void product_kernel(Product a) {
   }
 }
 
+// Products with many token rows: BW weight rows (kGateUp: BW / 2 rows of W1 and the same of
+// W3) times BT tokens a workgroup, both operands through LDS in kStages buffers of one block
+// of K each, filled straight from global memory (no registers between).  The workgroup's waves
+// are WW along the weight rows by WT along the tokens, MW x TT instruction tiles each; a
+// block's results enter the accumulators while the next tile's instructions run.
+//
+// LDS rows are the 128 bytes of a block.  Row r keeps its 16-byte piece c at place
+// c ^ ((r >> 1) & 7): the sixteen rows of an operand read then lie in sixteen different
+// places modulo 256 bytes.  The loads write LDS in lane order, so the lanes take their
+// source pieces in that order.
+__device__ const uint4 kZeroPiece = {0, 0, 0, 0};   // what lies past the end of a row
+
+typedef const __attribute__((address_space(4))) float* ScalarPtr;   // read by scalar loads
+typedef const __attribute__((address_space(1))) void* GlobalPtr;
+typedef __attribute__((address_space(3))) void* LdsPtr;
+
+// `out`: the piece lies past the end of its row and is zero.  (The empty statement keeps the
+// choice an address: two loads under a branch would be made of it.)
+__device__ __forceinline__ void to_lds16(const uint8_t* src, bool out, uint8_t* dst) {
+  src = out ? reinterpret_cast<const uint8_t*>(&kZeroPiece) : src;
+  asm("" : "+v"(src));
+  __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 16, 0, 0);
+}
+__device__ __forceinline__ void to_lds4(const float* src, float* dst) {
+  __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 4, 0, 0);
+}
+// All but this wave's last N loads are done, and those of the workgroup's other waves too.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");   // no read of LDS moves above the barrier
+}
+
+template <int BW, int BT, int kStages>
+struct TileLds {
+  static constexpr int kScales = BT < 64 ? 64 : BT;
+  static constexpr int kStage = (BW + BT) * kQuantBlock + kScales * 4;
+  static constexpr int kBytes = kStages * kStage;
+};
+
+template <Kind kKind, int BW, int BT, int WW, int WT, int kStages>
+__global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
+  using L = TileLds<BW, BT, kStages>;
+  constexpr int kThreads = 64 * WW * WT;
+  constexpr int MW = BW / WW / 16, TT = BT / WT / 16;
+  constexpr int kRows = kThreads / 8;                       // rows of one load of the workgroup
+  constexpr int LW = BW / kRows, LT = BT >= kRows ? BT / kRows : 1;
+  constexpr int kLoads = LW + LT + 1;                       // of a wave and stage
+  constexpr int kUnits = kKind == kGateUp ? BW / 2 : BW;    // output columns of a workgroup
+  constexpr int kGroup = BT >= 256 ? TT : 2;                // token tiles worked on together
+  static_assert(kKind != kGateUp || MW % 2 == 0, "W1 and W3 tiles in pairs");
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ww = wave % WW, wt = wave / WW;
+  const int n = lane & 15, g = lane >> 4;
+  const int N = a.N, K = a.K;
+  const int nb = (K + kQuantBlock - 1) / kQuantBlock, nbN = (N + kQuantBlock - 1) / kQuantBlock;
+  int first, live;
+  const uint8_t *w1 = a.w1, *w3 = a.w3;
+  const float *s1 = a.s1, *s3 = a.s3;
+  if constexpr (kKind == kLinear) {
+    first = blockIdx.y * BT;
+    live = min(BT, a.rows - first);
+  } else {
+    if ((int)blockIdx.y >= a.counts[1]) return;
+    const int4 t = a.tiles[blockIdx.y];
+    first = t.y;
+    live = t.z;
+    const int e = __builtin_amdgcn_readfirstlane(t.x);
+    w1 += (size_t)e * N * K;
+    s1 += (size_t)e * nbN * nb;
+    if constexpr (kKind == kGateUp) {
+      w3 += (size_t)e * N * K;
+      s3 += (size_t)e * nbN * nb;
+    }
+  }
+  const int n0 = blockIdx.x * kUnits;
+  // LDS row R of the weights: tile (R / 16) % MW of wave R / (16 MW) along the weight rows
+  const uint8_t* wsrc[LW];
+  const int piece = 16 * ((lane & 7) ^ (((tid >> 3) >> 1) & 7));
+#pragma unroll
+  for (int j = 0; j < LW; ++j) {
+    const int R = j * kRows + (tid >> 3);
+    const uint8_t* w = w1;
+    int unit = n0 + R;
+    if constexpr (kKind == kGateUp) {
+      const int m = (R / 16) % MW;
+      w = m < MW / 2 ? w1 : w3;
+      unit = n0 + R / (16 * MW) * (8 * MW) + m % (MW / 2) * 16 + R % 16;
+    }
+    wsrc[j] = w + (size_t)min(unit, N - 1) * K + piece;
+  }
+  const uint8_t* xsrc[LT];
+#pragma unroll
+  for (int j = 0; j < LT; ++j) {
+    const int p = first + min((j * kRows + (tid >> 3)) % BT, live - 1);
+    const int r = kKind == kGateUp ? a.perm[p] / a.k : p;
+    xsrc[j] = a.xq + (size_t)r * K + piece;
+  }
+  const float* ssrc;
+  {
+    const int p = first + min(((wave * 64) % L::kScales) + lane, live - 1);
+    const int r = kKind == kGateUp ? a.perm[p] / a.k : p;
+    ssrc = a.xs + (size_t)r * nb;
+  }
+  auto load = [&](int b, uint8_t* stage) {
+    const int at = b * kQuantBlock;
+    const bool out = at + piece >= K;      // past the end of a last, partial block
+#pragma unroll
+    for (int j = 0; j < LW; ++j)
+      to_lds16(wsrc[j] + at, out,
+               stage + (j * kRows + wave * 8) * kQuantBlock);
+#pragma unroll
+    for (int j = 0; j < LT; ++j)
+      to_lds16(xsrc[j] + at, out,
+               stage + (BW + (j * kRows + wave * 8) % BT) * kQuantBlock);
+    to_lds4(ssrc + b,
+            reinterpret_cast<float*>(stage + (BW + BT) * kQuantBlock) + (wave * 64) % L::kScales);
+  };
+  // a wave's weight rows share one scale a block (two with kGateUp)
+  const int u0 = n0 + ww * (kKind == kGateUp ? 8 * MW : 16 * MW);
+  const size_t srow = (size_t)min(u0 / kQuantBlock, nbN - 1) * nb;
+  const ScalarPtr f1 = (ScalarPtr)(s1 + srow);
+  const ScalarPtr f3 = kKind == kGateUp ? (ScalarPtr)(s3 + srow) : f1;
+  const int nt = (live - wt * 16 * TT + 15) / 16;      // live tiles of this wave, at most TT
+  floatx4 acc[MW][TT];
+#pragma unroll
+  for (int m = 0; m < MW; ++m)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) acc[m][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const int swz = (n >> 1) & 7;
+  const int lo = 16 * (g ^ swz), hi = 16 * ((4 + g) ^ swz);
+  auto operand = [&](const uint8_t* row) {
+    const int4 u = *reinterpret_cast<const int4*>(row + lo);
+    const int4 v = *reinterpret_cast<const int4*>(row + hi);
+    return i32x8{u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s)
+    if (s < nb) load(s, lds + s * L::kStage);
+  // Block b from its buffer while a later block's loads fill another.  The two pointers are
+  // declared apart: without that every read of LDS would wait for every load in flight.
+  auto step = [&](int b, const uint8_t* __restrict__ stage, uint8_t* __restrict__ next) {
+    if (b + kStages - 1 < nb) load(b + kStages - 1, next);
+    const uint8_t* const wl = stage + (ww * 16 * MW + n) * kQuantBlock;
+    const uint8_t* const xl = stage + (BW + wt * 16 * TT + n) * kQuantBlock;
+    const float* const sl =
+        reinterpret_cast<const float*>(stage + (BW + BT) * kQuantBlock) + wt * 16 * TT + n;
+    const float fw1 = f1[b], fw3 = f3[b];
+    i32x8 w[MW];
+#pragma unroll
+    for (int m = 0; m < MW; ++m) w[m] = operand(wl + 16 * m * kQuantBlock);
+    // token tiles in groups, so that what waits in one tile has the others' work to hide it
+#pragma unroll
+    for (int t0 = 0; t0 < TT; t0 += kGroup) {
+      if (t0 >= nt) break;
+#pragma unroll
+      for (int t = t0; t < t0 + kGroup; ++t) {
+        const i32x8 x = operand(xl + 16 * t * kQuantBlock);
+        const float sx = sl[16 * t];
+#pragma unroll
+        for (int m = 0; m < MW; ++m) {
+          const floatx4 v = mfma128(w[m], x);
+          const float s = sx * (kKind == kGateUp && m >= MW / 2 ? fw3 : fw1);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[m][t][i] = __builtin_fmaf(v[i], s, acc[m][t][i]);
+        }
+      }
+    }
+  };
+  int cur = 0;                                         // the buffer of block b
+  for (int b = 0; b < nb; ++b) {
+    // the loads of this block are done; those of the kStages - 2 after it may be in flight
+    if (b + kStages - 2 < nb)
+      wait_loads<kLoads*(kStages - 2)>();
+    else
+      wait_loads<0>();
+    step(b, lds + cur * L::kStage, lds + (cur == 0 ? kStages - 1 : cur - 1) * L::kStage);
+    cur = cur + 1 == kStages ? 0 : cur + 1;
+  }
+
+  // lane (n, g) holds units 4 g .. 4 g + 3 of weight tile m for token n of tile t
+  if constexpr (kKind == kGateUp) {
+    constexpr int MH = MW / 2;
+    __syncthreads();                                   // the last block's reads of LDS
+    uint32_t* const part = reinterpret_cast<uint32_t*>(lds);   // [WW][BT] maxima
+    static_assert(kUnits == kQuantBlock, "a workgroup holds one block of the hidden row");
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int u = 0; u < MH; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float v = acc[u][t][i];
+          const float h = v / (1.0f + expf(-v)) * acc[MH + u][t][i];
+          const int c = u0 + 16 * u + 4 * g + i;
+          acc[u][t][i] = c < N ? h : 0.0f;
+          m = max(m, __float_as_uint(acc[u][t][i]) & 0x7FFFFFFFu);
+        }
+      m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+      m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+      if (g == 0) part[ww * BT + wt * 16 * TT + 16 * t + n] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      const int tok = wt * 16 * TT + 16 * t + n;
+      uint32_t m = 0;
+#pragma unroll
+      for (int w = 0; w < WW; ++w) m = max(m, part[w * BT + tok]);
+      if (tok >= live) continue;
+      const Quantum z = quantum(m);
+      const size_t row = first + tok;
+#pragma unroll
+      for (int u = 0; u < MH; ++u) {
+        const int c = u0 + 16 * u + 4 * g;
+        const float v[4] = {acc[u][t][0], acc[u][t][1], acc[u][t][2], acc[u][t][3]};
+        if (c < N) *reinterpret_cast<uint32_t*>(a.hq + row * N + c) = codes4(z, v);
+      }
+      if (ww == 0 && g == 0) a.hs[row * nbN + n0 / kQuantBlock] = z.scale;
+    }
+  } else {
+    const bool whole = kKind == kDown || (a.ldy % 4 == 0 && ((uintptr_t)a.y & 7) == 0);
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      const int tok = wt * 16 * TT + 16 * t + n;
+      if (tok >= live) continue;
+      const size_t row = kKind == kDown ? a.perm[first + tok] : first + tok;
+#pragma unroll
+      for (int m = 0; m < MW; ++m) {
+        const int c = u0 + 16 * m + 4 * g;
+        if constexpr (kKind == kDown) {
+          if (c < N) *reinterpret_cast<floatx4*>(a.out + row * N + c) = acc[m][t];
+        } else if (whole && c + 3 < N) {
+          const uint32_t p0 = to_bf16(acc[m][t][0]) | (uint32_t)to_bf16(acc[m][t][1]) << 16;
+          const uint32_t p1 = to_bf16(acc[m][t][2]) | (uint32_t)to_bf16(acc[m][t][3]) << 16;
+          *reinterpret_cast<uint2*>(a.y + row * a.ldy + c) = make_uint2(p0, p1);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (c + i < N) a.y[row * a.ldy + c + i] = to_bf16(acc[m][t][i]);
+        }
+      }
+    }
+  }
+}
+
+template <Kind kKind, int BW, int BT, int WW, int WT, int kStages>
+hipError_t launch_tile(const Product& a, int tiles, hipStream_t stream) {
+  constexpr int kBytes = TileLds<BW, BT, kStages>::kBytes;
+  static_assert(kBytes <= 160 * 1024, "LDS of a compute unit");
+  const auto kernel = tile_kernel<kKind, BW, BT, WW, WT, kStages>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+  if (e != hipSuccess) return e;
+  const int cols = kKind == kGateUp ? BW / 2 : BW;
+  kernel<<<dim3((a.N + cols - 1) / cols, tiles), 64 * WW * WT, kBytes, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <Kind kKind>
+hipError_t launch_tiles(const Product& a, int rows, int tiles, hipStream_t stream) {
+  if (rows == 256) return launch_tile<kKind, 256, 256, 4, 2, 2>(a, tiles, stream);
+  if (rows == 128) return launch_tile<kKind, 256, 128, 8, 1, 3>(a, tiles, stream);
+  return launch_tile<kKind, 256, 64, 8, 1, 3>(a, tiles, stream);
+}
+
 template <Kind kKind>
 hipError_t launch_product(const Product& a, int tiles, hipStream_t stream) {
   constexpr int MR = 4;
@@ -330,8 +603,8 @@ hipError_t launch_product(const Product& a, int tiles, hipStream_t stream) {
 // of every expert (in LDS) and, wave by wave, its own; its rows begin after those of the
 // experts before it, its tiles likewise, and its pairs are listed in ascending order.
 __global__ __launch_bounds__(1024) void index_kernel(const int32_t* ids, int pairs, int E,
-                                                     int32_t* counts, int32_t* perm,
-                                                     int4* tiles) {
+                                                     int tile_rows, int32_t* counts,
+                                                     int32_t* perm, int4* tiles) {
   __shared__ int count[kMaxExperts];
   __shared__ int mine[16];
   __shared__ int sum_rows[16], sum_tiles[16];
@@ -351,7 +624,7 @@ __global__ __launch_bounds__(1024) void index_kernel(const int32_t* ids, int pai
   __syncthreads();
   // rows and tiles of the experts before e, and of all
   const int c = tid < E ? count[tid] : 0;
-  const int tl = (c + kTileRows - 1) / kTileRows;
+  const int tl = (c + tile_rows - 1) / tile_rows;
   int before = tid < e ? c : 0, before_t = tid < e ? tl : 0;
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) {
@@ -372,10 +645,10 @@ __global__ __launch_bounds__(1024) void index_kernel(const int32_t* ids, int pai
   const int n = count[e];
   if (e == E - 1 && tid == 0) {
     counts[0] = row0 + n;
-    counts[1] = tile0 + (n + kTileRows - 1) / kTileRows;
+    counts[1] = tile0 + (n + tile_rows - 1) / tile_rows;
   }
-  for (int i = tid * kTileRows; i < n; i += 1024 * kTileRows)
-    tiles[tile0 + i / kTileRows] = make_int4(e, row0 + i, min(kTileRows, n - i), 0);
+  for (int i = tid * tile_rows; i < n; i += 1024 * tile_rows)
+    tiles[tile0 + i / tile_rows] = make_int4(e, row0 + i, min(tile_rows, n - i), 0);
   for (int i = from; i < to; i += 64) {
     const bool hit = i + lane < to && ids[i + lane] == e;
     const uint64_t hits = __ballot(hit);
@@ -428,15 +701,22 @@ hipError_t launch_block_linear(const BlockLinearArgs& a, hipStream_t stream) {
   p.rows = a.T;
   p.y = a.y;
   p.ldy = a.ldy;
+  if (a.T > 128)
+    return launch_tile<kLinear, 256, 256, 4, 2, 2>(p, (a.T + 255) / 256, stream);
+  if (a.T > kTileRows)
+    return launch_tile<kLinear, 256, 128, 8, 1, 3>(p, (a.T + 127) / 128, stream);
   return launch_product<kLinear>(p, (a.T + kTileRows - 1) / kTileRows, stream);
 }
 
 hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   const int pairs = a.T * a.k;
-  const int tiles = pair_tiles(pairs, a.E, kTileRows);
+  // rows of an expert with a pair, on average, if every expert has one
+  const int mean = pairs / (pairs < a.E ? pairs : a.E);
+  const int rows = mean >= 160 ? 256 : mean >= 40 ? 128 : mean >= 12 ? 64 : kTileRows;
+  const int tiles = pair_tiles(pairs, a.E, rows);
   hipError_t e = quantize_rows(a.x, a.T, a.d, a.ldx, a.xq, a.xs, nullptr, stream);
   if (e != hipSuccess) return e;
-  index_kernel<<<a.E, 1024, 0, stream>>>(a.ids, pairs, a.E, a.counts, a.perm, a.tiles);
+  index_kernel<<<a.E, 1024, 0, stream>>>(a.ids, pairs, a.E, rows, a.counts, a.perm, a.tiles);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   Product p{};
   p.xq = a.xq;
@@ -452,8 +732,14 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   p.counts = a.counts;
   p.perm = a.perm;
   p.out = a.h;
-  if ((e = launch_product<kGateUp>(p, tiles, stream)) != hipSuccess) return e;
-  e = quantize_rows(a.h, pairs, a.f, a.f, a.hq, a.hs, a.counts, stream);
+  p.hq = a.hq;
+  p.hs = a.hs;
+  if (rows == kTileRows) {
+    if ((e = launch_product<kGateUp>(p, tiles, stream)) != hipSuccess) return e;
+    e = quantize_rows(a.h, pairs, a.f, a.f, a.hq, a.hs, a.counts, stream);
+  } else {
+    e = launch_tiles<kGateUp>(p, rows, tiles, stream);
+  }
   if (e != hipSuccess) return e;
   p.xq = a.hq;
   p.xs = a.hs;
@@ -462,7 +748,9 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   p.N = a.d;
   p.K = a.f;
   p.out = a.o;
-  if ((e = launch_product<kDown>(p, tiles, stream)) != hipSuccess) return e;
+  e = rows == kTileRows ? launch_product<kDown>(p, tiles, stream)
+                        : launch_tiles<kDown>(p, rows, tiles, stream);
+  if (e != hipSuccess) return e;
   combine_kernel<<<dim3(a.T, (a.d / 8 + 255) / 256), 256, 0, stream>>>(a.o, a.ids, a.w, a.k, a.E,
                                                                      a.d, a.y, a.ldy);
   return hipGetLastError();
