@@ -39,8 +39,8 @@ hipError_t launch_gate_backward(const GateArgs& a, hipStream_t stream);
 hipError_t launch_block_quantize(const uint16_t* x, int rows, int cols, long ld, int block_rows,
                                  uint8_t* q, float* scales, hipStream_t stream);
 
-// Rows of a token tile of the grouped products.
-constexpr int kTileRows = 32;
+// Least rows of a token tile of the grouped products.
+constexpr int kTileRows = 16;
 
 struct BlockLinearLayout {
   size_t xq;                   // uint8 [T, k]  codes of x

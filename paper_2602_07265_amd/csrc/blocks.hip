@@ -17,6 +17,13 @@
 
 #include "blocks.h"
 
+#ifndef XS_FEW_4
+#define XS_FEW_4 4096
+#endif
+#ifndef XS_FEW_2
+#define XS_FEW_2 1024
+#endif
+
 namespace xs {
 namespace {
 
@@ -199,28 +206,22 @@ struct Product {
   long ldy;
 };
 
-constexpr int kTokTiles = kTileRows / 16;
+typedef const __attribute__((address_space(4))) float* ScalarPtr;   // read by scalar loads
 
-// The bytes of lane group g of one row of a block.  `p`: the row's block, at the lane's 16 g;
-// lo, hi: whether either half lies inside the row.
-__device__ __forceinline__ i32x8 load_operand(const uint8_t* p, bool lo, bool hi) {
-  const int4 zero = make_int4(0, 0, 0, 0);
-  const int4 a = lo ? *reinterpret_cast<const int4*>(p) : zero;
-  const int4 b = hi ? *reinterpret_cast<const int4*>(p + 64) : zero;
-  return i32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-}
-
-// A workgroup's product: 16 MR weight rows (kGateUp: half of W1, half of W3) times a tile of
-// kTileRows tokens.  Its four waves take the blocks of K in turn, so that no wave reads what
-// another does and no barrier stands in the loop; their sums meet in LDS at the end, added in
-// wave order.
-template <Kind kKind, int MR>
-__global__ __launch_bounds__(256) void product_kernel(Product a) {
-  constexpr int NT = kTokTiles;
+// Products with few token rows: a workgroup's share is 16 MR weight rows (kGateUp: half of W1,
+// half of W3) times a tile of 16 NT tokens.  Its KW waves take the blocks of K in turn, so that
+// no wave reads what another does and no barrier stands in the loop; the weights go from
+// memory straight into the instruction's operands, the next block's loads in flight under
+// this one's instructions.  The waves' sums meet in LDS at the end, added in wave order.
+template <Kind kKind, int MR, int NT, int KW>
+__global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
+  constexpr int kRows = 16 * NT;
   constexpr int MW = kKind == kGateUp ? MR / 2 : MR;    // tiles of one matrix
   constexpr int LD = 16 * MR + 4;
-  __shared__ float red[4][16 * NT][LD];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  static_assert(kKind != kGateUp || MR % 2 == 0, "W1 and W3 tiles in pairs");
+  __shared__ float red[KW][kRows][LD];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int N = a.N, K = a.K;
   const int nb = (K + kQuantBlock - 1) / kQuantBlock, nbN = (N + kQuantBlock - 1) / kQuantBlock;
@@ -228,18 +229,19 @@ __global__ __launch_bounds__(256) void product_kernel(Product a) {
   const uint8_t *w1 = a.w1, *w3 = a.w3;
   const float *s1 = a.s1, *s3 = a.s3;
   if constexpr (kKind == kLinear) {
-    first = blockIdx.y * kTileRows;
-    live = min(kTileRows, a.rows - first);
+    first = blockIdx.y * kRows;
+    live = min(kRows, a.rows - first);
   } else {
     if ((int)blockIdx.y >= a.counts[1]) return;
     const int4 t = a.tiles[blockIdx.y];
     first = t.y;
     live = t.z;
-    w1 += (size_t)t.x * N * K;
-    s1 += (size_t)t.x * nbN * nb;
+    const int e = __builtin_amdgcn_readfirstlane(t.x);
+    w1 += (size_t)e * N * K;
+    s1 += (size_t)e * nbN * nb;
     if constexpr (kKind == kGateUp) {
-      w3 += (size_t)t.x * N * K;
-      s3 += (size_t)t.x * nbN * nb;
+      w3 += (size_t)e * N * K;
+      s3 += (size_t)e * nbN * nb;
     }
   }
   const int n0 = blockIdx.x * 16 * MW;
@@ -250,8 +252,8 @@ __global__ __launch_bounds__(256) void product_kernel(Product a) {
     const int r = min(n0 + 16 * (m % MW) + n, N - 1);
     wrow[m] = (m < MW ? w1 : w3) + (size_t)r * K + 16 * g;
   }
-  const float* const sw1 = s1 + (size_t)(n0 / kQuantBlock) * nb;
-  const float* const sw3 = kKind == kGateUp ? s3 + (size_t)(n0 / kQuantBlock) * nb : nullptr;
+  const ScalarPtr f1 = (ScalarPtr)(s1 + (size_t)(n0 / kQuantBlock) * nb);
+  const ScalarPtr f3 = kKind == kGateUp ? (ScalarPtr)(s3 + (size_t)(n0 / kQuantBlock) * nb) : f1;
   const uint8_t* xrow[NT];
   const float* srow[NT];
 #pragma unroll
@@ -261,37 +263,82 @@ __global__ __launch_bounds__(256) void product_kernel(Product a) {
     xrow[t] = a.xq + (size_t)r * K + 16 * g;
     srow[t] = a.xs + (size_t)r * nb;
   }
-  const int nt = live > 16 ? NT : 1;
   floatx4 acc[MR][NT];
 #pragma unroll
   for (int m = 0; m < MR; ++m)
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[m][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  for (int b = wave; b < nb; b += 4) {
+  struct Block {
+    int4 w[MR][2], x[NT][2];
+    float sx[NT], f1, f3;
+  };
+  auto load = [&](Block& r, int b) {
     const int at = b * kQuantBlock;
-    const bool lo = at + 16 * g < K, hi = at + 64 + 16 * g < K;
-    i32x8 w[MR], x[NT];
 #pragma unroll
-    for (int m = 0; m < MR; ++m) w[m] = load_operand(wrow[m] + at, lo, hi);
-    float sx[NT];
+    for (int m = 0; m < MR; ++m) {
+      r.w[m][0] = *reinterpret_cast<const int4*>(wrow[m] + at);
+      r.w[m][1] = *reinterpret_cast<const int4*>(wrow[m] + at + 64);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      r.x[t][0] = *reinterpret_cast<const int4*>(xrow[t] + at);
+      r.x[t][1] = *reinterpret_cast<const int4*>(xrow[t] + at + 64);
+      r.sx[t] = srow[t][b];
+    }
+    r.f1 = f1[b];
+    if constexpr (kKind == kGateUp) r.f3 = f3[b];
+  };
+  auto whole = [](const int4 (&v)[2]) {
+    return i32x8{v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+  };
+  auto add = [&](const Block& r) {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
-      if (t < nt) {
-        x[t] = load_operand(xrow[t] + at, lo, hi);
-        sx[t] = srow[t][b];
+#pragma unroll
+      for (int m = 0; m < MR; ++m) {
+        const floatx4 v = mfma128(whole(r.w[m]), whole(r.x[t]));
+        const float s = r.sx[t] * (m < MW ? r.f1 : r.f3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[m][t][i] = __builtin_fmaf(v[i], s, acc[m][t][i]);
       }
-    const float f1 = sw1[b], f3 = kKind == kGateUp ? sw3[b] : 0.0f;
+  };
+  const int full = K / kQuantBlock;                     // blocks without an end in them
+  if (wave < full) {
+    const int last = full - 1;
+    Block u, v;
+    int b = wave;
+    load(u, b);
+    while (true) {                                      // (the last loads repeat block `last`)
+      load(v, min(b + KW, last));
+      __builtin_amdgcn_sched_barrier(0);                // loads stay above the instructions
+      add(u);
+      if ((b += KW) >= full) break;
+      load(u, min(b + KW, last));
+      __builtin_amdgcn_sched_barrier(0);
+      add(v);
+      if ((b += KW) >= full) break;
+    }
+  }
+  if (full < nb && wave == full % KW) {                 // the rows end inside this block
+    const int at = full * kQuantBlock;
+    const bool lo = at + 16 * g < K, hi = at + 64 + 16 * g < K;
+    const int4 zero = make_int4(0, 0, 0, 0);
+    Block r;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-      if (t < nt)
+    for (int m = 0; m < MR; ++m) {
+      r.w[m][0] = lo ? *reinterpret_cast<const int4*>(wrow[m] + at) : zero;
+      r.w[m][1] = hi ? *reinterpret_cast<const int4*>(wrow[m] + at + 64) : zero;
+    }
 #pragma unroll
-        for (int m = 0; m < MR; ++m) {
-          const floatx4 v = mfma128(w[m], x[t]);
-          const float s = sx[t] * (m < MW ? f1 : f3);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[m][t][i] = __builtin_fmaf(v[i], s, acc[m][t][i]);
-        }
+    for (int t = 0; t < NT; ++t) {
+      r.x[t][0] = lo ? *reinterpret_cast<const int4*>(xrow[t] + at) : zero;
+      r.x[t][1] = hi ? *reinterpret_cast<const int4*>(xrow[t] + at + 64) : zero;
+      r.sx[t] = srow[t][full];
+    }
+    r.f1 = f1[full];
+    if constexpr (kKind == kGateUp) r.f3 = f3[full];
+    add(r);
   }
   // lane (n, g) holds rows 4 g .. 4 g + 3 of weight tile m for token n of tile t
 #pragma unroll
@@ -300,11 +347,14 @@ __global__ __launch_bounds__(256) void product_kernel(Product a) {
     for (int m = 0; m < MR; ++m)
       *reinterpret_cast<floatx4*>(&red[wave][16 * t + n][16 * m + 4 * g]) = acc[m][t];
   __syncthreads();
-  for (int i = threadIdx.x; i < live * 16 * MW; i += 256) {
+  for (int i = threadIdx.x; i < live * 16 * MW; i += 64 * KW) {
     const int t = i / (16 * MW), c = i - t * 16 * MW;
     if (n0 + c >= N) continue;
     auto sum = [&](int col) {
-      return ((red[0][t][col] + red[1][t][col]) + red[2][t][col]) + red[3][t][col];
+      float s = red[0][t][col];
+#pragma unroll
+      for (int w = 1; w < KW; ++w) s += red[w][t][col];
+      return s;
     };
     const float v = sum(c);
     if constexpr (kKind == kLinear) {
@@ -329,7 +379,6 @@ __global__ __launch_bounds__(256) void product_kernel(Product a) {
 // source pieces in that order.
 __device__ const uint4 kZeroPiece = {0, 0, 0, 0};   // what lies past the end of a row
 
-typedef const __attribute__((address_space(4))) float* ScalarPtr;   // read by scalar loads
 typedef const __attribute__((address_space(1))) void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
@@ -588,13 +637,23 @@ hipError_t launch_tiles(const Product& a, int rows, int tiles, hipStream_t strea
   return launch_tile<kKind, 256, 64, 8, 1, 3>(a, tiles, stream);
 }
 
-template <Kind kKind>
+template <Kind kKind, int MR, int NT, int KW>
 hipError_t launch_product(const Product& a, int tiles, hipStream_t stream) {
-  constexpr int MR = 4;
   const int cols = 16 * (kKind == kGateUp ? MR / 2 : MR);
-  product_kernel<kKind, MR>
-      <<<dim3((a.N + cols - 1) / cols, tiles), 256, 0, stream>>>(a);
+  product_kernel<kKind, MR, NT, KW>
+      <<<dim3((a.N + cols - 1) / cols, tiles), 64 * KW, 0, stream>>>(a);
   return hipGetLastError();
+}
+
+// A product with few token rows: `tiles` tiles of 16 NT rows at most, `expect` of them live.
+template <Kind kKind, int NT>
+hipError_t launch_few(const Product& a, int tiles, int expect, hipStream_t stream) {
+  // weight rows in 16s, of both matrices
+  const long rows = (long)expect * ((a.N + 15) / 16) * (kKind == kGateUp ? 2 : 1);
+  constexpr int kLeast = kKind == kGateUp ? 2 : 1;
+  if (rows >= XS_FEW_4) return launch_product<kKind, 4, NT, 4>(a, tiles, stream);
+  if (rows >= XS_FEW_2) return launch_product<kKind, 2, NT, 8>(a, tiles, stream);
+  return launch_product<kKind, kLeast, NT, 16>(a, tiles, stream);
 }
 
 // ---------------------------------------------------------------------------- experts
@@ -705,15 +764,17 @@ hipError_t launch_block_linear(const BlockLinearArgs& a, hipStream_t stream) {
     return launch_tile<kLinear, 256, 256, 4, 2, 2>(p, (a.T + 255) / 256, stream);
   if (a.T > kTileRows)
     return launch_tile<kLinear, 256, 128, 8, 1, 3>(p, (a.T + 127) / 128, stream);
-  return launch_product<kLinear>(p, (a.T + kTileRows - 1) / kTileRows, stream);
+  return a.T > 16 ? launch_few<kLinear, 2>(p, (a.T + 31) / 32, (a.T + 31) / 32, stream)
+                  : launch_few<kLinear, 1>(p, 1, 1, stream);
 }
 
 hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   const int pairs = a.T * a.k;
   // rows of an expert with a pair, on average, if every expert has one
   const int mean = pairs / (pairs < a.E ? pairs : a.E);
-  const int rows = mean >= 160 ? 256 : mean >= 40 ? 128 : mean >= 12 ? 64 : kTileRows;
+  const int rows = mean >= 160 ? 256 : mean >= 40 ? 128 : mean >= 12 ? 64 : mean >= 6 ? 32 : 16;
   const int tiles = pair_tiles(pairs, a.E, rows);
+  const int expect = pairs < a.E ? pairs : a.E;
   hipError_t e = quantize_rows(a.x, a.T, a.d, a.ldx, a.xq, a.xs, nullptr, stream);
   if (e != hipSuccess) return e;
   index_kernel<<<a.E, 1024, 0, stream>>>(a.ids, pairs, a.E, rows, a.counts, a.perm, a.tiles);
@@ -734,8 +795,10 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   p.out = a.h;
   p.hq = a.hq;
   p.hs = a.hs;
-  if (rows == kTileRows) {
-    if ((e = launch_product<kGateUp>(p, tiles, stream)) != hipSuccess) return e;
+  if (rows <= 32) {
+    e = rows == 32 ? launch_few<kGateUp, 2>(p, tiles, expect, stream)
+                   : launch_few<kGateUp, 1>(p, tiles, expect, stream);
+    if (e != hipSuccess) return e;
     e = quantize_rows(a.h, pairs, a.f, a.f, a.hq, a.hs, a.counts, stream);
   } else {
     e = launch_tiles<kGateUp>(p, rows, tiles, stream);
@@ -748,8 +811,9 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   p.N = a.d;
   p.K = a.f;
   p.out = a.o;
-  e = rows == kTileRows ? launch_product<kDown>(p, tiles, stream)
-                        : launch_tiles<kDown>(p, rows, tiles, stream);
+  e = rows == 16   ? launch_few<kDown, 1>(p, tiles, expect, stream)
+      : rows == 32 ? launch_few<kDown, 2>(p, tiles, expect, stream)
+                   : launch_tiles<kDown>(p, rows, tiles, stream);
   if (e != hipSuccess) return e;
   combine_kernel<<<dim3(a.T, (a.d / 8 + 255) / 256), 256, 0, stream>>>(a.o, a.ids, a.w, a.k, a.E,
                                                                      a.d, a.y, a.ldy);
