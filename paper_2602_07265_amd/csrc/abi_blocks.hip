@@ -196,7 +196,8 @@ xshare_status xshare_block_experts(const xshare_block_experts_args* p) {
   a.xs = at<float>(p->ws, L.xs);
   a.counts = at<int32_t>(p->ws, L.counts);
   a.perm = at<int32_t>(p->ws, L.perm);
-  a.tiles = at<int4>(p->ws, L.tiles);
+  a.up_tiles = at<int4>(p->ws, L.up_tiles);
+  a.down_tiles = at<int4>(p->ws, L.down_tiles);
   a.h = at<float>(p->ws, L.h);
   a.hq = at<uint8_t>(p->ws, L.hq);
   a.hs = at<float>(p->ws, L.hs);

@@ -76,9 +76,10 @@ inline int pair_tiles(int pairs, int E, int tile_rows) {
 
 struct BlockExpertsLayout {
   size_t xq, xs;               // as BlockLinearLayout, of x [T, d]
-  size_t counts;               // int32 [4]: pairs, tiles
+  size_t counts;               // int32 [3]: pairs, tiles of gate/up, tiles of down
   size_t perm;                 // int32 [T * k] pair (t * k + r) of each row in expert order
-  size_t tiles;                // int4 [pair_tiles] {expert, first row, rows, 0}
+  size_t up_tiles;             // int4 [pair_tiles] {expert, first row, rows, 0} of gate/up
+  size_t down_tiles;           // and of down
   size_t h;                    // fp32 [T * k, f] hidden rows in expert order
   size_t hq, hs;               // their codes [T * k, f] and scales [T * k, ceil(f / 128)]
   size_t o;                    // fp32 [T * k, d] the pairs' outputs, by pair
@@ -92,7 +93,9 @@ inline BlockExpertsLayout block_experts_layout(int T, int k, int E, int d, int f
   L.xs = o;     o += align256(sizeof(float) * size_t(T) * quant_blocks(d));
   L.counts = o; o += 256;
   L.perm = o;   o += align256(sizeof(int32_t) * rows);
-  L.tiles = o;  o += align256(sizeof(int32_t) * 4 * size_t(pair_tiles(int(rows), E, kTileRows)));
+  const size_t tiles = align256(sizeof(int32_t) * 4 * size_t(pair_tiles(int(rows), E, kTileRows)));
+  L.up_tiles = o;   o += tiles;
+  L.down_tiles = o; o += tiles;
   L.h = o;      o += align256(sizeof(float) * rows * f);
   L.hq = o;     o += align256(rows * f);
   L.hs = o;     o += align256(sizeof(float) * rows * quant_blocks(f));
@@ -115,7 +118,8 @@ struct BlockExpertsArgs {
   float* xs;
   int32_t* counts;
   int32_t* perm;
-  int4* tiles;
+  int4* up_tiles;
+  int4* down_tiles;
   float* h;
   uint8_t* hq;
   float* hs;

@@ -17,13 +17,6 @@
 
 #include "blocks.h"
 
-#ifndef XS_FEW_4
-#define XS_FEW_4 4096
-#endif
-#ifndef XS_FEW_2
-#define XS_FEW_2 1024
-#endif
-
 namespace xs {
 namespace {
 
@@ -184,6 +177,8 @@ hipError_t quantize_rows(const In* x, long rows, int cols, long ld, uint8_t* q, 
 
 // ---------------------------------------------------------------------------- products
 
+constexpr int kUnits = 256;    // compute units of the GPU
+
 enum Kind { kLinear, kGateUp, kDown };
 
 struct Product {
@@ -197,7 +192,7 @@ struct Product {
   int rows;                    // kLinear: token rows
   int k;                       // pairs of a token
   const int4* tiles;           // kGateUp, kDown: {expert, first row, rows, 0}
-  const int32_t* counts;       // [1]: tiles
+  const int32_t* n_tiles;      // how many of them there are
   const int32_t* perm;         // pair of each row in expert order
   float* out;                  // kGateUp: h [row, N]; kDown: o [pair, N]
   uint8_t* hq;                 // kGateUp of the tiled kernel: the codes and scales of h
@@ -232,7 +227,7 @@ __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
     first = blockIdx.y * kRows;
     live = min(kRows, a.rows - first);
   } else {
-    if ((int)blockIdx.y >= a.counts[1]) return;
+    if ((int)blockIdx.y >= *a.n_tiles) return;
     const int4 t = a.tiles[blockIdx.y];
     first = t.y;
     live = t.z;
@@ -400,11 +395,18 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");   // no read of LDS moves above the barrier
 }
 
+constexpr int kScaleBlocks = 4;
+
+// LDS of the tiled kernel: kStages blocks of both operands, then two buffers of the scales of
+// kScaleBlocks blocks: the tokens' [BT][kScaleBlocks] and, one load's 64 floats, the weights'
+// [2][kScaleBlocks] (kGateUp: W1's and W3's; else the first 128 rows' and the next ones').
 template <int BW, int BT, int kStages>
 struct TileLds {
-  static constexpr int kScales = BT < 64 ? 64 : BT;
-  static constexpr int kStage = (BW + BT) * kQuantBlock + kScales * 4;
-  static constexpr int kBytes = kStages * kStage;
+  static constexpr int kStage = (BW + BT) * kQuantBlock;
+  static constexpr int kScales = kStages * kStage;
+  static constexpr int kTokenFloats = BT * kScaleBlocks;
+  static constexpr int kScaleBytes = (kTokenFloats + 64) * 4;
+  static constexpr int kBytes = kScales + 2 * kScaleBytes;
 };
 
 template <Kind kKind, int BW, int BT, int WW, int WT, int kStages>
@@ -414,9 +416,14 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
   constexpr int MW = BW / WW / 16, TT = BT / WT / 16;
   constexpr int kRows = kThreads / 8;                       // rows of one load of the workgroup
   constexpr int LW = BW / kRows, LT = BT >= kRows ? BT / kRows : 1;
-  constexpr int kLoads = LW + LT + 1;                       // of a wave and stage
-  constexpr int kUnits = kKind == kGateUp ? BW / 2 : BW;    // output columns of a workgroup
-  constexpr int kGroup = BT >= 256 ? TT : 2;                // token tiles worked on together
+  constexpr int kLoads = LW + LT;                           // of a wave and stage
+  constexpr int kScaleLoads = BT / 16 > WW * WT ? BT / 16 / (WW * WT) : 1;   // and chunk of scales
+  constexpr int kCols = kKind == kGateUp ? BW / 2 : BW;    // output columns of a workgroup
+  // token tiles worked on together; where a workgroup's tokens may be few, the rest is skipped
+  constexpr int kGroup = BT >= 256 ? TT : 2;
+  static_assert(TT % kGroup == 0, "whole groups");
+  constexpr int kLead = kStages > 3 ? kStages - 2 : 1;
+  static_assert(kLead <= kScaleBlocks, "two buffers of scales");
   static_assert(kKind != kGateUp || MW % 2 == 0, "W1 and W3 tiles in pairs");
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -432,7 +439,7 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
     first = blockIdx.y * BT;
     live = min(BT, a.rows - first);
   } else {
-    if ((int)blockIdx.y >= a.counts[1]) return;
+    if ((int)blockIdx.y >= *a.n_tiles) return;
     const int4 t = a.tiles[blockIdx.y];
     first = t.y;
     live = t.z;
@@ -444,7 +451,7 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
       s3 += (size_t)e * nbN * nb;
     }
   }
-  const int n0 = blockIdx.x * kUnits;
+  const int n0 = blockIdx.x * kCols;
   // LDS row R of the weights: tile (R / 16) % MW of wave R / (16 MW) along the weight rows
   const uint8_t* wsrc[LW];
   const int piece = 16 * ((lane & 7) ^ (((tid >> 3) >> 1) & 7));
@@ -467,31 +474,42 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
     const int r = kKind == kGateUp ? a.perm[p] / a.k : p;
     xsrc[j] = a.xq + (size_t)r * K + piece;
   }
-  const float* ssrc;
-  {
-    const int p = first + min(((wave * 64) % L::kScales) + lane, live - 1);
+  // lane l of a load of scales takes block l % 4 of token l / 4
+  const float* ssrc[kScaleLoads];
+  uint32_t sdst[kScaleLoads];
+#pragma unroll
+  for (int j = 0; j < kScaleLoads; ++j) {
+    const int t0 = ((wave + j * WW * WT) * 16) % BT;
+    const int p = first + min(t0 + lane / kScaleBlocks, live - 1);
     const int r = kKind == kGateUp ? a.perm[p] / a.k : p;
-    ssrc = a.xs + (size_t)r * nb;
+    ssrc[j] = a.xs + (size_t)r * nb;
+    sdst[j] = L::kScales + t0 * kScaleBlocks * 4;
   }
-  auto load = [&](int b, uint8_t* stage) {
+  // the i-th of a wave's loads of block b
+  auto load = [&](int b, uint8_t* stage, int i) {
     const int at = b * kQuantBlock;
     const bool out = at + piece >= K;      // past the end of a last, partial block
-#pragma unroll
-    for (int j = 0; j < LW; ++j)
-      to_lds16(wsrc[j] + at, out,
-               stage + (j * kRows + wave * 8) * kQuantBlock);
-#pragma unroll
-    for (int j = 0; j < LT; ++j)
-      to_lds16(xsrc[j] + at, out,
-               stage + (BW + (j * kRows + wave * 8) % BT) * kQuantBlock);
-    to_lds4(ssrc + b,
-            reinterpret_cast<float*>(stage + (BW + BT) * kQuantBlock) + (wave * 64) % L::kScales);
+    if (i < LW)
+      to_lds16(wsrc[i < LW ? i : 0] + at, out, stage + (i * kRows + wave * 8) * kQuantBlock);
+    else
+      to_lds16(xsrc[i < LW ? 0 : i - LW] + at, out,
+               stage + (BW + ((i - LW) * kRows + wave * 8) % BT) * kQuantBlock);
   };
-  // a wave's weight rows share one scale a block (two with kGateUp)
+  const int n_block = n0 / kQuantBlock;
+  const float* const fsrc =
+      kKind == kGateUp ? (lane / kScaleBlocks % 2 ? s3 : s1) + (size_t)n_block * nb
+                       : s1 + (size_t)min(n_block + lane / kScaleBlocks % 2, nbN - 1) * nb;
+  auto load_scales = [&](int b) {          // of blocks b .. b + 3, b a multiple of four
+    const int at = min(b + lane % kScaleBlocks, nb - 1);
+    const int buffer = (b / kScaleBlocks & 1) * L::kScaleBytes;
+#pragma unroll
+    for (int j = 0; j < kScaleLoads; ++j)
+      to_lds4(ssrc[j] + at, reinterpret_cast<float*>(lds + sdst[j] + buffer));
+    to_lds4(fsrc + at,
+            reinterpret_cast<float*>(lds + L::kScales + buffer) + L::kTokenFloats);
+  };
+  // first output column of the wave; its weight rows lie in one block of 128 (of each matrix)
   const int u0 = n0 + ww * (kKind == kGateUp ? 8 * MW : 16 * MW);
-  const size_t srow = (size_t)min(u0 / kQuantBlock, nbN - 1) * nb;
-  const ScalarPtr f1 = (ScalarPtr)(s1 + srow);
-  const ScalarPtr f3 = kKind == kGateUp ? (ScalarPtr)(s3 + srow) : f1;
   const int nt = (live - wt * 16 * TT + 15) / 16;      // live tiles of this wave, at most TT
   floatx4 acc[MW][TT];
 #pragma unroll
@@ -506,56 +524,87 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
     const int4 v = *reinterpret_cast<const int4*>(row + hi);
     return i32x8{u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
   };
+  load_scales(0);
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s)
-    if (s < nb) load(s, lds + s * L::kStage);
-  // Block b from its buffer while a later block's loads fill another.  The two pointers are
-  // declared apart: without that every read of LDS would wait for every load in flight.
-  auto step = [&](int b, const uint8_t* __restrict__ stage, uint8_t* __restrict__ next) {
-    if (b + kStages - 1 < nb) load(b + kStages - 1, next);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(min(s, nb - 1), lds + s * L::kStage, i);
+  // Block b from its buffer while a later block's loads fill another.  The order is written
+  // out and held: the loads go between the matrix instructions (at the step's start, all waves
+  // at once, they would hold up the reads of LDS), a token tile's operand is read while the
+  // tile before it is worked on, and an instruction's result enters its accumulator two
+  // instructions later.  The pointers are declared apart: without that every read of LDS
+  // would wait for every load in flight.
+  auto step = [&](int b, const uint8_t* __restrict__ stage, const float* __restrict__ scales,
+                  uint8_t* __restrict__ next) {
+    const int ahead = min(b + kStages - 1, nb - 1);    // (past the end: block nb - 1 again)
     const uint8_t* const wl = stage + (ww * 16 * MW + n) * kQuantBlock;
     const uint8_t* const xl = stage + (BW + wt * 16 * TT + n) * kQuantBlock;
-    const float* const sl =
-        reinterpret_cast<const float*>(stage + (BW + BT) * kQuantBlock) + wt * 16 * TT + n;
-    const float fw1 = f1[b], fw3 = f3[b];
-    i32x8 w[MW];
+    const float* const sl = scales + (wt * 16 * TT + n) * kScaleBlocks + b % kScaleBlocks;
+    const float* const fl = scales + L::kTokenFloats + b % kScaleBlocks;
+    auto load_share = [&](int i) {                     // the loads before instruction i
+#pragma unroll
+      for (int l = (i * kLoads + MW * TT - 1) / (MW * TT); l * MW * TT < (i + 1) * kLoads; ++l)
+        load(ahead, next, l);
+    };
+    i32x8 w[MW], x[2];
+    float sx[TT];
+    x[0] = operand(xl);
 #pragma unroll
     for (int m = 0; m < MW; ++m) w[m] = operand(wl + 16 * m * kQuantBlock);
-    // token tiles in groups, so that what waits in one tile has the others' work to hide it
+    const float fw1 = kKind == kGateUp ? fl[0] : fl[(u0 / kQuantBlock - n_block) * kScaleBlocks];
+    const float fw3 = kKind == kGateUp ? fl[kScaleBlocks] : fw1;
+#pragma unroll
+    for (int t = 0; t < TT; ++t) sx[t] = sl[16 * t * kScaleBlocks];
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int t0 = 0; t0 < TT; t0 += kGroup) {
-      if (t0 >= nt) break;
+      if (kGroup < TT && t0 >= nt) {                   // no tokens here: the loads alone
 #pragma unroll
-      for (int t = t0; t < t0 + kGroup; ++t) {
-        const i32x8 x = operand(xl + 16 * t * kQuantBlock);
-        const float sx = sl[16 * t];
-#pragma unroll
-        for (int m = 0; m < MW; ++m) {
-          const floatx4 v = mfma128(w[m], x);
-          const float s = sx * (kKind == kGateUp && m >= MW / 2 ? fw3 : fw1);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[m][t][i] = __builtin_fmaf(v[i], s, acc[m][t][i]);
-        }
+        for (int i = t0 * MW; i < (t0 + kGroup) * MW; ++i) load_share(i);
+        continue;
       }
+      floatx4 v[3];
+      auto enter = [&](int i) {
+        const int t = t0 + i / MW, m = i % MW;
+        const float s = sx[t] * (kKind == kGateUp && m >= MW / 2 ? fw3 : fw1);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          acc[m][t][c] = __builtin_fmaf(v[i % 3][c], s, acc[m][t][c]);
+      };
+#pragma unroll
+      for (int i = 0; i < kGroup * MW; ++i) {
+        const int t = t0 + i / MW, m = i % MW, at = t0 * MW + i;
+        if (m == 0 && t + 1 < TT) x[(t + 1) & 1] = operand(xl + 16 * (t + 1) * kQuantBlock);
+        load_share(at);
+        v[i % 3] = mfma128(w[m], x[t & 1]);
+        if (i >= 2) enter(i - 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      enter(kGroup * MW - 2);
+      enter(kGroup * MW - 1);
     }
   };
   int cur = 0;                                         // the buffer of block b
   for (int b = 0; b < nb; ++b) {
-    // the loads of this block are done; those of the kStages - 2 after it may be in flight
-    if (b + kStages - 2 < nb)
-      wait_loads<kLoads*(kStages - 2)>();
-    else
-      wait_loads<0>();
-    step(b, lds + cur * L::kStage, lds + (cur == 0 ? kStages - 1 : cur - 1) * L::kStage);
+    // The loads of this block are done; those of the kStages - 2 after it may be in flight.
+    // A chunk of scales is loaded kLead steps before its first block, so that it is older than
+    // any load that may be in flight then; its buffer was last read the step before, or earlier.
+    wait_loads<kLoads*(kStages - 2)>();
+    if ((b + kLead) % kScaleBlocks == 0 && b + kLead < nb) load_scales(b + kLead);
+    step(b, lds + cur * L::kStage,
+         reinterpret_cast<const float*>(lds + L::kScales +
+                                        (b / kScaleBlocks & 1) * L::kScaleBytes),
+         lds + (cur == 0 ? kStages - 1 : cur - 1) * L::kStage);
     cur = cur + 1 == kStages ? 0 : cur + 1;
   }
+  wait_loads<0>();                                     // LDS is free
 
   // lane (n, g) holds units 4 g .. 4 g + 3 of weight tile m for token n of tile t
   if constexpr (kKind == kGateUp) {
     constexpr int MH = MW / 2;
-    __syncthreads();                                   // the last block's reads of LDS
     uint32_t* const part = reinterpret_cast<uint32_t*>(lds);   // [WW][BT] maxima
-    static_assert(kUnits == kQuantBlock, "a workgroup holds one block of the hidden row");
+    static_assert(kCols == kQuantBlock, "a workgroup holds one block of the hidden row");
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       uint32_t m = 0;
@@ -630,13 +679,6 @@ hipError_t launch_tile(const Product& a, int tiles, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <Kind kKind>
-hipError_t launch_tiles(const Product& a, int rows, int tiles, hipStream_t stream) {
-  if (rows == 256) return launch_tile<kKind, 256, 256, 4, 2, 2>(a, tiles, stream);
-  if (rows == 128) return launch_tile<kKind, 256, 128, 8, 1, 3>(a, tiles, stream);
-  return launch_tile<kKind, 256, 64, 8, 1, 3>(a, tiles, stream);
-}
-
 template <Kind kKind, int MR, int NT, int KW>
 hipError_t launch_product(const Product& a, int tiles, hipStream_t stream) {
   const int cols = 16 * (kKind == kGateUp ? MR / 2 : MR);
@@ -645,28 +687,43 @@ hipError_t launch_product(const Product& a, int tiles, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// A product with few token rows: `tiles` tiles of 16 NT rows at most, `expect` of them live.
-template <Kind kKind, int NT>
-hipError_t launch_few(const Product& a, int tiles, int expect, hipStream_t stream) {
-  // weight rows in 16s, of both matrices
-  const long rows = (long)expect * ((a.N + 15) / 16) * (kKind == kGateUp ? 2 : 1);
-  constexpr int kLeast = kKind == kGateUp ? 2 : 1;
-  if (rows >= XS_FEW_4) return launch_product<kKind, 4, NT, 4>(a, tiles, stream);
-  if (rows >= XS_FEW_2) return launch_product<kKind, 2, NT, 8>(a, tiles, stream);
-  return launch_product<kKind, kLeast, NT, 16>(a, tiles, stream);
-}
+// The forms of y = x W^T: weight rows and tokens of a workgroup, and what a block of 128 inputs
+// costs it in microseconds where the GPU's 256 compute units each run one (measured from 64 to
+// 4000 tokens and 200 to 14336 weight rows; a launch takes about 2.5 us more).  The product's
+// time is that times the workgroups a compute unit has to run after each other: several
+// workgroups of the few-row forms share a unit without gaining by it, the tiled forms' LDS
+// leaves room for one.
+struct LinearForm {
+  int rows, tokens;
+  float cost;
+  hipError_t (*launch)(const Product&, int, hipStream_t);
+};
+const LinearForm kLinearForms[] = {
+    {16, 16, 0.136f, launch_product<kLinear, 1, 1, 4>},
+    {32, 16, 0.195f, launch_product<kLinear, 2, 1, 4>},
+    {64, 16, 0.32f, launch_product<kLinear, 4, 1, 4>},
+    {16, 32, 0.225f, launch_product<kLinear, 1, 2, 4>},
+    {32, 32, 0.29f, launch_product<kLinear, 2, 2, 4>},
+    {64, 64, 0.33f, launch_tile<kLinear, 64, 64, 2, 2, 6>},
+    {128, 64, 0.42f, launch_tile<kLinear, 128, 64, 4, 2, 5>},
+    {128, 128, 0.67f, launch_tile<kLinear, 128, 128, 2, 4, 4>},
+    {256, 128, 1.13f, launch_tile<kLinear, 256, 128, 2, 4, 3>},
+    {256, 256, 2.1f, launch_tile<kLinear, 256, 256, 2, 4, 2>},
+};
 
 // ---------------------------------------------------------------------------- experts
 
 // The pairs in expert order: one workgroup an expert, each over all ids.  It counts the pairs
 // of every expert (in LDS) and, wave by wave, its own; its rows begin after those of the
-// experts before it, its tiles likewise, and its pairs are listed in ascending order.
+// experts before it, its tiles of either product likewise, and its pairs are listed in
+// ascending order.
 __global__ __launch_bounds__(1024) void index_kernel(const int32_t* ids, int pairs, int E,
-                                                     int tile_rows, int32_t* counts,
-                                                     int32_t* perm, int4* tiles) {
+                                                     int up_rows, int down_rows,
+                                                     int32_t* counts, int32_t* perm,
+                                                     int4* up_tiles, int4* down_tiles) {
   __shared__ int count[kMaxExperts];
   __shared__ int mine[16];
-  __shared__ int sum_rows[16], sum_tiles[16];
+  __shared__ int sums[3][16];
   const int e = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   count[tid] = 0;
   __syncthreads();
@@ -681,33 +738,34 @@ __global__ __launch_bounds__(1024) void index_kernel(const int32_t* ids, int pai
   }
   if (lane == 0) mine[wave] = own;
   __syncthreads();
-  // rows and tiles of the experts before e, and of all
-  const int c = tid < E ? count[tid] : 0;
-  const int tl = (c + tile_rows - 1) / tile_rows;
-  int before = tid < e ? c : 0, before_t = tid < e ? tl : 0;
+  // rows and tiles of the experts before e
+  auto tiles_of = [](int rows, int tile) { return (rows + tile - 1) / tile; };
+  const int c = tid < e ? count[tid] : 0;
+  int before[3] = {c, tiles_of(c, up_rows), tiles_of(c, down_rows)};
 #pragma unroll
-  for (int s = 1; s < 64; s *= 2) {
-    before += __shfl_xor(before, s);
-    before_t += __shfl_xor(before_t, s);
-  }
-  if (lane == 0) {
-    sum_rows[wave] = before;
-    sum_tiles[wave] = before_t;
+  for (int i = 0; i < 3; ++i) {
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) before[i] += __shfl_xor(before[i], s);
+    if (lane == 0) sums[i][wave] = before[i];
   }
   __syncthreads();
-  int row0 = 0, tile0 = 0, at = 0;
+  int row0 = 0, up0 = 0, down0 = 0, at = 0;
   for (int w = 0; w < 16; ++w) {
-    row0 += sum_rows[w];
-    tile0 += sum_tiles[w];
+    row0 += sums[0][w];
+    up0 += sums[1][w];
+    down0 += sums[2][w];
     if (w < wave) at += mine[w];
   }
   const int n = count[e];
   if (e == E - 1 && tid == 0) {
     counts[0] = row0 + n;
-    counts[1] = tile0 + (n + tile_rows - 1) / tile_rows;
+    counts[1] = up0 + tiles_of(n, up_rows);
+    counts[2] = down0 + tiles_of(n, down_rows);
   }
-  for (int i = tid * tile_rows; i < n; i += 1024 * tile_rows)
-    tiles[tile0 + i / tile_rows] = make_int4(e, row0 + i, min(tile_rows, n - i), 0);
+  for (int i = tid * up_rows; i < n; i += 1024 * up_rows)
+    up_tiles[up0 + i / up_rows] = make_int4(e, row0 + i, min(up_rows, n - i), 0);
+  for (int i = tid * down_rows; i < n; i += 1024 * down_rows)
+    down_tiles[down0 + i / down_rows] = make_int4(e, row0 + i, min(down_rows, n - i), 0);
   for (int i = from; i < to; i += 64) {
     const bool hit = i + lane < to && ids[i + lane] == e;
     const uint64_t hits = __ballot(hit);
@@ -760,24 +818,38 @@ hipError_t launch_block_linear(const BlockLinearArgs& a, hipStream_t stream) {
   p.rows = a.T;
   p.y = a.y;
   p.ldy = a.ldy;
-  if (a.T > 128)
-    return launch_tile<kLinear, 256, 256, 4, 2, 2>(p, (a.T + 255) / 256, stream);
-  if (a.T > kTileRows)
-    return launch_tile<kLinear, 256, 128, 8, 1, 3>(p, (a.T + 127) / 128, stream);
-  return a.T > 16 ? launch_few<kLinear, 2>(p, (a.T + 31) / 32, (a.T + 31) / 32, stream)
-                  : launch_few<kLinear, 1>(p, 1, 1, stream);
+  const LinearForm* best = nullptr;
+  float least = 0.0f;
+  for (const LinearForm& f : kLinearForms) {
+    const long groups = long((a.n + f.rows - 1) / f.rows) * ((a.T + f.tokens - 1) / f.tokens);
+    const float cost = f.cost * float((groups + kUnits - 1) / kUnits);
+    if (!best || cost < least) {
+      best = &f;
+      least = cost;
+    }
+  }
+  return best->launch(p, (a.T + best->tokens - 1) / best->tokens, stream);
 }
 
 hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   const int pairs = a.T * a.k;
-  // rows of an expert with a pair, on average, if every expert has one
-  const int mean = pairs / (pairs < a.E ? pairs : a.E);
-  const int rows = mean >= 160 ? 256 : mean >= 40 ? 128 : mean >= 12 ? 64 : mean >= 6 ? 32 : 16;
-  const int tiles = pair_tiles(pairs, a.E, rows);
-  const int expect = pairs < a.E ? pairs : a.E;
+  // Rows of an expert on average, if as many experts as can be have a pair.  From 12 rows on
+  // tiles of 128 tokens cost no more than narrower ones (their empty 32s are skipped) and read
+  // the weights of nearly every expert once; below, tiles of 32 have less to load.  The tiled
+  // form wants a workgroup for most compute units: one token of eight (2048, 768) experts has 48
+  // in gate/up and takes 13 us in it, 8 in the few-row form; down of two (4096, 14336) experts
+  // has 32, 53 against 21 us; eight of them with 16 rows 128, 105 in the form of 256 x 128
+  // against 85 in that of 128 x 64.
+  const int expect = pairs < a.E ? pairs : a.E, mean = pairs / expect;
+  const int wide = mean >= 12 ? 128 : 32;
+  const long spans = (mean + wide - 1) / wide;
+  const bool few_up = mean <= 16 && long(expect) * ((a.f + 127) / 128) < 96;
+  const bool few_groups = long(expect) * spans * ((a.d + 255) / 256) < 192;
+  const int up_rows = few_up ? 16 : wide, down_rows = !few_groups ? wide : mean <= 8 ? 16 : 64;
   hipError_t e = quantize_rows(a.x, a.T, a.d, a.ldx, a.xq, a.xs, nullptr, stream);
   if (e != hipSuccess) return e;
-  index_kernel<<<a.E, 1024, 0, stream>>>(a.ids, pairs, a.E, rows, a.counts, a.perm, a.tiles);
+  index_kernel<<<a.E, 1024, 0, stream>>>(a.ids, pairs, a.E, up_rows, down_rows, a.counts, a.perm,
+                                         a.up_tiles, a.down_tiles);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   Product p{};
   p.xq = a.xq;
@@ -789,19 +861,19 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   p.N = a.f;
   p.K = a.d;
   p.k = a.k;
-  p.tiles = a.tiles;
-  p.counts = a.counts;
+  p.tiles = a.up_tiles;
+  p.n_tiles = a.counts + 1;
   p.perm = a.perm;
   p.out = a.h;
   p.hq = a.hq;
   p.hs = a.hs;
-  if (rows <= 32) {
-    e = rows == 32 ? launch_few<kGateUp, 2>(p, tiles, expect, stream)
-                   : launch_few<kGateUp, 1>(p, tiles, expect, stream);
-    if (e != hipSuccess) return e;
+  const int up = pair_tiles(pairs, a.E, up_rows), down = pair_tiles(pairs, a.E, down_rows);
+  if (few_up) {
+    if ((e = launch_product<kGateUp, 2, 1, 4>(p, up, stream)) != hipSuccess) return e;
     e = quantize_rows(a.h, pairs, a.f, a.f, a.hq, a.hs, a.counts, stream);
   } else {
-    e = launch_tiles<kGateUp>(p, rows, tiles, stream);
+    e = wide == 32 ? launch_tile<kGateUp, 256, 32, 8, 1, 4>(p, up, stream)
+                   : launch_tile<kGateUp, 256, 128, 4, 2, 3>(p, up, stream);
   }
   if (e != hipSuccess) return e;
   p.xq = a.hq;
@@ -810,10 +882,15 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   p.s1 = a.s2;
   p.N = a.d;
   p.K = a.f;
+  p.tiles = a.down_tiles;
+  p.n_tiles = a.counts + 2;
   p.out = a.o;
-  e = rows == 16   ? launch_few<kDown, 1>(p, tiles, expect, stream)
-      : rows == 32 ? launch_few<kDown, 2>(p, tiles, expect, stream)
-                   : launch_tiles<kDown>(p, rows, tiles, stream);
+  if (few_groups)
+    e = mean <= 8 ? launch_product<kDown, 2, 1, 4>(p, down, stream)
+                  : launch_tile<kDown, 128, 64, 4, 2, 5>(p, down, stream);
+  else
+    e = wide == 32 ? launch_tile<kDown, 256, 32, 8, 1, 4>(p, down, stream)
+                   : launch_tile<kDown, 256, 128, 4, 2, 3>(p, down, stream);
   if (e != hipSuccess) return e;
   combine_kernel<<<dim3(a.T, (a.d / 8 + 255) / 256), 256, 0, stream>>>(a.o, a.ids, a.w, a.k, a.E,
                                                                      a.d, a.y, a.ldy);
