@@ -20,6 +20,7 @@
 #include <algorithm>
 
 #include "internal.h"
+#include "wave.h"
 
 namespace xs {
 namespace {
@@ -57,46 +58,6 @@ __device__ __forceinline__ float exp_fixed(float x) {
   p = p * r + 1.0f;
   p = p * r + 1.0f;
   return ldexpf(p, (int)n);
-}
-
-// Order-preserving map of finite fp32 values to uint32 (> 0); 0 marks "no value".
-__device__ __forceinline__ uint32_t ord(float h) {
-  const uint32_t b = __float_as_uint(h);
-  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-}
-__device__ __forceinline__ float unord(uint32_t k) {
-  return __uint_as_float((k & 0x80000000u) ? (k & 0x7FFFFFFFu) : ~k);
-}
-
-// One DPP step of a reduction: the value of the lane that Ctrl names, or the reduction's
-// identity in rows outside RowMask.  With the identity as the "old" operand the compiler
-// folds the move into the reducing instruction (one v_max_u32_dpp / v_min_u32_dpp per step
-// instead of two moves and the max).
-template <int Ctrl, int RowMask, uint32_t Identity>
-__device__ __forceinline__ uint32_t dpp(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp((int)Identity, (int)v, Ctrl, RowMask, 0xF, false);
-}
-
-// Wave-wide max / min of a uint32 with DPP (quad swaps, row mirrors, row broadcasts);
-// lane 63 ends with the result, which is returned to every lane.
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-  v = max(v, dpp<0xB1, 0xF, 0u>(v));   // quad_perm [1,0,3,2]
-  v = max(v, dpp<0x4E, 0xF, 0u>(v));   // quad_perm [2,3,0,1]
-  v = max(v, dpp<0x141, 0xF, 0u>(v));  // row_half_mirror
-  v = max(v, dpp<0x140, 0xF, 0u>(v));  // row_mirror
-  v = max(v, dpp<0x142, 0xA, 0u>(v));  // row_bcast:15
-  v = max(v, dpp<0x143, 0xC, 0u>(v));  // row_bcast:31
-  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
-__device__ __forceinline__ uint32_t wave_min(uint32_t v) {
-  constexpr uint32_t kId = 0xFFFFFFFFu;
-  v = min(v, dpp<0xB1, 0xF, kId>(v));
-  v = min(v, dpp<0x4E, 0xF, kId>(v));
-  v = min(v, dpp<0x141, 0xF, kId>(v));
-  v = min(v, dpp<0x140, 0xF, kId>(v));
-  v = min(v, dpp<0x142, 0xA, kId>(v));
-  v = min(v, dpp<0x143, 0xC, kId>(v));
-  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 __device__ __forceinline__ float lane_value(float v, int lane) {

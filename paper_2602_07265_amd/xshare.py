@@ -905,9 +905,23 @@ def _rows(t, dtype, name, cols=None):
 
 
 def _same_device(x, *others):
+    at = x.device
     for t in others:
-        if t is not None and t.device != x.device:
-            raise ValueError(f"tensors on {x.device} and {t.device}")
+        if t is not None and t.device != at:
+            raise ValueError(f"tensors on {at} and {t.device}")
+
+
+# The handle of a device's current stream without a Stream object (3 us less a call, of about
+# 8 that the shortest of these calls take).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(x, stream):
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream(x.device).cuda_stream
+    return _raw_stream(x.device.index)
 
 
 def _gate_params(N, top_k, score, n_groups, top_groups, group_score, renormalize, scale):
@@ -934,18 +948,20 @@ def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_grou
     k = int(top_k)
     if bias is not None:
         _dev(bias, torch.float32, (N,), "bias")
-    out = {} if out is None else out
-    ids, w = out.get("ids"), out.get("w")
+        _same_device(logits, bias)
+    ids, w = (None, None) if out is None else (out.get("ids"), out.get("w"))
     if ids is None:
-        ids = torch.empty((T, max(k, 0)), dtype=torch.int32, device=logits.device)
+        ids = logits.new_empty((T, max(k, 0)), dtype=torch.int32)
+    else:
+        _same_device(logits, _dev(ids, torch.int32, (T, k), "ids"))
     if w is None:
-        w = torch.empty((T, max(k, 0)), dtype=torch.float32, device=logits.device)
-    _dev(ids, torch.int32, (T, k), "ids")
-    _dev(w, torch.float32, (T, k), "w")
-    _same_device(logits, bias, ids, w)
+        w = logits.new_empty((T, max(k, 0)), dtype=torch.float32)
+    else:
+        _same_device(logits, _dev(w, torch.float32, (T, k), "w"))
     p = _gate_params(N, k, score, n_groups, top_groups, group_score, renormalize, scale)
-    st = lib().xshare_gate(_ptr(logits), dtype, T, ld, _ptr(bias), ctypes.byref(p), _ptr(ids),
-                           _ptr(w), _stream(stream))
+    st = lib().xshare_gate(logits.data_ptr(), dtype, T, ld,
+                           None if bias is None else bias.data_ptr(), ctypes.byref(p),
+                           ids.data_ptr(), w.data_ptr(), _stream_of(logits, stream))
     _check(st, "xshare_gate")
     return dict(ids=ids, w=w)
 
@@ -961,12 +977,14 @@ def gate_backward(logits: torch.Tensor, ids: torch.Tensor, dw: torch.Tensor, *, 
     _dev(ids, torch.int32, (T, k), "ids")
     _dev(dw, torch.float32, (T, k), "dw")
     if out is None:
-        out = torch.empty((T, N), dtype=torch.float32, device=logits.device)
-    _dev(out, torch.float32, (T, N), "out")
+        out = logits.new_empty((T, N), dtype=torch.float32)
+    else:
+        _dev(out, torch.float32, (T, N), "out")
     _same_device(logits, ids, dw, out)
     p = _gate_params(N, k, score, 1, 1, "max", renormalize, scale)
-    st = lib().xshare_gate_backward(_ptr(logits), dtype, T, ld, ctypes.byref(p), _ptr(ids),
-                                    _ptr(dw), _ptr(out), _stream(stream))
+    st = lib().xshare_gate_backward(logits.data_ptr(), dtype, T, ld, ctypes.byref(p),
+                                    ids.data_ptr(), dw.data_ptr(), out.data_ptr(),
+                                    _stream_of(logits, stream))
     _check(st, "xshare_gate_backward")
     return out
 
@@ -984,14 +1002,15 @@ def block_quantize(x: torch.Tensor, block_rows: int = 1, *, out=None, stream=Non
     shape = (-(-rows // step), _blocks(cols))
     q, s = (None, None) if out is None else out
     if q is None:
-        q = torch.empty((rows, cols), dtype=torch.uint8, device=x.device)
+        q = x.new_empty((rows, cols), dtype=torch.uint8)
+    else:
+        _same_device(x, _dev(q, torch.uint8, (rows, cols), "codes"))
     if s is None:
-        s = torch.empty(shape, dtype=torch.float32, device=x.device)
-    _dev(q, torch.uint8, (rows, cols), "codes")
-    _dev(s, torch.float32, shape, "scales")
-    _same_device(x, q, s)
-    st = lib().xshare_block_quantize(_ptr(x), rows, cols, ld, int(block_rows), _ptr(q), _ptr(s),
-                                     _stream(stream))
+        s = x.new_empty(shape, dtype=torch.float32)
+    else:
+        _same_device(x, _dev(s, torch.float32, shape, "scales"))
+    st = lib().xshare_block_quantize(x.data_ptr(), rows, cols, ld, int(block_rows), q.data_ptr(),
+                                     s.data_ptr(), _stream_of(x, stream))
     _check(st, "xshare_block_quantize")
     return q, s
 
@@ -1019,19 +1038,23 @@ def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale
         _dev(x_scale, torch.float32, (x.shape[0], _blocks(k)), "x_scale")
     T = x.shape[0]
     if y is None:
-        y = torch.empty((T, n), dtype=torch.bfloat16, device=x.device)
-    ldy = _rows(y, torch.bfloat16, "y", n)
-    if y.shape[0] != T:
-        raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
-    _same_device(x, wq, ws, x_scale, y, workspace)
-    need = 0 if x_scale is not None else block_linear_workspace_bytes(T, n, k)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        y, ldy = x.new_empty((T, n), dtype=torch.bfloat16), n
+    else:
+        ldy = _rows(y, torch.bfloat16, "y", n)
+        if y.shape[0] != T:
+            raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
     own = x_scale is None
-    st = lib().xshare_block_linear(_ptr(x) if own else None, ldx, None if own else _ptr(x),
-                                   _ptr(x_scale), T, n, k, _ptr(wq), _ptr(ws), _ptr(y), ldy,
-                                   _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                                   _stream(stream))
+    if workspace is None and own:
+        workspace = x.new_empty(lib().xshare_block_linear_workspace_bytes(T, n, k),
+                                dtype=torch.uint8)
+    _same_device(x, wq, ws, x_scale, y, workspace)
+    px = x.data_ptr()
+    st = lib().xshare_block_linear(px if own else None, ldx, None if own else px,
+                                   None if own else x_scale.data_ptr(), T, n, k, wq.data_ptr(),
+                                   ws.data_ptr(), y.data_ptr(), ldy,
+                                   None if workspace is None else workspace.data_ptr(),
+                                   0 if workspace is None else workspace.numel(),
+                                   _stream_of(x, stream))
     _check(st, "xshare_block_linear")
     return y
 
@@ -1063,19 +1086,20 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
     _dev(s3, torch.float32, (N, _blocks(f), _blocks(d)), "w3 scales")
     _dev(s2, torch.float32, (N, _blocks(d), _blocks(f)), "w2 scales")
     if y is None:
-        y = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
-    ldy = _rows(y, torch.bfloat16, "y", d)
-    if y.shape[0] != T:
-        raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
-    _same_device(x, ids, w, q1, q3, q2, s1, s3, s2, y, workspace)
+        y, ldy = x.new_empty((T, d)), d
+    else:
+        ldy = _rows(y, torch.bfloat16, "y", d)
+        if y.shape[0] != T:
+            raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
     if workspace is None:
-        workspace = torch.empty(max(block_experts_workspace_bytes(T, k, N, d, f), 256),
-                                dtype=torch.uint8, device=x.device)
+        workspace = x.new_empty(lib().xshare_block_experts_workspace_bytes(T, k, N, d, f),
+                                dtype=torch.uint8)
+    _same_device(x, ids, w, q1, q3, q2, s1, s3, s2, y, workspace)
     a = BlockExpertsArgs(ctypes.sizeof(BlockExpertsArgs), T, k, N, d, f, x.data_ptr(), ldx,
                          ids.data_ptr(), w.data_ptr(), q1.data_ptr(), q3.data_ptr(),
                          q2.data_ptr(), s1.data_ptr(), s3.data_ptr(), s2.data_ptr(),
                          y.data_ptr(), ldy, workspace.data_ptr(), workspace.numel(),
-                         _stream(stream))
+                         _stream_of(x, stream))
     _check(lib().xshare_block_experts(ctypes.byref(a)), "xshare_block_experts")
     return y
 
