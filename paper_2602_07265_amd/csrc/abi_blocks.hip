@@ -140,16 +140,21 @@ xshare_status xshare_block_linear(const uint16_t* x, int64_t ldx, const uint8_t*
   if (!wq || !aligned16(wq) || !wscale || !aligned4(wscale) || !y) return XSHARE_EINVAL;
   if (x ? (xq || xs || !valid_x(x, ldx, k)) : (!xq || !xs || !aligned16(xq) || !aligned4(xs)))
     return XSHARE_EINVAL;
-  xs::BlockLinearArgs a{T, n, k, xq, xs, wq, wscale, y, ldy};
+  xs::BlockLinearArgs a{T, n, k, nullptr, 0, xq, xs, wq, wscale, y, ldy};
   if (x) {
     const xs::BlockLinearLayout L = xs::block_linear_layout(T, k);
     if (!ws || ws_bytes < L.total) return XSHARE_EWORKSPACE;
-    uint8_t* const q = at<uint8_t>(ws, L.xq);
-    float* const s = at<float>(ws, L.xs);
-    if (xs::launch_block_quantize(x, T, k, ldx, 1, q, s, stream) != hipSuccess)
-      return XSHARE_EHIP;
-    a.xq = q;
-    a.xs = s;
+    if (xs::block_linear_small(T, k)) {
+      a.x = x;
+      a.ldx = ldx;
+    } else {
+      uint8_t* const q = at<uint8_t>(ws, L.xq);
+      float* const s = at<float>(ws, L.xs);
+      if (xs::launch_block_quantize(x, T, k, ldx, 1, q, s, stream) != hipSuccess)
+        return XSHARE_EHIP;
+      a.xq = q;
+      a.xs = s;
+    }
   }
   return status_of(xs::launch_block_linear(a, stream));
 }

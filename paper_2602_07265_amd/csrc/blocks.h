@@ -57,8 +57,14 @@ inline BlockLinearLayout block_linear_layout(int T, int k) {
   return L;
 }
 
+// Whether a product quantises x as it goes (launch_block_linear with x given): up to 16 rows and
+// 32768 values.
+inline bool block_linear_small(int T, int k) { return T <= 16 && long(T) * k <= 32768; }
+
 struct BlockLinearArgs {
   int T, n, k;
+  const uint16_t* x;           // bf16 rows, of block_linear_small sizes; or null, with
+  long ldx;
   const uint8_t* xq;
   const float* xs;
   const uint8_t* wq;
@@ -126,6 +132,8 @@ struct BlockExpertsArgs {
   float* hs;
   float* o;
 };
+// Whether one token's experts run in the two launches of their own.
+inline bool block_experts_one(int T, int k, int f) { return T == 1 && long(k) * f <= 32768; }
 hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream);
 
 }  // namespace xs

@@ -20,6 +20,7 @@
 namespace xs {
 namespace {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
@@ -64,8 +65,7 @@ __device__ __forceinline__ Quantum quantum(uint32_t abs_bits) {
 __device__ __forceinline__ float quotient(const Quantum& z, float x) {
   const float t = x * z.pre;
   const float q = t * z.r;
-  const float c = __builtin_fmaf(__builtin_fmaf(-q, z.a, t), z.r, q);
-  return fminf(fmaxf(c, -kMaxCode), kMaxCode);
+  return __builtin_fmaf(__builtin_fmaf(-q, z.a, t), z.r, q);   // |x| <= a: at most 448
 }
 // The codes of four values, first in the low byte.
 __device__ __forceinline__ uint32_t codes4(const Quantum& z, const float* x) {
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
 #pragma unroll
   for (int m = 0; m < MR; ++m) {
     const int r = min(n0 + 16 * (m % MW) + n, N - 1);
-    wrow[m] = (m < MW ? w1 : w3) + (size_t)r * K + 16 * g;
+    wrow[m] = (m < MW ? w1 : w3) + (size_t)r * K;
   }
   const ScalarPtr f1 = (ScalarPtr)(s1 + (size_t)(n0 / kQuantBlock) * nb);
   const ScalarPtr f3 = kKind == kGateUp ? (ScalarPtr)(s3 + (size_t)(n0 / kQuantBlock) * nb) : f1;
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
   for (int t = 0; t < NT; ++t) {
     const int p = first + min(16 * t + n, live - 1);
     const int r = kKind == kGateUp ? a.perm[p] / a.k : p;
-    xrow[t] = a.xq + (size_t)r * K + 16 * g;
+    xrow[t] = a.xq + (size_t)r * K;
     srow[t] = a.xs + (size_t)r * nb;
   }
   floatx4 acc[MR][NT];
@@ -265,75 +265,62 @@ __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
     for (int t = 0; t < NT; ++t) acc[m][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 
   struct Block {
-    int4 w[MR][2], x[NT][2];
+    i32x4 w[MR][2], x[NT][2];
     float sx[NT], f1, f3;
   };
-  auto load = [&](Block& r, int b) {
-    const int at = b * kQuantBlock;
+  // Pieces past the row's end, and blocks past the last, read the last one.
+  auto load = [&](Block& r, int at_block) {
+    const int b = min(at_block, nb - 1);
+    const int lo = min(b * kQuantBlock + 16 * g, K - 16);
+    const int hi = min(b * kQuantBlock + 64 + 16 * g, K - 16);
 #pragma unroll
     for (int m = 0; m < MR; ++m) {
-      r.w[m][0] = *reinterpret_cast<const int4*>(wrow[m] + at);
-      r.w[m][1] = *reinterpret_cast<const int4*>(wrow[m] + at + 64);
+      r.w[m][0] = *reinterpret_cast<const i32x4*>(wrow[m] + lo);
+      r.w[m][1] = *reinterpret_cast<const i32x4*>(wrow[m] + hi);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      r.x[t][0] = *reinterpret_cast<const int4*>(xrow[t] + at);
-      r.x[t][1] = *reinterpret_cast<const int4*>(xrow[t] + at + 64);
+      r.x[t][0] = *reinterpret_cast<const i32x4*>(xrow[t] + lo);
+      r.x[t][1] = *reinterpret_cast<const i32x4*>(xrow[t] + hi);
       r.sx[t] = srow[t][b];
     }
     r.f1 = f1[b];
     if constexpr (kKind == kGateUp) r.f3 = f3[b];
   };
-  auto whole = [](const int4 (&v)[2]) {
-    return i32x8{v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
-  };
-  auto add = [&](const Block& r) {
+  auto add = [&](const Block& r, int b) {
+    // where the rows end inside this block, what was read past them is not theirs
+    const int lo = b * kQuantBlock + 16 * g < K ? -1 : 0;
+    const int hi = b * kQuantBlock + 64 + 16 * g < K ? -1 : 0;
+    auto whole = [&](const i32x4 (&v)[2]) {
+      return __builtin_shufflevector(v[0] & lo, v[1] & hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    i32x8 w[MR];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int m = 0; m < MR; ++m) w[m] = whole(r.w[m]);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const i32x8 x = whole(r.x[t]);
 #pragma unroll
       for (int m = 0; m < MR; ++m) {
-        const floatx4 v = mfma128(whole(r.w[m]), whole(r.x[t]));
+        const floatx4 v = mfma128(w[m], x);
         const float s = r.sx[t] * (m < MW ? r.f1 : r.f3);
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[m][t][i] = __builtin_fmaf(v[i], s, acc[m][t][i]);
       }
+    }
   };
-  const int full = K / kQuantBlock;                     // blocks without an end in them
-  if (wave < full) {
-    const int last = full - 1;
-    Block u, v;
-    int b = wave;
-    load(u, b);
-    while (true) {                                      // (the last loads repeat block `last`)
-      load(v, min(b + KW, last));
-      __builtin_amdgcn_sched_barrier(0);                // loads stay above the instructions
-      add(u);
-      if ((b += KW) >= full) break;
-      load(u, min(b + KW, last));
-      __builtin_amdgcn_sched_barrier(0);
-      add(v);
-      if ((b += KW) >= full) break;
-    }
-  }
-  if (full < nb && wave == full % KW) {                 // the rows end inside this block
-    const int at = full * kQuantBlock;
-    const bool lo = at + 16 * g < K, hi = at + 64 + 16 * g < K;
-    const int4 zero = make_int4(0, 0, 0, 0);
-    Block r;
-#pragma unroll
-    for (int m = 0; m < MR; ++m) {
-      r.w[m][0] = lo ? *reinterpret_cast<const int4*>(wrow[m] + at) : zero;
-      r.w[m][1] = hi ? *reinterpret_cast<const int4*>(wrow[m] + at + 64) : zero;
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      r.x[t][0] = lo ? *reinterpret_cast<const int4*>(xrow[t] + at) : zero;
-      r.x[t][1] = hi ? *reinterpret_cast<const int4*>(xrow[t] + at + 64) : zero;
-      r.sx[t] = srow[t][full];
-    }
-    r.f1 = f1[full];
-    if constexpr (kKind == kGateUp) r.f3 = f3[full];
-    add(r);
+  Block u, v;
+  int b = wave;
+  load(u, b);
+  while (b < nb) {
+    load(v, b + KW);
+    __builtin_amdgcn_sched_barrier(0);                  // loads stay above the instructions
+    add(u, b);
+    if ((b += KW) >= nb) break;
+    load(u, b + KW);
+    __builtin_amdgcn_sched_barrier(0);
+    add(v, b);
+    b += KW;
   }
   // lane (n, g) holds rows 4 g .. 4 g + 3 of weight tile m for token n of tile t
 #pragma unroll
@@ -372,16 +359,10 @@ __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
 // c ^ ((r >> 1) & 7): the sixteen rows of an operand read then lie in sixteen different
 // places modulo 256 bytes.  The loads write LDS in lane order, so the lanes take their
 // source pieces in that order.
-__device__ const uint4 kZeroPiece = {0, 0, 0, 0};   // what lies past the end of a row
-
 typedef const __attribute__((address_space(1))) void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
-// `out`: the piece lies past the end of its row and is zero.  (The empty statement keeps the
-// choice an address: two loads under a branch would be made of it.)
-__device__ __forceinline__ void to_lds16(const uint8_t* src, bool out, uint8_t* dst) {
-  src = out ? reinterpret_cast<const uint8_t*>(&kZeroPiece) : src;
-  asm("" : "+v"(src));
+__device__ __forceinline__ void to_lds16(const uint8_t* src, uint8_t* dst) {
   __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)dst, 16, 0, 0);
 }
 __device__ __forceinline__ void to_lds4(const float* src, float* dst) {
@@ -453,26 +434,27 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
   }
   const int n0 = blockIdx.x * kCols;
   // LDS row R of the weights: tile (R / 16) % MW of wave R / (16 MW) along the weight rows
-  const uint8_t* wsrc[LW];
+  // (offsets from the tile's first row fit 32 bits: 256 rows of at most 2^20 bytes)
+  const uint8_t *const wbase1 = w1 + (size_t)n0 * K, *const wbase3 = w3 + (size_t)n0 * K;
+  uint32_t woff[LW];
   const int piece = 16 * ((lane & 7) ^ (((tid >> 3) >> 1) & 7));
 #pragma unroll
   for (int j = 0; j < LW; ++j) {
     const int R = j * kRows + (tid >> 3);
-    const uint8_t* w = w1;
-    int unit = n0 + R;
-    if constexpr (kKind == kGateUp) {
-      const int m = (R / 16) % MW;
-      w = m < MW / 2 ? w1 : w3;
-      unit = n0 + R / (16 * MW) * (8 * MW) + m % (MW / 2) * 16 + R % 16;
-    }
-    wsrc[j] = w + (size_t)min(unit, N - 1) * K + piece;
+    const int unit = kKind == kGateUp
+                         ? R / (16 * MW) * (8 * MW) + R / 16 % MW % (MW / 2) * 16 + R % 16
+                         : R;
+    woff[j] = (uint32_t)min(unit, N - 1 - n0) * (uint32_t)K;
   }
-  const uint8_t* xsrc[LT];
+  // whether load j is of W3 is the wave's to know: its eight rows lie in one tile
+  auto of_w3 = [&](int j) { return kKind == kGateUp && (j * kRows + wave * 8) / 16 % MW >= MW / 2; };
+  const uint8_t* const xbase = kKind == kGateUp ? a.xq : a.xq + (size_t)first * K;
+  size_t xoff[LT];
 #pragma unroll
   for (int j = 0; j < LT; ++j) {
-    const int p = first + min((j * kRows + (tid >> 3)) % BT, live - 1);
-    const int r = kKind == kGateUp ? a.perm[p] / a.k : p;
-    xsrc[j] = a.xq + (size_t)r * K + piece;
+    const int p = min((j * kRows + (tid >> 3)) % BT, live - 1);
+    xoff[j] = kKind == kGateUp ? (size_t)(a.perm[first + p] / a.k) * K
+                               : (size_t)((uint32_t)p * (uint32_t)K);
   }
   // lane l of a load of scales takes block l % 4 of token l / 4
   const float* ssrc[kScaleLoads];
@@ -485,14 +467,14 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
     ssrc[j] = a.xs + (size_t)r * nb;
     sdst[j] = L::kScales + t0 * kScaleBlocks * 4;
   }
-  // the i-th of a wave's loads of block b
+  // the i-th of a wave's loads of block b (what lies past the row's end: its last piece)
   auto load = [&](int b, uint8_t* stage, int i) {
-    const int at = b * kQuantBlock;
-    const bool out = at + piece >= K;      // past the end of a last, partial block
+    const uint32_t at = (uint32_t)min(b * kQuantBlock + piece, K - 16);
     if (i < LW)
-      to_lds16(wsrc[i < LW ? i : 0] + at, out, stage + (i * kRows + wave * 8) * kQuantBlock);
+      to_lds16((of_w3(i) ? wbase3 : wbase1) + (woff[i < LW ? i : 0] + at),
+               stage + (i * kRows + wave * 8) * kQuantBlock);
     else
-      to_lds16(xsrc[i < LW ? 0 : i - LW] + at, out,
+      to_lds16(xbase + (xoff[i < LW ? 0 : i - LW] + at),
                stage + (BW + ((i - LW) * kRows + wave * 8) % BT) * kQuantBlock);
   };
   const int n_block = n0 / kQuantBlock;
@@ -591,6 +573,20 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
     // A chunk of scales is loaded kLead steps before its first block, so that it is older than
     // any load that may be in flight then; its buffer was last read the step before, or earlier.
     wait_loads<kLoads*(kStages - 2)>();
+    if (b == nb - 1 && K % kQuantBlock != 0) {         // the rows end inside this block
+      uint8_t* const mine = lds + cur * L::kStage + wave * 8 * kQuantBlock + 16 * lane;
+      if (b * kQuantBlock + piece >= K) {
+#pragma unroll
+        for (int i = 0; i < LW; ++i)
+          *reinterpret_cast<i32x4*>(mine + i * kRows * kQuantBlock) = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < LT; ++i)
+          *reinterpret_cast<i32x4*>(lds + cur * L::kStage + 16 * lane +
+                                    (BW + (i * kRows + wave * 8) % BT) * kQuantBlock) =
+              i32x4{0, 0, 0, 0};
+      }
+      __syncthreads();
+    }
     if ((b + kLead) % kScaleBlocks == 0 && b + kLead < nb) load_scales(b + kLead);
     step(b, lds + cur * L::kStage,
          reinterpret_cast<const float*>(lds + L::kScales +
@@ -711,6 +707,199 @@ const LinearForm kLinearForms[] = {
     {256, 256, 2.1f, launch_tile<kLinear, 256, 256, 2, 4, 2>},
 };
 
+// ---------------------------------------------------------------------------- one token
+
+// Products whose token rows are few enough to be quantised by every workgroup for itself, into
+// LDS: a linear product of up to 16 short rows, and the two products of one token's experts, so
+// that these calls are one launch and two.  The waves take the blocks of K in turn as in
+// product_kernel.
+//   kLinear  x rows [T, K] bf16; 16 MR weight rows a workgroup.
+//   kGateUp  the one token's x; workgroup (., r) the expert of pair r: h[r] = silu(W1 x) (W3 x).
+//   kDown    all pairs' h rows [k, K]; y = sum_r w_r W2_{id_r} q(h_r), the pairs one after the
+//            other in every wave, no outputs of single pairs in between.
+struct Small {
+  const uint16_t* x;           // kLinear, kGateUp
+  long ldx;
+  const float* hin;            // kDown
+  int T, N, K;
+  const uint8_t *w1, *w3;
+  const float *s1, *s3;
+  const int32_t* ids;          // [k]
+  const float* w;
+  int k, E;
+  float* h;                    // kGateUp: [k, N]
+  uint16_t* y;                 // kLinear [T, N], kDown [N]
+  long ldy;
+};
+
+constexpr int kSmallPairs = kMaxTopK;
+// Bytes of a code row in LDS: whole blocks, rows 16 bytes past a multiple of 128 apart.
+__host__ __device__ inline int small_pitch(int K) {
+  return (K + kQuantBlock - 1) / kQuantBlock * kQuantBlock + 16;
+}
+inline long small_lds(long rows, int K) { return rows * (small_pitch(K) + 4 * quant_blocks(K)); }
+
+template <Kind kKind, int MR, int KW>
+__global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
+  constexpr int kRows = kKind == kLinear ? 16 : 1;
+  constexpr int MW = kKind == kGateUp ? MR / 2 : MR;
+  constexpr int LD = 16 * MR + 4;
+  __shared__ float red[KW][kRows][LD];
+  __shared__ int expert[kSmallPairs];
+  __shared__ int pair[kSmallPairs];
+  extern __shared__ __attribute__((aligned(16))) uint8_t codes[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  const int N = a.N, K = a.K;
+  const int nb = (K + kQuantBlock - 1) / kQuantBlock, nbN = (N + kQuantBlock - 1) / kQuantBlock;
+  const int pitch = small_pitch(K);
+  const int n0 = blockIdx.x * 16 * MW;
+  int e0 = 0, pairs = 1;                   // kGateUp's expert; pairs that the workgroup adds up
+  if constexpr (kKind == kGateUp) {
+    e0 = __builtin_amdgcn_readfirstlane(a.ids[blockIdx.y]);
+    if (e0 < 0 || e0 >= a.E) return;
+  }
+  if constexpr (kKind == kDown) {
+    const int id = lane < a.k ? a.ids[lane] : -1;
+    const uint64_t live = __ballot(id >= 0 && id < a.E);
+    pairs = __popcll(live);
+    const int at = __popcll(live & ((1ull << lane) - 1));
+    if (wave == 0 && ((live >> lane) & 1)) {
+      expert[at] = id;
+      pair[at] = lane;
+    }
+    __syncthreads();
+  }
+  const int rows = kKind == kLinear ? a.T : pairs;
+  float* const scales = reinterpret_cast<float*>(codes + (size_t)rows * pitch);   // [rows][nb]
+
+  // rows past the end repeat the last one; their results are not stored
+  size_t wrow[MW];
+#pragma unroll
+  for (int m = 0; m < MW; ++m) wrow[m] = (size_t)min(n0 + 16 * m + n, N - 1) * K;
+  floatx4 acc[MR];
+#pragma unroll
+  for (int m = 0; m < MR; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  struct Block {
+    i32x4 w[MR][2];
+    float f1, f3;
+  };
+  struct Item {                            // block b of pair q
+    int q, b;
+  };
+  auto next = [&](Item i) {
+    i.b += KW;
+    while (i.b >= nb && i.q + 1 < pairs) {
+      i.b -= nb;
+      ++i.q;
+    }
+    return i;
+  };
+  // Pieces past the row's end, and blocks past the last, read the last one.
+  auto load = [&](Block& r, Item i) {
+    const int b = min(i.b, nb - 1);
+    const int e = kKind == kDown ? __builtin_amdgcn_readfirstlane(expert[i.q]) : e0;
+    const int lo = min(b * kQuantBlock + 16 * g, K - 16);
+    const int hi = min(b * kQuantBlock + 64 + 16 * g, K - 16);
+    const size_t s = ((size_t)e * nbN + n0 / kQuantBlock) * nb + b;
+    r.f1 = a.s1[s];
+    if constexpr (kKind == kGateUp) r.f3 = a.s3[s];
+#pragma unroll
+    for (int m = 0; m < MR; ++m) {
+      const uint8_t* const p = (m < MW ? a.w1 : a.w3) + (size_t)e * N * K + wrow[m % MW];
+      r.w[m][0] = *reinterpret_cast<const i32x4*>(p + lo);
+      r.w[m][1] = *reinterpret_cast<const i32x4*>(p + hi);
+    }
+  };
+  auto add = [&](const Block& r, Item i) {
+    const int row = kKind == kLinear ? min(n, a.T - 1) : i.q;
+    const int at = i.b * kQuantBlock + 16 * g;
+    const uint8_t* const p = codes + row * pitch + at;
+    const i32x8 x = __builtin_shufflevector(*reinterpret_cast<const i32x4*>(p),
+                                            *reinterpret_cast<const i32x4*>(p + 64), 0, 1, 2, 3,
+                                            4, 5, 6, 7);
+    const float sx = scales[row * nb + i.b];
+    // where the rows end inside this block, what was read past them is not theirs
+    const int lo = at < K ? -1 : 0, hi = at + 64 < K ? -1 : 0;
+#pragma unroll
+    for (int m = 0; m < MR; ++m) {
+      const i32x8 w = __builtin_shufflevector(r.w[m][0] & lo, r.w[m][1] & hi, 0, 1, 2, 3, 4, 5, 6,
+                                              7);
+      const floatx4 t = mfma128(w, x);
+      const float s = sx * (m < MW ? r.f1 : r.f3);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[m][j] = __builtin_fmaf(t[j], s, acc[m][j]);
+    }
+  };
+  Block u, v;
+  Item i{0, wave};
+  while (i.b >= nb && i.q + 1 < pairs) {                // (fewer blocks than waves)
+    i.b -= nb;
+    ++i.q;
+  }
+  if (pairs > 0) load(u, i);                            // under way while the rows are quantised
+
+  for (int o = tid >> 4; o < rows * nb; o += 4 * KW) {
+    const int r = o / nb, b = o - r * nb, c = b * kQuantBlock + 8 * (tid & 15);
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (c < K) {
+      if constexpr (kKind == kDown)
+        load8(a.hin + (size_t)pair[r] * K + c, v);
+      else
+        load8(a.x + (size_t)r * a.ldx + c, v);
+    }
+    uint32_t m = abs_max8(v);
+#pragma unroll
+    for (int s = 1; s < 16; s *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, s));
+    const Quantum z = quantum(m);
+    *reinterpret_cast<uint2*>(codes + r * pitch + c) = make_uint2(codes4(z, v), codes4(z, v + 4));
+    if ((tid & 15) == 0) scales[o] = z.scale * (kKind == kDown ? a.w[pair[r]] : 1.0f);
+  }
+  __syncthreads();
+  if (pairs > 0) {
+    while (i.b < nb) {
+      const Item j = next(i);
+      load(v, j);
+      __builtin_amdgcn_sched_barrier(0);
+      add(u, i);
+      if (j.b >= nb) break;
+      i = next(j);
+      load(u, i);
+      __builtin_amdgcn_sched_barrier(0);
+      add(v, j);
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+    if (n < kRows) *reinterpret_cast<floatx4*>(&red[wave][n][16 * m + 4 * g]) = acc[m];
+  __syncthreads();
+  const int live = kKind == kLinear ? a.T : 1;
+  for (int i = tid; i < live * 16 * MW; i += 64 * KW) {
+    const int t = i / (16 * MW), c = i - t * 16 * MW;
+    if (n0 + c >= N) continue;
+    auto sum = [&](int col) {
+      float s = red[0][t][col];
+#pragma unroll
+      for (int w = 1; w < KW; ++w) s += red[w][t][col];
+      return s;
+    };
+    const float v = sum(c);
+    if constexpr (kKind == kGateUp)
+      a.h[(size_t)blockIdx.y * N + n0 + c] = v / (1.0f + expf(-v)) * sum(16 * MW + c);
+    else
+      a.y[(size_t)t * a.ldy + n0 + c] = to_bf16(v);
+  }
+}
+
+template <Kind kKind, int MR, int KW>
+hipError_t launch_small(const Small& a, int rows, int groups, hipStream_t stream) {
+  const int cols = 16 * (kKind == kGateUp ? MR / 2 : MR);
+  small_kernel<kKind, MR, KW><<<dim3((a.N + cols - 1) / cols, groups), 64 * KW,
+                               small_lds(rows, a.K), stream>>>(a);
+  return hipGetLastError();
+}
+
 // ---------------------------------------------------------------------------- experts
 
 // The pairs in expert order: one workgroup an expert, each over all ids.  It counts the pairs
@@ -818,6 +1007,22 @@ hipError_t launch_block_linear(const BlockLinearArgs& a, hipStream_t stream) {
   p.rows = a.T;
   p.y = a.y;
   p.ldy = a.ldy;
+  if (a.x) {
+    // Up to 16 rows of 32768 values in all are quantised by every workgroup for itself.
+    Small s{};
+    s.x = a.x;
+    s.ldx = a.ldx;
+    s.T = a.T;
+    s.N = a.n;
+    s.K = a.k;
+    s.w1 = a.wq;
+    s.s1 = a.wscale;
+    s.y = a.y;
+    s.ldy = a.ldy;
+    if (a.n >= 14336) return launch_small<kLinear, 4, 4>(s, a.T, 1, stream);
+    if (a.n >= 7168) return launch_small<kLinear, 2, 4>(s, a.T, 1, stream);
+    return launch_small<kLinear, 1, 4>(s, a.T, 1, stream);
+  }
   const LinearForm* best = nullptr;
   float least = 0.0f;
   for (const LinearForm& f : kLinearForms) {
@@ -846,6 +1051,31 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   const bool few_up = mean <= 16 && long(expect) * ((a.f + 127) / 128) < 96;
   const bool few_groups = long(expect) * spans * ((a.d + 255) / 256) < 192;
   const int up_rows = few_up ? 16 : wide, down_rows = !few_groups ? wide : mean <= 8 ? 16 : 64;
+  if (block_experts_one(a.T, a.k, a.f)) {
+    Small s{};
+    s.x = a.x;
+    s.T = 1;
+    s.N = a.f;
+    s.K = a.d;
+    s.w1 = a.w1;
+    s.w3 = a.w3;
+    s.s1 = a.s1;
+    s.s3 = a.s3;
+    s.ids = a.ids;
+    s.w = a.w;
+    s.k = a.k;
+    s.E = a.E;
+    s.h = a.h;
+    const hipError_t e = launch_small<kGateUp, 2, 8>(s, 1, a.k, stream);
+    if (e != hipSuccess) return e;
+    s.hin = a.h;
+    s.N = a.d;
+    s.K = a.f;
+    s.w1 = a.w2;
+    s.s1 = a.s2;
+    s.y = a.y;
+    return launch_small<kDown, 1, 8>(s, a.k, 1, stream);
+  }
   hipError_t e = quantize_rows(a.x, a.T, a.d, a.ldx, a.xq, a.xs, nullptr, stream);
   if (e != hipSuccess) return e;
   index_kernel<<<a.E, 1024, 0, stream>>>(a.ids, pairs, a.E, up_rows, down_rows, a.counts, a.perm,
