@@ -111,16 +111,14 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
   x[7] = b.w;
 }
 
-// Blocks of 1 x 128: 16 lanes a block, eight neighbouring values a lane.  `live`: nullable
-// count of rows on the device, at most `rows`.
+// Blocks of 1 x 128: 16 lanes a block, eight neighbouring values a lane; this thread's 16 lanes
+// take every `step`-th block from `i` on.
 template <typename In>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const In* x, int rows, int cols,
-                                                            long ld, uint8_t* q, float* scales,
-                                                            const int32_t* live) {
+__device__ __forceinline__ void quantize_rows(const In* x, long rows, int cols, long ld, uint8_t* q,
+                                              float* scales, long i, long step) {
   const int nb = (cols + kQuantBlock - 1) / kQuantBlock;
-  const long n = (long)(live ? *live : rows) * nb;
   const int l = threadIdx.x & 15;
-  for (long i = (long)blockIdx.x * 16 + (threadIdx.x >> 4); i < n; i += (long)gridDim.x * 16) {
+  for (; i < rows * nb; i += step) {
     const long r = i / nb;
     const int b = (int)(i - r * nb), c = b * kQuantBlock + 8 * l;
     const bool in = c < cols;
@@ -134,6 +132,15 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const In* x, int row
       *reinterpret_cast<uint2*>(q + r * cols + c) = make_uint2(codes4(z, v), codes4(z, v + 4));
     if (l == 0) scales[i] = z.scale;
   }
+}
+
+// `live`: nullable count of rows on the device, at most `rows`.
+template <typename In>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const In* x, int rows, int cols,
+                                                            long ld, uint8_t* q, float* scales,
+                                                            const int32_t* live) {
+  quantize_rows(x, live ? *live : rows, cols, ld, q, scales,
+                (long)blockIdx.x * 16 + (threadIdx.x >> 4), (long)gridDim.x * 16);
 }
 
 // Blocks of 128 x 128: one workgroup a block, 64 values a thread (row threadIdx / 16 + 16 i).
@@ -166,7 +173,7 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(const uint16_t* x, i
 }
 
 template <typename In>
-hipError_t quantize_rows(const In* x, long rows, int cols, long ld, uint8_t* q, float* scales,
+hipError_t launch_quantize_rows(const In* x, long rows, int cols, long ld, uint8_t* q, float* scales,
                          const int32_t* live, hipStream_t stream) {
   const long groups = (rows * quant_blocks(cols) + 15) / 16;
   const int grid = (int)(groups < 16384 ? groups : 16384);
@@ -902,14 +909,33 @@ hipError_t launch_small(const Small& a, int rows, int groups, hipStream_t stream
 
 // ---------------------------------------------------------------------------- experts
 
-// The pairs in expert order: one workgroup an expert, each over all ids.  It counts the pairs
+// What the products of the experts need: x quantised, and the pairs in expert order.  The first E
+// workgroups are an expert's each, over all ids; the rest take the blocks of x.  The one counts the pairs
 // of every expert (in LDS) and, wave by wave, its own; its rows begin after those of the
 // experts before it, its tiles of either product likewise, and its pairs are listed in
 // ascending order.
-__global__ __launch_bounds__(1024) void index_kernel(const int32_t* ids, int pairs, int E,
-                                                     int up_rows, int down_rows,
-                                                     int32_t* counts, int32_t* perm,
-                                                     int4* up_tiles, int4* down_tiles) {
+struct Prepare {
+  const uint16_t* x;
+  int T, d;
+  long ldx;
+  uint8_t* xq;
+  float* xs;
+  const int32_t* ids;
+  int pairs, E, up_rows, down_rows;
+  int32_t* counts;
+  int32_t* perm;
+  int4* up_tiles;
+  int4* down_tiles;
+};
+__global__ __launch_bounds__(1024) void prepare_kernel(Prepare a) {
+  if ((int)blockIdx.x >= a.E) {
+    quantize_rows(a.x, a.T, a.d, a.ldx, a.xq, a.xs,
+                  (long)(blockIdx.x - a.E) * 64 + (threadIdx.x >> 4),
+                  (long)(gridDim.x - a.E) * 64);
+    return;
+  }
+  const int32_t* const ids = a.ids;
+  const int pairs = a.pairs, E = a.E;
   __shared__ int count[kMaxExperts];
   __shared__ int mine[16];
   __shared__ int sums[3][16];
@@ -930,7 +956,7 @@ __global__ __launch_bounds__(1024) void index_kernel(const int32_t* ids, int pai
   // rows and tiles of the experts before e
   auto tiles_of = [](int rows, int tile) { return (rows + tile - 1) / tile; };
   const int c = tid < e ? count[tid] : 0;
-  int before[3] = {c, tiles_of(c, up_rows), tiles_of(c, down_rows)};
+  int before[3] = {c, tiles_of(c, a.up_rows), tiles_of(c, a.down_rows)};
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
 #pragma unroll
@@ -947,18 +973,18 @@ __global__ __launch_bounds__(1024) void index_kernel(const int32_t* ids, int pai
   }
   const int n = count[e];
   if (e == E - 1 && tid == 0) {
-    counts[0] = row0 + n;
-    counts[1] = up0 + tiles_of(n, up_rows);
-    counts[2] = down0 + tiles_of(n, down_rows);
+    a.counts[0] = row0 + n;
+    a.counts[1] = up0 + tiles_of(n, a.up_rows);
+    a.counts[2] = down0 + tiles_of(n, a.down_rows);
   }
-  for (int i = tid * up_rows; i < n; i += 1024 * up_rows)
-    up_tiles[up0 + i / up_rows] = make_int4(e, row0 + i, min(up_rows, n - i), 0);
-  for (int i = tid * down_rows; i < n; i += 1024 * down_rows)
-    down_tiles[down0 + i / down_rows] = make_int4(e, row0 + i, min(down_rows, n - i), 0);
+  for (int i = tid * a.up_rows; i < n; i += 1024 * a.up_rows)
+    a.up_tiles[up0 + i / a.up_rows] = make_int4(e, row0 + i, min(a.up_rows, n - i), 0);
+  for (int i = tid * a.down_rows; i < n; i += 1024 * a.down_rows)
+    a.down_tiles[down0 + i / a.down_rows] = make_int4(e, row0 + i, min(a.down_rows, n - i), 0);
   for (int i = from; i < to; i += 64) {
     const bool hit = i + lane < to && ids[i + lane] == e;
     const uint64_t hits = __ballot(hit);
-    if (hit) perm[row0 + at + __popcll(hits & ((1ull << lane) - 1))] = i + lane;
+    if (hit) a.perm[row0 + at + __popcll(hits & ((1ull << lane) - 1))] = i + lane;
     at += __popcll(hits);
   }
 }
@@ -990,7 +1016,8 @@ __global__ __launch_bounds__(256) void combine_kernel(const float* o, const int3
 
 hipError_t launch_block_quantize(const uint16_t* x, int rows, int cols, long ld, int block_rows,
                                  uint8_t* q, float* scales, hipStream_t stream) {
-  if (block_rows == 1) return quantize_rows(x, rows, cols, ld, q, scales, nullptr, stream);
+  if (block_rows == 1)
+    return launch_quantize_rows(x, rows, cols, ld, q, scales, nullptr, stream);
   quantize_tile_kernel<<<dim3(quant_blocks(cols), quant_blocks(rows)), 256, 0, stream>>>(
       x, rows, cols, ld, q, scales);
   return hipGetLastError();
@@ -1076,11 +1103,12 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
     s.y = a.y;
     return launch_small<kDown, 1, 8>(s, a.k, 1, stream);
   }
-  hipError_t e = quantize_rows(a.x, a.T, a.d, a.ldx, a.xq, a.xs, nullptr, stream);
+  const long groups = (long(a.T) * quant_blocks(a.d) + 63) / 64;
+  prepare_kernel<<<int(a.E + (groups < 4096 ? groups : 4096)), 1024, 0, stream>>>(
+      {a.x, a.T, a.d, a.ldx, a.xq, a.xs, a.ids, pairs, a.E, up_rows, down_rows, a.counts, a.perm,
+       a.up_tiles, a.down_tiles});
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  index_kernel<<<a.E, 1024, 0, stream>>>(a.ids, pairs, a.E, up_rows, down_rows, a.counts, a.perm,
-                                         a.up_tiles, a.down_tiles);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
   Product p{};
   p.xq = a.xq;
   p.xs = a.xs;
@@ -1100,7 +1128,7 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   const int up = pair_tiles(pairs, a.E, up_rows), down = pair_tiles(pairs, a.E, down_rows);
   if (few_up) {
     if ((e = launch_product<kGateUp, 2, 1, 4>(p, up, stream)) != hipSuccess) return e;
-    e = quantize_rows(a.h, pairs, a.f, a.f, a.hq, a.hs, a.counts, stream);
+    e = launch_quantize_rows(a.h, pairs, a.f, a.f, a.hq, a.hs, a.counts, stream);
   } else {
     e = wide == 32 ? launch_tile<kGateUp, 256, 32, 8, 1, 4>(p, up, stream)
                    : launch_tile<kGateUp, 256, 128, 4, 2, 3>(p, up, stream);
