@@ -4,7 +4,8 @@ A token's scores are s_j = exp(h_j - max h) / sum (softmax) or 1 / (1 + exp(-h_j
 Experts rank by c_j = s_j + bias_j, or by h_j without a bias; a group's score is the largest
 c_j of its N / G consecutive experts, or the sum of its two largest s_j (+ bias_j); ties go to
 the lower index.  The k best experts of the top_groups best groups are taken, with weights
-w_r = s_{id_r}, divided by their sum if asked, times `scale`.
+w_r = s_{id_r}, divided by their sum if asked, times `scale`.  A logit of -inf masks its expert:
+score 0, ranked last, 0 in a sum of two.
 """
 from __future__ import annotations
 
@@ -14,9 +15,11 @@ import numpy as np
 def scores(h, score):
     h = np.asarray(h, np.float64)
     if score == "sigmoid":
-        return 1.0 / (1.0 + np.exp(-h))
-    e = np.exp(h - h.max(axis=1, keepdims=True))
-    return e / e.sum(axis=1, keepdims=True)
+        with np.errstate(over="ignore"):
+            return 1.0 / (1.0 + np.exp(-h))
+    m = h.max(axis=1, keepdims=True)
+    e = np.exp(h - np.where(np.isfinite(m), m, 0.0))
+    return e / np.maximum(e.sum(axis=1, keepdims=True), 2.0 ** -126)
 
 
 def _best(values, n):
@@ -31,15 +34,19 @@ def gate(h, top_k, score="softmax", bias=None, n_groups=1, top_groups=1, group_s
     h = np.asarray(h, np.float64)
     T, N = h.shape
     s = scores(h, score)
-    c = h if bias is None else s + np.asarray(bias, np.float64)
+    masked = np.isneginf(h)
+    c = h if bias is None else np.where(masked, -np.inf, s + np.asarray(bias, np.float64))
     margin = np.full(T, np.inf)
 
     def gap(ranked):
+        ranked = np.where(np.isfinite(ranked), ranked, -1e30)
         d = ranked[:, :-1] - ranked[:, 1:]
         return np.where(d > 0, d, np.inf).min(axis=1, initial=np.inf)
 
     if top_groups < n_groups:
-        base = c if group_score == "max" or bias is not None else s
+        base = c
+        if group_score == "top2":
+            base = np.where(masked, 0.0, s if bias is None else c)
         per = -np.sort(-base.reshape(T, n_groups, -1), axis=2)
         gs = per[:, :, 0] if group_score == "max" else per[:, :, 0] + per[:, :, 1]
         order = _best(gs, n_groups)
@@ -50,7 +57,6 @@ def gate(h, top_k, score="softmax", bias=None, n_groups=1, top_groups=1, group_s
         c = np.where(np.repeat(keep, N // n_groups, axis=1), c, -np.inf)
     order = _best(c, min(top_k + 1, N))
     ranked = np.take_along_axis(c, order, 1)
-    ranked = np.where(np.isfinite(ranked), ranked, -1e30)
     margin = np.minimum(margin, gap(ranked))
     ids = order[:, :top_k]
     w = np.take_along_axis(s, ids, 1)

@@ -40,8 +40,6 @@ hipError_t launch_gate_backward(const GateArgs& a, hipStream_t stream);
 hipError_t launch_block_quantize(const uint16_t* x, int rows, int cols, long ld, int block_rows,
                                  uint8_t* q, float* scales, hipStream_t stream);
 
-// Least rows of a token tile of the grouped products.
-constexpr int kTileRows = 16;
 
 struct BlockLinearLayout {
   size_t xq;                   // uint8 [T, k]  codes of x
@@ -81,13 +79,43 @@ inline int pair_tiles(int pairs, int E, int tile_rows) {
   return some + (pairs - some) / tile_rows;
 }
 
+// The forms of the experts' two products, by the rows of an expert on average if as many experts
+// as can be have a pair.  From 12 rows on tiles of 128 tokens cost no more than narrower ones
+// (their empty 32s are skipped) and read the weights of nearly every expert once; below, tiles
+// of 32 have less to load.  The tiled form wants a workgroup for most compute units: four tokens
+// of 64 (1024, 256) experts have 32 in gate/up and take 9 us in it, 6 in the few-row form; down
+// of two (4096, 14336) experts has 32, 53 against 21 us; eight of them with 16 rows 128, 105 in
+// the form of 256 x 128 against 85 in that of 128 x 64.  One token's pairs, where their hidden
+// rows are short enough for every workgroup to quantise them, take two launches of their own
+// (one of eight (2048, 768) experts 34.7 -> 16.6 us a call).
+struct BlockExpertsPlan {
+  bool one;                    // one token: the launches without tiles
+  bool few_up, few_down;       // few workgroups: gate/up in the few-row form; down in that or 128 x 64
+  int wide;                    // tokens of the tiled form's tiles
+  int up_rows, down_rows;      // rows of a tile of either product
+};
+inline BlockExpertsPlan block_experts_plan(int T, int k, int E, int d, int f) {
+  BlockExpertsPlan p{};
+  const int pairs = T > 0 ? T * k : k;
+  const int expect = pairs < E ? pairs : E, mean = pairs / expect;
+  p.one = T == 1 && long(k) * f <= 32768;
+  p.wide = mean >= 12 ? 128 : 32;
+  const long spans = (mean + p.wide - 1) / p.wide;
+  p.few_up = mean <= 16 && long(expect) * ((f + 127) / 128) < 96;
+  p.few_down = long(expect) * spans * ((d + 255) / 256) < 192;
+  p.up_rows = p.few_up ? 16 : p.wide;
+  p.down_rows = !p.few_down ? p.wide : mean <= 8 ? 16 : 64;
+  return p;
+}
+
 struct BlockExpertsLayout {
   size_t xq, xs;               // as BlockLinearLayout, of x [T, d]
   size_t counts;               // int32 [3]: pairs, tiles of gate/up, tiles of down
   size_t perm;                 // int32 [T * k] pair (t * k + r) of each row in expert order
   size_t up_tiles;             // int4 [pair_tiles] {expert, first row, rows, 0} of gate/up
   size_t down_tiles;           // and of down
-  size_t h;                    // fp32 [T * k, f] hidden rows in expert order
+  size_t h;                    // fp32 [T * k, f] hidden rows in expert order, where a plan
+                               //      quantises them after gate/up
   size_t hq, hs;               // their codes [T * k, f] and scales [T * k, ceil(f / 128)]
   size_t o;                    // fp32 [T * k, d] the pairs' outputs, by pair
   size_t total;
@@ -100,10 +128,10 @@ inline BlockExpertsLayout block_experts_layout(int T, int k, int E, int d, int f
   L.xs = o;     o += align256(sizeof(float) * size_t(T) * quant_blocks(d));
   L.counts = o; o += 256;
   L.perm = o;   o += align256(sizeof(int32_t) * rows);
-  const size_t tiles = align256(sizeof(int32_t) * 4 * size_t(pair_tiles(int(rows), E, kTileRows)));
-  L.up_tiles = o;   o += tiles;
-  L.down_tiles = o; o += tiles;
-  L.h = o;      o += align256(sizeof(float) * rows * f);
+  const BlockExpertsPlan p = block_experts_plan(T, k, E, d, f);
+  L.up_tiles = o;   o += align256(16 * size_t(pair_tiles(int(rows), E, p.up_rows)));
+  L.down_tiles = o; o += align256(16 * size_t(pair_tiles(int(rows), E, p.down_rows)));
+  L.h = o;      o += p.one || p.few_up ? align256(sizeof(float) * rows * f) : 0;
   L.hq = o;     o += align256(rows * f);
   L.hs = o;     o += align256(sizeof(float) * rows * quant_blocks(f));
   L.o = o;      o += align256(sizeof(float) * rows * d);
@@ -132,8 +160,6 @@ struct BlockExpertsArgs {
   float* hs;
   float* o;
 };
-// Whether one token's experts run in the two launches of their own.
-inline bool block_experts_one(int T, int k, int f) { return T == 1 && long(k) * f <= 32768; }
 hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream);
 
 }  // namespace xs

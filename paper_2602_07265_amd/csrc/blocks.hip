@@ -531,10 +531,18 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
     const uint8_t* const xl = stage + (BW + wt * 16 * TT + n) * kQuantBlock;
     const float* const sl = scales + (wt * 16 * TT + n) * kScaleBlocks + b % kScaleBlocks;
     const float* const fl = scales + L::kTokenFloats + b % kScaleBlocks;
-    auto load_share = [&](int i) {                     // the loads before instruction i
+    // The loads before instruction i: spread over the step, or with two buffers, where the last
+    // has the rest of this step alone to arrive in, one at every second instruction
+    // (4000 x 4096 x 7168 in 256 x 256 tiles 136-143 -> 125-133 us).
+    auto load_share = [&](int i) {
+      constexpr int kTotal = MW * TT;
+      if constexpr (kStages == 2 && kTotal >= 2 * kLoads) {
+        if (i % 2 == 0 && i / 2 < kLoads) load(ahead, next, i / 2);
+      } else {
 #pragma unroll
-      for (int l = (i * kLoads + MW * TT - 1) / (MW * TT); l * MW * TT < (i + 1) * kLoads; ++l)
-        load(ahead, next, l);
+        for (int l = (i * kLoads + kTotal - 1) / kTotal; l * kTotal < (i + 1) * kLoads; ++l)
+          load(ahead, next, l);
+      }
     };
     i32x8 w[MW], x[2];
     float sx[TT];
@@ -1065,20 +1073,8 @@ hipError_t launch_block_linear(const BlockLinearArgs& a, hipStream_t stream) {
 
 hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   const int pairs = a.T * a.k;
-  // Rows of an expert on average, if as many experts as can be have a pair.  From 12 rows on
-  // tiles of 128 tokens cost no more than narrower ones (their empty 32s are skipped) and read
-  // the weights of nearly every expert once; below, tiles of 32 have less to load.  The tiled
-  // form wants a workgroup for most compute units: one token of eight (2048, 768) experts has 48
-  // in gate/up and takes 13 us in it, 8 in the few-row form; down of two (4096, 14336) experts
-  // has 32, 53 against 21 us; eight of them with 16 rows 128, 105 in the form of 256 x 128
-  // against 85 in that of 128 x 64.
-  const int expect = pairs < a.E ? pairs : a.E, mean = pairs / expect;
-  const int wide = mean >= 12 ? 128 : 32;
-  const long spans = (mean + wide - 1) / wide;
-  const bool few_up = mean <= 16 && long(expect) * ((a.f + 127) / 128) < 96;
-  const bool few_groups = long(expect) * spans * ((a.d + 255) / 256) < 192;
-  const int up_rows = few_up ? 16 : wide, down_rows = !few_groups ? wide : mean <= 8 ? 16 : 64;
-  if (block_experts_one(a.T, a.k, a.f)) {
+  const BlockExpertsPlan plan = block_experts_plan(a.T, a.k, a.E, a.d, a.f);
+  if (plan.one) {
     Small s{};
     s.x = a.x;
     s.T = 1;
@@ -1105,8 +1101,8 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   }
   const long groups = (long(a.T) * quant_blocks(a.d) + 63) / 64;
   prepare_kernel<<<int(a.E + (groups < 4096 ? groups : 4096)), 1024, 0, stream>>>(
-      {a.x, a.T, a.d, a.ldx, a.xq, a.xs, a.ids, pairs, a.E, up_rows, down_rows, a.counts, a.perm,
-       a.up_tiles, a.down_tiles});
+      {a.x, a.T, a.d, a.ldx, a.xq, a.xs, a.ids, pairs, a.E, plan.up_rows, plan.down_rows, a.counts,
+       a.perm, a.up_tiles, a.down_tiles});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   Product p{};
@@ -1125,12 +1121,13 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   p.out = a.h;
   p.hq = a.hq;
   p.hs = a.hs;
-  const int up = pair_tiles(pairs, a.E, up_rows), down = pair_tiles(pairs, a.E, down_rows);
-  if (few_up) {
+  const int up = pair_tiles(pairs, a.E, plan.up_rows);
+  const int down = pair_tiles(pairs, a.E, plan.down_rows);
+  if (plan.few_up) {
     if ((e = launch_product<kGateUp, 2, 1, 4>(p, up, stream)) != hipSuccess) return e;
     e = launch_quantize_rows(a.h, pairs, a.f, a.f, a.hq, a.hs, a.counts, stream);
   } else {
-    e = wide == 32 ? launch_tile<kGateUp, 256, 32, 8, 1, 4>(p, up, stream)
+    e = plan.wide == 32 ? launch_tile<kGateUp, 256, 32, 8, 1, 4>(p, up, stream)
                    : launch_tile<kGateUp, 256, 128, 4, 2, 3>(p, up, stream);
   }
   if (e != hipSuccess) return e;
@@ -1143,11 +1140,11 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
   p.tiles = a.down_tiles;
   p.n_tiles = a.counts + 2;
   p.out = a.o;
-  if (few_groups)
-    e = mean <= 8 ? launch_product<kDown, 2, 1, 4>(p, down, stream)
-                  : launch_tile<kDown, 128, 64, 4, 2, 5>(p, down, stream);
+  if (plan.few_down)
+    e = plan.down_rows == 16 ? launch_product<kDown, 2, 1, 4>(p, down, stream)
+                             : launch_tile<kDown, 128, 64, 4, 2, 5>(p, down, stream);
   else
-    e = wide == 32 ? launch_tile<kDown, 256, 32, 8, 1, 4>(p, down, stream)
+    e = plan.wide == 32 ? launch_tile<kDown, 256, 32, 8, 1, 4>(p, down, stream)
                    : launch_tile<kDown, 256, 128, 4, 2, 3>(p, down, stream);
   if (e != hipSuccess) return e;
   combine_kernel<<<dim3(a.T, (a.d / 8 + 255) / 256), 256, 0, stream>>>(a.o, a.ids, a.w, a.k, a.E,

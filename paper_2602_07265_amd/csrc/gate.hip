@@ -87,9 +87,10 @@ __device__ __forceinline__ void load_row(const GateArgs& a, const void* row, int
 #pragma unroll
   for (int q = 1; q < Q; ++q) m = fmaxf(m, h[q]);
   m = wave_fmax(m);
+  m = m == -INFINITY ? 0.0f : m;         // a row of -inf: every score 0
 #pragma unroll
   for (int q = 0; q < Q; ++q) z += expf(h[q] - m);
-  z = wave_sum(z);
+  z = fmaxf(wave_sum(z), kLeastSum);
 }
 
 // The two best of a group, from its parts'.
@@ -170,8 +171,10 @@ __global__ __launch_bounds__(64 * kWaves) void gate_kernel(GateArgs a) {
     if (j >= a.N) continue;
     const bool plain = !a.bias && !(grouped && a.top2);
     const float s = plain ? 0.0f : score(a, h[q], m, z);
-    key[q] = ord(a.bias ? s + a.bias[j] : h[q]);
-    base[q] = a.top2 && !a.bias ? ord(s) : key[q];
+    const float c = a.bias ? s + a.bias[j] : h[q];
+    const bool masked = h[q] == -INFINITY;           // ranks last, whatever its bias
+    key[q] = ord(masked ? -INFINITY : c);
+    base[q] = a.top2 ? ord(masked ? 0.0f : a.bias ? c : s) : key[q];
   }
   if (grouped) limit_groups<Q>(a, lane, copies[wave], base, key);
   int id = 0;   // lane r: the expert of rank r

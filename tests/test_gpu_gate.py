@@ -118,6 +118,30 @@ def test_extreme_logits():
     assert got["w"].tolist() == [[0.0, 0.0]]
 
 
+@pytest.mark.parametrize("form", range(4))
+@pytest.mark.parametrize("group_score", ["max", "top2"])
+def test_masked_experts(form, group_score):
+    """-inf masks an expert, whatever its bias; rows with fewer experts left than k, and with none,
+    still give k indices, and weights of 0 for what is masked."""
+    from paper_2602_07265_amd import xshare as X
+    rng = np.random.default_rng(40 + form)
+    for N, G, tg, k in ((64, 1, 1, 6), (256, 8, 4, 8), (60, 4, 2, 5)):
+        for bias in (None, (0.5 * rng.normal(0, 1, N)).astype(np.float32)):
+            kw = dict(top_k=k, bias=bias, n_groups=G, top_groups=tg, group_score=group_score,
+                      **FORMS[form])
+            h = _rows(rng, 9, N, kw, "fp32")
+            h[1, ::2] = h[2, 5:] = h[3, :-3] = h[4] = h[6, 0] = -np.inf
+            keep = OG.gate(h, **kw)[2] >= MARGIN
+            got = _check(h[keep], "fp32", kw, "masked")
+            w = got["w"].cpu().numpy()
+            hidden = np.isneginf(np.take_along_axis(h[keep], got["ids"].cpu().numpy(), 1))
+            assert np.isfinite(w).all() and (w[hidden] == 0).all()
+            dw = torch.randn(w.shape, device=DEV)
+            d = X.gate_backward(_device(h[keep], "fp32"), got["ids"], dw, **FORMS[form])
+            d = d.cpu().numpy()
+            assert np.isfinite(d).all() and (d[np.isneginf(h[keep])] == 0).all()
+
+
 def test_strided_rows_guards_and_empty_batch():
     from paper_2602_07265_amd import xshare as X
     rng = np.random.default_rng(9)
