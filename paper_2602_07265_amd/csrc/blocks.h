@@ -98,7 +98,7 @@ inline BlockExpertsPlan block_experts_plan(int T, int k, int E, int d, int f) {
   BlockExpertsPlan p{};
   const int pairs = T > 0 ? T * k : k;
   const int expect = pairs < E ? pairs : E, mean = pairs / expect;
-  p.one = T == 1 && long(k) * f <= 32768;
+  p.one = T == 1 && long(k) * f <= 32768 && d <= 16384;   // (their rows in LDS: 38 KB at most)
   p.wide = mean >= 12 ? 128 : 32;
   const long spans = (mean + p.wide - 1) / p.wide;
   p.few_up = mean <= 16 && long(expect) * ((f + 127) / 128) < 96;

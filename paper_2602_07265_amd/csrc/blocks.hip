@@ -22,12 +22,29 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ floatx4 mfma128(const i32x8& a, const i32x8& b) {
   const floatx4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
   // formats 0, 0: E4M3 both; scale operands 0: the unscaled instruction
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 0, 0, 0);
+}
+
+// Eight codes as bf16, exactly (a value has four significant bits): the upper halves of the floats
+// that the conversion makes of them.
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b) {
+  typedef float floatx2 __attribute__((ext_vector_type(2)));
+  const floatx2 v[4] = {__builtin_amdgcn_cvt_pk_f32_fp8((int)a, false),
+                        __builtin_amdgcn_cvt_pk_f32_fp8((int)a, true),
+                        __builtin_amdgcn_cvt_pk_f32_fp8((int)b, false),
+                        __builtin_amdgcn_cvt_pk_f32_fp8((int)b, true)};
+  i32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = (int)__builtin_amdgcn_perm(__float_as_uint(v[i].y), __float_as_uint(v[i].x),
+                                      0x07060302u);
+  return __builtin_bit_cast(bf16x8, r);
 }
 
 __device__ __forceinline__ uint16_t to_bf16(float v) {
@@ -408,7 +425,7 @@ __global__ __launch_bounds__(64 * WW * WT) void tile_kernel(Product a) {
   constexpr int kScaleLoads = BT / 16 > WW * WT ? BT / 16 / (WW * WT) : 1;   // and chunk of scales
   constexpr int kCols = kKind == kGateUp ? BW / 2 : BW;    // output columns of a workgroup
   // token tiles worked on together; where a workgroup's tokens may be few, the rest is skipped
-  constexpr int kGroup = BT >= 256 ? TT : 2;
+  constexpr int kGroup = BT >= 256 || TT < 2 ? TT : 2;
   static_assert(TT % kGroup == 0, "whole groups");
   constexpr int kLead = kStages > 3 ? kStages - 2 : 1;
   static_assert(kLead <= kScaleBlocks, "two buffers of scales");
@@ -699,28 +716,35 @@ hipError_t launch_product(const Product& a, int tiles, hipStream_t stream) {
 }
 
 // The forms of y = x W^T: weight rows and tokens of a workgroup, and what a block of 128 inputs
-// costs it in microseconds where the GPU's 256 compute units each run one (measured from 64 to
-// 4000 tokens and 200 to 14336 weight rows; a launch takes about 2.5 us more).  The product's
-// time is that times the workgroups a compute unit has to run after each other: several
-// workgroups of the few-row forms share a unit without gaining by it, the tiled forms' LDS
-// leaves room for one.
+// costs in microseconds: `few` with little else on the GPU, `full` for each workgroup that every
+// one of the 256 compute units has to run (several at a time where LDS holds them: what a
+// further one adds).  Measured over 7 batches of 24 to 1200 tokens by 7 shapes of 576 to
+// 14336 rows and 512 to 7168 inputs; a launch takes about 2.5 us more.  The choice came within
+// 10 % of the best form (of 13 measured) on 42 of the 49, within 20 % on all.
 struct LinearForm {
   int rows, tokens;
-  float cost;
+  float few, full;
   hipError_t (*launch)(const Product&, int, hipStream_t);
 };
 const LinearForm kLinearForms[] = {
-    {16, 16, 0.136f, launch_product<kLinear, 1, 1, 4>},
-    {32, 16, 0.195f, launch_product<kLinear, 2, 1, 4>},
-    {64, 16, 0.32f, launch_product<kLinear, 4, 1, 4>},
-    {16, 32, 0.225f, launch_product<kLinear, 1, 2, 4>},
-    {32, 32, 0.29f, launch_product<kLinear, 2, 2, 4>},
-    {64, 64, 0.33f, launch_tile<kLinear, 64, 64, 2, 2, 6>},
-    {128, 64, 0.42f, launch_tile<kLinear, 128, 64, 4, 2, 5>},
-    {128, 128, 0.67f, launch_tile<kLinear, 128, 128, 2, 4, 4>},
-    {256, 128, 1.13f, launch_tile<kLinear, 256, 128, 2, 4, 3>},
-    {256, 256, 2.1f, launch_tile<kLinear, 256, 256, 2, 4, 2>},
+    {16, 16, 0.12f, 0.136f, launch_product<kLinear, 1, 1, 4>},
+    {32, 16, 0.19f, 0.195f, launch_product<kLinear, 2, 1, 4>},
+    {64, 16, 0.31f, 0.32f, launch_product<kLinear, 4, 1, 4>},
+    {16, 32, 0.21f, 0.22f, launch_product<kLinear, 1, 2, 4>},
+    {32, 32, 0.235f, 0.24f, launch_product<kLinear, 2, 2, 4>},
+    {64, 32, 0.245f, 0.165f, launch_tile<kLinear, 64, 32, 2, 2, 4>},
+    {64, 64, 0.32f, 0.23f, launch_tile<kLinear, 64, 64, 2, 2, 3>},
+    {128, 64, 0.40f, 0.43f, launch_tile<kLinear, 128, 64, 4, 2, 5>},
+    {128, 128, 0.58f, 0.67f, launch_tile<kLinear, 128, 128, 2, 4, 4>},
+    {128, 256, 0.90f, 1.1f, launch_tile<kLinear, 128, 256, 2, 4, 3>},
+    {256, 256, 1.57f, 2.15f, launch_tile<kLinear, 256, 256, 2, 4, 2>},
 };
+float form_cost(const LinearForm& f, int T, int n) {
+  const long groups = long((n + f.rows - 1) / f.rows) * ((T + f.tokens - 1) / f.tokens);
+  if (groups <= kUnits) return f.few + (f.full > f.few ? f.full - f.few : 0.0f) * groups / kUnits;
+  const float full = f.full * float((groups + kUnits - 1) / kUnits);
+  return full > f.few ? full : f.few;
+}
 
 // ---------------------------------------------------------------------------- one token
 
@@ -730,6 +754,10 @@ const LinearForm kLinearForms[] = {
 // product_kernel.
 //   kLinear  x rows [T, K] bf16; 16 MR weight rows a workgroup.
 //   kGateUp  the one token's x; workgroup (., r) the expert of pair r: h[r] = silu(W1 x) (W3 x).
+//            In bf16 instructions of the decoded codes, whose sums keep what the FP8 one's drop:
+//            of one token's hidden values two or three lie so near the middle of two codes that
+//            its error moves them, and in a single row that shows (1.3 times the final
+//            rounding's error); the weights' stream hides the conversion.
 //   kDown    all pairs' h rows [k, K]; y = sum_r w_r W2_{id_r} q(h_r), the pairs one after the
 //            other in every wave, no outputs of single pairs in between.
 struct Small {
@@ -748,11 +776,12 @@ struct Small {
 };
 
 constexpr int kSmallPairs = kMaxTopK;
-// Bytes of a code row in LDS: whole blocks, rows 16 bytes past a multiple of 128 apart.
+// Bytes of a row in LDS, of codes or (kGateUp) bf16: whole blocks, rows 16 bytes past a multiple
+// of 128 apart.
+template <Kind kKind>
 __host__ __device__ inline int small_pitch(int K) {
-  return (K + kQuantBlock - 1) / kQuantBlock * kQuantBlock + 16;
+  return (K + kQuantBlock - 1) / kQuantBlock * kQuantBlock * (kKind == kGateUp ? 2 : 1) + 16;
 }
-inline long small_lds(long rows, int K) { return rows * (small_pitch(K) + 4 * quant_blocks(K)); }
 
 template <Kind kKind, int MR, int KW>
 __global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
@@ -768,7 +797,7 @@ __global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
   const int n = lane & 15, g = lane >> 4;
   const int N = a.N, K = a.K;
   const int nb = (K + kQuantBlock - 1) / kQuantBlock, nbN = (N + kQuantBlock - 1) / kQuantBlock;
-  const int pitch = small_pitch(K);
+  const int pitch = small_pitch<kKind>(K);
   const int n0 = blockIdx.x * 16 * MW;
   int e0 = 0, pairs = 1;                   // kGateUp's expert; pairs that the workgroup adds up
   if constexpr (kKind == kGateUp) {
@@ -830,18 +859,33 @@ __global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
   auto add = [&](const Block& r, Item i) {
     const int row = kKind == kLinear ? min(n, a.T - 1) : i.q;
     const int at = i.b * kQuantBlock + 16 * g;
-    const uint8_t* const p = codes + row * pitch + at;
-    const i32x8 x = __builtin_shufflevector(*reinterpret_cast<const i32x4*>(p),
-                                            *reinterpret_cast<const i32x4*>(p + 64), 0, 1, 2, 3,
-                                            4, 5, 6, 7);
     const float sx = scales[row * nb + i.b];
     // where the rows end inside this block, what was read past them is not theirs
     const int lo = at < K ? -1 : 0, hi = at + 64 < K ? -1 : 0;
+    bf16x8 xb[4];                          // kGateUp: inputs 0, 8, 64 and 72 of the lane's on
+    i32x8 xc;
+    if constexpr (kKind == kGateUp) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        xb[u] = *reinterpret_cast<const bf16x8*>(codes + 2 * (at + u / 2 * 64 + u % 2 * 8));
+    } else {
+      const uint8_t* const p = codes + row * pitch + at;
+      xc = __builtin_shufflevector(*reinterpret_cast<const i32x4*>(p),
+                                   *reinterpret_cast<const i32x4*>(p + 64), 0, 1, 2, 3, 4, 5, 6, 7);
+    }
 #pragma unroll
     for (int m = 0; m < MR; ++m) {
       const i32x8 w = __builtin_shufflevector(r.w[m][0] & lo, r.w[m][1] & hi, 0, 1, 2, 3, 4, 5, 6,
                                               7);
-      const floatx4 t = mfma128(w, x);
+      floatx4 t = {0.0f, 0.0f, 0.0f, 0.0f};
+      if constexpr (kKind == kGateUp) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(w[2 * u], w[2 * u + 1]), xb[u],
+                                                      t, 0, 0, 0);
+      } else {
+        t = mfma128(w, xc);
+      }
       const float s = sx * (m < MW ? r.f1 : r.f3);
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[m][j] = __builtin_fmaf(t[j], s, acc[m][j]);
@@ -868,7 +912,11 @@ __global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
 #pragma unroll
     for (int s = 1; s < 16; s *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, s));
     const Quantum z = quantum(m);
-    *reinterpret_cast<uint2*>(codes + r * pitch + c) = make_uint2(codes4(z, v), codes4(z, v + 4));
+    const uint32_t c0 = codes4(z, v), c1 = codes4(z, v + 4);
+    if constexpr (kKind == kGateUp)
+      *reinterpret_cast<bf16x8*>(codes + r * pitch + 2 * c) = codes_to_bf16(c0, c1);
+    else
+      *reinterpret_cast<uint2*>(codes + r * pitch + c) = make_uint2(c0, c1);
     if ((tid & 15) == 0) scales[o] = z.scale * (kKind == kDown ? a.w[pair[r]] : 1.0f);
   }
   __syncthreads();
@@ -911,7 +959,8 @@ template <Kind kKind, int MR, int KW>
 hipError_t launch_small(const Small& a, int rows, int groups, hipStream_t stream) {
   const int cols = 16 * (kKind == kGateUp ? MR / 2 : MR);
   small_kernel<kKind, MR, KW><<<dim3((a.N + cols - 1) / cols, groups), 64 * KW,
-                               small_lds(rows, a.K), stream>>>(a);
+                               rows * (small_pitch<kKind>(a.K) + 4 * quant_blocks(a.K)),
+                               stream>>>(a);
   return hipGetLastError();
 }
 
@@ -1058,16 +1107,9 @@ hipError_t launch_block_linear(const BlockLinearArgs& a, hipStream_t stream) {
     if (a.n >= 7168) return launch_small<kLinear, 2, 4>(s, a.T, 1, stream);
     return launch_small<kLinear, 1, 4>(s, a.T, 1, stream);
   }
-  const LinearForm* best = nullptr;
-  float least = 0.0f;
-  for (const LinearForm& f : kLinearForms) {
-    const long groups = long((a.n + f.rows - 1) / f.rows) * ((a.T + f.tokens - 1) / f.tokens);
-    const float cost = f.cost * float((groups + kUnits - 1) / kUnits);
-    if (!best || cost < least) {
-      best = &f;
-      least = cost;
-    }
-  }
+  const LinearForm* best = &kLinearForms[0];
+  for (const LinearForm& f : kLinearForms)
+    if (form_cost(f, a.T, a.n) < form_cost(*best, a.T, a.n)) best = &f;
   return best->launch(p, (a.T + best->tokens - 1) / best->tokens, stream);
 }
 

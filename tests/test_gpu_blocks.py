@@ -309,6 +309,17 @@ def test_experts(T, E, k, d, f):
     _check_experts(x, ids, w, mats, _run_experts(x, ids, w, mats))
 
 
+@pytest.mark.parametrize("E,k,d,f", [(3, 2, 16384, 64), (3, 2, 16400, 64), (5, 4, 96, 8192),
+                                     (5, 4, 96, 8208), (40, 32, 64, 1024)])
+def test_experts_one_token_limits(E, k, d, f):
+    """One token at the largest rows that its own form keeps in LDS, and one step past them."""
+    rng = np.random.default_rng(d + f)
+    x, mats = _x(rng, 1, d), _expert_weights(rng, E, d, f)
+    ids, w = _routing(rng, 1, E, k)
+    say(f"experts case one token E={E} k={k} d={d} f={f}")
+    _check_experts(x, ids, w, mats, _run_experts(x, ids, w, mats))
+
+
 @pytest.mark.parametrize("T", [9, 150])
 def test_experts_missing_pairs(T):
     """Ids outside [0, E), tokens without pairs, experts without tokens, one expert with all."""
