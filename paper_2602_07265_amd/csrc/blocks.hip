@@ -12,6 +12,9 @@
 // The instruction aligns the products of eight neighbouring inputs to their largest and keeps
 // about 13 bits below it: 1.4e-5 of the result's RMS on Gaussian data, against 1.7e-3 of the
 // final rounding to bf16.
+//
+// With the four multiply-adds that enter a result, an instruction takes 37 cycles of its matrix
+// core, 32 without (3.6 and 4.4 PFLOP/s over the whole GPU when nothing else is done).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -151,7 +154,9 @@ __device__ __forceinline__ void quantize_rows(const In* x, long rows, int cols, 
   }
 }
 
-// `live`: nullable count of rows on the device, at most `rows`.
+// Bound by memory: 4000 x 7168 in 18.2 us, 4.7 TB/s of reads and writes (a large copy: 4.9); wide
+// loads and stores, several blocks in flight a thread row.  `live`: nullable count of rows on
+// the device, at most `rows`.
 template <typename In>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const In* x, int rows, int cols,
                                                             long ld, uint8_t* q, float* scales,
@@ -160,7 +165,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const In* x, int row
                 (long)blockIdx.x * 16 + (threadIdx.x >> 4), (long)gridDim.x * 16);
 }
 
-// Blocks of 128 x 128: one workgroup a block, 64 values a thread (row threadIdx / 16 + 16 i).
+// Blocks of 128 x 128: one workgroup a block, 64 values a thread (row threadIdx / 16 + 16 i), which
+// stay in registers between the maximum and the codes: one read.  14336 x 4096 in 34 us, the
+// rate of a large copy.
 __global__ __launch_bounds__(256) void quantize_tile_kernel(const uint16_t* x, int rows, int cols,
                                                             long ld, uint8_t* q, float* scales) {
   __shared__ uint32_t part[4];
@@ -232,6 +239,8 @@ typedef const __attribute__((address_space(4))) float* ScalarPtr;   // read by s
 // no wave reads what another does and no barrier stands in the loop; the weights go from
 // memory straight into the instruction's operands, the next block's loads in flight under
 // this one's instructions.  The waves' sums meet in LDS at the end, added in wave order.
+// Bound by the weights' stream, and below a few MB by its latency: 16 x 7168 x 2048 takes 5.9 us
+// (2.5 TB/s), 45 x 1367 x 2720 5.5; more waves over K (8, 16) measured equal or slower.
 template <Kind kKind, int MR, int NT, int KW>
 __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
   constexpr int kRows = 16 * NT;
@@ -383,6 +392,15 @@ __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
 // c ^ ((r >> 1) & 7): the sixteen rows of an operand read then lie in sixteen different
 // places modulo 256 bytes.  The loads write LDS in lane order, so the lanes take their
 // source pieces in that order.
+//
+// Few tokens an expert: bound by HBM, 228 us for the 1.41 GB of 48 experts' W1 and W3 (6.2 TB/s)
+// and 128 us for W2 (5.5).  64 tokens an expert over 256 of them: 1.43 ms (5.3 TB/s; the
+// experts past 128 tokens read their weights again) and 0.86 ms, of which the fp32 outputs'
+// stores are 0.12.  4000 x 4096 x 7168 in 256 x 256 tiles: 117 us, 2.0 PFLOP/s, at a clock that
+// falls to 1.5-2.0 GHz; the loads alone would take 88 us, the instructions and reads of LDS
+// alone 108.  Tried without gain: tiles ordered for the eight L2 caches, prefetching into
+// them, persistent workgroups that load the next tile's operands before they store, 16 waves,
+// reading the next block's operands under this one's instructions.
 typedef const __attribute__((address_space(1))) void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
@@ -760,6 +778,9 @@ float form_cost(const LinearForm& f, int T, int n) {
 //            rounding's error); the weights' stream hides the conversion.
 //   kDown    all pairs' h rows [k, K]; y = sum_r w_r W2_{id_r} q(h_r), the pairs one after the
 //            other in every wave, no outputs of single pairs in between.
+// Bound by the weights' latency and stream: 1 x 7168 x 2048 in 6.1 us; eight (2048, 768) experts'
+// 25 MB and 13 MB in 8.9 and 7.1 us.  The first weights are under way while the rows are
+// quantised (9.7 -> 8.9 us).
 struct Small {
   const uint16_t* x;           // kLinear, kGateUp
   long ldx;
@@ -967,10 +988,11 @@ hipError_t launch_small(const Small& a, int rows, int groups, hipStream_t stream
 // ---------------------------------------------------------------------------- experts
 
 // What the products of the experts need: x quantised, and the pairs in expert order.  The first E
-// workgroups are an expert's each, over all ids; the rest take the blocks of x.  The one counts the pairs
-// of every expert (in LDS) and, wave by wave, its own; its rows begin after those of the
+// workgroups are an expert's each, over all ids; the rest take the blocks of x.  An expert's
+// counts the pairs of every expert (in LDS) and, wave by wave, its own; its rows begin after those of the
 // experts before it, its tiles of either product likewise, and its pairs are listed in
-// ascending order.
+// ascending order.  No atomics but those counts, so every call lists them alike.  4.8 us for 32
+// tokens of 7168 and 256 experts, 20 us for 2048 (the E passes over 16384 ids).
 struct Prepare {
   const uint16_t* x;
   int T, d;
@@ -1046,7 +1068,9 @@ __global__ __launch_bounds__(1024) void prepare_kernel(Prepare a) {
   }
 }
 
-// y_i = sum_r w_ir o[i k + r], rank order, eight columns a thread.
+// y_i = sum_r w_ir o[i k + r], rank order, eight columns a thread.  The pairs' outputs stay fp32:
+// rounded to bf16 their error (1.6 times the final rounding's) would show in y.  Bound by
+// reading them: 2048 tokens of 8 x 7168 in 100 us, 5.0 TB/s.
 __global__ __launch_bounds__(256) void combine_kernel(const float* o, const int32_t* ids,
                                                       const float* w, int k, int E, int d,
                                                       uint16_t* y, long ldy) {

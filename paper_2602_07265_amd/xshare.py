@@ -110,7 +110,6 @@ class BlockExpertsArgs(ctypes.Structure):
 WEIGHTS = {"bf16": 0, "fp8": 1, "mxfp4": 2}
 GATE = {"softmax": 0, "sigmoid": 1}
 GROUP = {"max": 0, "top2": 1}
-LOGITS = {torch.float32: 0, torch.bfloat16: 1}
 
 STATS_FIELDS = ("n_selected", "n_active", "n_vanilla_union", "n_warmup", "n_start",
                 "budget_eff", "max_group_load")
@@ -898,7 +897,7 @@ def _rows(t, dtype, name, cols=None):
     if t.dim() != 2 or (cols is not None and t.shape[1] != cols):
         raise ValueError(f"{name} must be a matrix" + ("" if cols is None else f" of {cols} columns")
                          + f", got {tuple(t.shape)}")
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: the elements of a row must be neighbours")
     return ld
@@ -911,17 +910,15 @@ def _same_device(x, *others):
             raise ValueError(f"tensors on {at} and {t.device}")
 
 
-# The handle of a device's current stream without a Stream object (3 us less a call, of about
-# 8 that the shortest of these calls take).
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-
 def _stream_of(x, stream):
+    """The handle of x's device's current stream, without a Stream object where torch gives it
+    (3 us less a call, of about 10 that the shortest of these calls take)."""
     if stream is not None:
         return stream.cuda_stream
-    if _raw_stream is None:
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
         return torch.cuda.current_stream(x.device).cuda_stream
-    return _raw_stream(x.device.index)
+    return raw(x.device.index)
 
 
 def _gate_params(N, top_k, score, n_groups, top_groups, group_score, renormalize, scale):
@@ -932,9 +929,10 @@ def _gate_params(N, top_k, score, n_groups, top_groups, group_score, renormalize
 
 
 def _logits(logits):
-    if not isinstance(logits, torch.Tensor) or logits.dtype not in LOGITS:
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in (torch.float32,
+                                                                    torch.bfloat16):
         raise ValueError("logits must be a float32 or bfloat16 GPU tensor")
-    return LOGITS[logits.dtype], _rows(logits, logits.dtype, "logits")
+    return int(logits.dtype == torch.bfloat16), _rows(logits, logits.dtype, "logits")
 
 
 def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_groups: int = 1,
