@@ -108,6 +108,7 @@ class BlockExpertsArgs(ctypes.Structure):
 
 
 WEIGHTS = {"bf16": 0, "fp8": 1, "mxfp4": 2}
+_EXPERTS_ARGS_BYTES = ctypes.sizeof(BlockExpertsArgs)
 GATE = {"softmax": 0, "sigmoid": 1}
 GROUP = {"max": 0, "top2": 1}
 
@@ -903,11 +904,19 @@ def _rows(t, dtype, name, cols=None):
     return ld
 
 
-def _same_device(x, *others):
-    at = x.device
-    for t in others:
-        if t is not None and t.device != at:
-            raise ValueError(f"tensors on {at} and {t.device}")
+def _fit(device, *wanted):
+    """Checks (tensor, dtype, shape, name) against a call's device, in few lookups: the shortest
+    calls take about as long as their checks."""
+    for t, dtype, shape, name in wanted:
+        if t.dtype is not dtype or t.shape != shape or t.device != device \
+                or not t.is_contiguous():
+            _dev(t, dtype, shape, name)
+            raise ValueError(f"{name} is on {t.device}, not {device}")
+
+
+def _on(device, t, name):
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
 
 
 def _stream_of(x, stream):
@@ -945,17 +954,16 @@ def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_grou
     T, N = logits.shape
     k = int(top_k)
     if bias is not None:
-        _dev(bias, torch.float32, (N,), "bias")
-        _same_device(logits, bias)
+        _fit(logits.device, (bias, torch.float32, (N,), "bias"))
     ids, w = (None, None) if out is None else (out.get("ids"), out.get("w"))
     if ids is None:
         ids = logits.new_empty((T, max(k, 0)), dtype=torch.int32)
     else:
-        _same_device(logits, _dev(ids, torch.int32, (T, k), "ids"))
+        _fit(logits.device, (ids, torch.int32, (T, k), "ids"))
     if w is None:
         w = logits.new_empty((T, max(k, 0)), dtype=torch.float32)
     else:
-        _same_device(logits, _dev(w, torch.float32, (T, k), "w"))
+        _fit(logits.device, (w, torch.float32, (T, k), "w"))
     p = _gate_params(N, k, score, n_groups, top_groups, group_score, renormalize, scale)
     st = lib().xshare_gate(logits.data_ptr(), dtype, T, ld,
                            None if bias is None else bias.data_ptr(), ctypes.byref(p),
@@ -972,13 +980,11 @@ def gate_backward(logits: torch.Tensor, ids: torch.Tensor, dw: torch.Tensor, *, 
     dtype, ld = _logits(logits)
     T, N = logits.shape
     k = ids.shape[1] if ids.dim() == 2 else -1
-    _dev(ids, torch.int32, (T, k), "ids")
-    _dev(dw, torch.float32, (T, k), "dw")
+    _fit(logits.device, (ids, torch.int32, (T, k), "ids"), (dw, torch.float32, (T, k), "dw"))
     if out is None:
         out = logits.new_empty((T, N), dtype=torch.float32)
     else:
-        _dev(out, torch.float32, (T, N), "out")
-    _same_device(logits, ids, dw, out)
+        _fit(logits.device, (out, torch.float32, (T, N), "out"))
     p = _gate_params(N, k, score, 1, 1, "max", renormalize, scale)
     st = lib().xshare_gate_backward(logits.data_ptr(), dtype, T, ld, ctypes.byref(p),
                                     ids.data_ptr(), dw.data_ptr(), out.data_ptr(),
@@ -1002,11 +1008,11 @@ def block_quantize(x: torch.Tensor, block_rows: int = 1, *, out=None, stream=Non
     if q is None:
         q = x.new_empty((rows, cols), dtype=torch.uint8)
     else:
-        _same_device(x, _dev(q, torch.uint8, (rows, cols), "codes"))
+        _fit(x.device, (q, torch.uint8, (rows, cols), "codes"))
     if s is None:
         s = x.new_empty(shape, dtype=torch.float32)
     else:
-        _same_device(x, _dev(s, torch.float32, shape, "scales"))
+        _fit(x.device, (s, torch.float32, shape, "scales"))
     st = lib().xshare_block_quantize(x.data_ptr(), rows, cols, ld, int(block_rows), q.data_ptr(),
                                      s.data_ptr(), _stream_of(x, stream))
     _check(st, "xshare_block_quantize")
@@ -1026,28 +1032,30 @@ def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale
     if wq.dim() != 2:
         raise ValueError("wq must be a matrix of codes")
     n, k = wq.shape
-    _dev(wq, torch.uint8, (n, k), "wq")
-    _dev(ws, torch.float32, (_blocks(n), _blocks(k)), "ws")
-    if x_scale is None:
+    own = x_scale is None
+    if own:
         ldx = _rows(x, torch.bfloat16, "x", k)
     else:
         ldx = k
         _dev(x, torch.uint8, (x.shape[0], k), "x codes")
-        _dev(x_scale, torch.float32, (x.shape[0], _blocks(k)), "x_scale")
-    T = x.shape[0]
+        _fit(x.device, (x_scale, torch.float32, (x.shape[0], _blocks(k)), "x_scale"))
+    dev, T, L = x.device, x.shape[0], lib()
+    _fit(dev, (wq, torch.uint8, (n, k), "wq"),
+         (ws, torch.float32, (_blocks(n), _blocks(k)), "ws"))
     if y is None:
         y, ldy = x.new_empty((T, n), dtype=torch.bfloat16), n
     else:
         ldy = _rows(y, torch.bfloat16, "y", n)
+        _on(dev, y, "y")
         if y.shape[0] != T:
             raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
-    own = x_scale is None
-    if workspace is None and own:
-        workspace = x.new_empty(lib().xshare_block_linear_workspace_bytes(T, n, k),
+    if workspace is not None:
+        _on(dev, workspace, "workspace")
+    elif own:
+        workspace = x.new_empty(L.xshare_block_linear_workspace_bytes(T, n, k),
                                 dtype=torch.uint8)
-    _same_device(x, wq, ws, x_scale, y, workspace)
     px = x.data_ptr()
-    st = lib().xshare_block_linear(px if own else None, ldx, None if own else px,
+    st = L.xshare_block_linear(px if own else None, ldx, None if own else px,
                                    None if own else x_scale.data_ptr(), T, n, k, wq.data_ptr(),
                                    ws.data_ptr(), y.data_ptr(), ldy,
                                    None if workspace is None else workspace.data_ptr(),
@@ -1075,30 +1083,30 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
         raise ValueError("weights are [N, f, d], ids [T, k]")
     N, f = q1.shape[0], q1.shape[1]
     k = ids.shape[1]
-    _dev(ids, torch.int32, (T, k), "ids")
-    _dev(w, torch.float32, (T, k), "w")
-    _dev(q1, torch.uint8, (N, f, d), "w1 codes")
-    _dev(q3, torch.uint8, (N, f, d), "w3 codes")
-    _dev(q2, torch.uint8, (N, d, f), "w2 codes")
-    _dev(s1, torch.float32, (N, _blocks(f), _blocks(d)), "w1 scales")
-    _dev(s3, torch.float32, (N, _blocks(f), _blocks(d)), "w3 scales")
-    _dev(s2, torch.float32, (N, _blocks(d), _blocks(f)), "w2 scales")
+    dev, L = x.device, lib()
+    up, down = (N, _blocks(f), _blocks(d)), (N, _blocks(d), _blocks(f))
+    _fit(dev, (ids, torch.int32, (T, k), "ids"), (w, torch.float32, (T, k), "w"),
+         (q1, torch.uint8, (N, f, d), "w1 codes"), (q3, torch.uint8, (N, f, d), "w3 codes"),
+         (q2, torch.uint8, (N, d, f), "w2 codes"), (s1, torch.float32, up, "w1 scales"),
+         (s3, torch.float32, up, "w3 scales"), (s2, torch.float32, down, "w2 scales"))
     if y is None:
         y, ldy = x.new_empty((T, d)), d
     else:
         ldy = _rows(y, torch.bfloat16, "y", d)
+        _on(dev, y, "y")
         if y.shape[0] != T:
             raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
     if workspace is None:
-        workspace = x.new_empty(lib().xshare_block_experts_workspace_bytes(T, k, N, d, f),
+        workspace = x.new_empty(L.xshare_block_experts_workspace_bytes(T, k, N, d, f),
                                 dtype=torch.uint8)
-    _same_device(x, ids, w, q1, q3, q2, s1, s3, s2, y, workspace)
-    a = BlockExpertsArgs(ctypes.sizeof(BlockExpertsArgs), T, k, N, d, f, x.data_ptr(), ldx,
+    else:
+        _on(dev, workspace, "workspace")
+    a = BlockExpertsArgs(_EXPERTS_ARGS_BYTES, T, k, N, d, f, x.data_ptr(), ldx,
                          ids.data_ptr(), w.data_ptr(), q1.data_ptr(), q3.data_ptr(),
                          q2.data_ptr(), s1.data_ptr(), s3.data_ptr(), s2.data_ptr(),
                          y.data_ptr(), ldy, workspace.data_ptr(), workspace.numel(),
                          _stream_of(x, stream))
-    _check(lib().xshare_block_experts(ctypes.byref(a)), "xshare_block_experts")
+    _check(L.xshare_block_experts(ctypes.byref(a)), "xshare_block_experts")
     return y
 
 
