@@ -34,6 +34,13 @@ constexpr float kLeastSum = 0x1p-126f;
 
 __device__ __forceinline__ float from_bf16(uint32_t b) { return __uint_as_float(b << 16); }
 
+// What a lane wrote to the wave's part of LDS before this, its other lanes read after it (the wave's
+// LDS operations are done in order; the compiler keeps that order here).
+__device__ __forceinline__ void lanes_meet() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Logit j of a row; + 0.0 makes -0.0 equal to +0.0.
 __device__ __forceinline__ float logit(const GateArgs& a, const void* row, int j) {
   const float h = a.bf16 ? from_bf16(static_cast<const uint16_t*>(row)[j])
@@ -132,6 +139,7 @@ __device__ __forceinline__ void limit_groups(const GateArgs& a, int lane, uint32
 #pragma unroll
     for (int q = 0; q < Q; ++q)
       if (Q * lane + q < a.N) copy[Q * lane + q] = base[q];
+    lanes_meet();
     if (lane < a.G)
       for (int i = 0; i < size; ++i) top.add(copy[lane * size + i]);
   }
@@ -229,7 +237,9 @@ __global__ __launch_bounds__(64 * kWaves) void gate_backward_kernel(GateArgs a) 
   const float dot = a.sigmoid || a.renormalize ? 0.0f : wave_sum(ds * s);
 #pragma unroll
   for (int q = 0; q < Q; ++q) mine[Q * lane + q] = 0.0f;
+  lanes_meet();
   if (id >= 0) mine[id] = ds;
+  lanes_meet();
   float* const out = a.dlogits + (size_t)t * a.N + Q * lane;
   float d[Q];
 #pragma unroll
