@@ -30,7 +30,7 @@ struct GateArgs {
   float* w;
   const float* dw;             // backward: [T, k]
   float* dlogits;              // [T, N]
-  int vec, vec_out;            // rows aligned for wide loads and stores (set by the launch)
+  int vec, vec_bias, vec_out;  // aligned for wide loads and stores (set by the launch)
 };
 
 hipError_t launch_gate(const GateArgs& a, hipStream_t stream);

@@ -8,8 +8,8 @@
 // lane for each group.
 //
 // A call reads T N logits and writes T k pairs, 9 MB at T = 8192, N = 256, about 2 us of
-// memory time; the instructions of the rounds and scores bound it there (11 us in groups of 32,
-// k = 8), the launch and the rounds' chain at T = 1 (4.4 us).  With reductions through LDS
+// memory time; the instructions of the rounds and scores bound it there (10.4 us in groups of 32,
+// k = 8), the launch and the rounds' chain at T = 1 (4.2 us).  With reductions through LDS
 // instead of DPP it took 19.5 and 7.5 us.
 //
 // Compiled with -ffp-contract=off: every step of a score is one fp32 operation.
@@ -102,6 +102,29 @@ __device__ __forceinline__ void load_row(const GateArgs& a, const void* row, int
   z = fmaxf(wave_sum(z), kLeastSum);
 }
 
+// The lane's biases (0 past N and where there are none), under way while the row is loaded.
+template <int Q>
+__device__ __forceinline__ void load_bias(const GateArgs& a, int lane, float (&b)[Q]) {
+  const int j0 = Q * lane;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) b[q] = 0.0f;
+  if (!a.bias) return;
+  if (Q > 1 && a.vec_bias) {
+    if (j0 < a.N) {
+#pragma unroll
+      for (int q = 0; q < Q; q += 2) {
+        const float2 v = *reinterpret_cast<const float2*>(a.bias + j0 + q);
+        b[q] = v.x;
+        b[q + (Q > 1)] = v.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+      if (j0 + q < a.N) b[q] = a.bias[j0 + q];
+  }
+}
+
 // The two best of a group, from its parts'.
 struct Top2 {
   uint32_t b1, b2;
@@ -170,7 +193,8 @@ __global__ __launch_bounds__(64 * kWaves) void gate_kernel(GateArgs a) {
   const int t = blockIdx.x * kWaves + wave;
   if (t >= a.T) return;
   const void* const row = logits_row(a, t);
-  float h[Q], m, z;
+  float h[Q], b[Q], m, z;
+  load_bias<Q>(a, lane, b);
   load_row<Q>(a, row, lane, h, m, z);
   const bool grouped = a.top_groups < a.G;
   uint32_t key[Q], base[Q];
@@ -181,7 +205,7 @@ __global__ __launch_bounds__(64 * kWaves) void gate_kernel(GateArgs a) {
     if (j >= a.N) continue;
     const bool plain = !a.bias && !(grouped && a.top2);
     const float s = plain ? 0.0f : score(a, h[q], m, z);
-    const float c = a.bias ? s + a.bias[j] : h[q];
+    const float c = a.bias ? s + b[q] : h[q];
     const bool masked = h[q] == -INFINITY;           // ranks last, whatever its bias
     key[q] = ord(masked ? -INFINITY : c);
     base[q] = a.top2 ? ord(masked ? 0.0f : a.bias ? c : s) : key[q];
@@ -222,6 +246,8 @@ __global__ __launch_bounds__(64 * kWaves) void gate_backward_kernel(GateArgs a) 
   if (t >= a.T) return;
   const void* const row = logits_row(a, t);
   float* const mine = rows[wave];
+#pragma unroll
+  for (int q = 0; q < Q; ++q) mine[Q * lane + q] = 0.0f;
   int id = lane < a.k ? a.ids[(size_t)t * a.k + lane] : -1;
   if (id < 0 || id >= a.N) id = -1;
   float h[Q], m, z;
@@ -235,8 +261,9 @@ __global__ __launch_bounds__(64 * kWaves) void gate_backward_kernel(GateArgs a) 
   }
   // softmax's common term, sum of ds s, which renormalised weights make zero
   const float dot = a.sigmoid || a.renormalize ? 0.0f : wave_sum(ds * s);
+  float sj[Q];
 #pragma unroll
-  for (int q = 0; q < Q; ++q) mine[Q * lane + q] = 0.0f;
+  for (int q = 0; q < Q; ++q) sj[q] = score(a, h[q], m, z);
   lanes_meet();
   if (id >= 0) mine[id] = ds;
   lanes_meet();
@@ -244,8 +271,8 @@ __global__ __launch_bounds__(64 * kWaves) void gate_backward_kernel(GateArgs a) 
   float d[Q];
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
-    const float sj = score(a, h[q], m, z), dj = mine[Q * lane + q];
-    d[q] = a.sigmoid ? dj * sj * (1.0f - sj) : sj * (dj - dot);
+    const float dj = mine[Q * lane + q];
+    d[q] = a.sigmoid ? dj * sj[q] * (1.0f - sj[q]) : sj[q] * (dj - dot);
   }
   if (Q > 1 && a.vec_out) {
     if (Q * lane < a.N)
@@ -280,6 +307,7 @@ hipError_t launch_gate(const GateArgs& args, hipStream_t stream) {
     constexpr int Q = decltype(q)::value;
     GateArgs a = args;
     a.vec = pairs_aligned(a.logits, a.ld, a.N, Q, a.bf16 ? 2 : 4);
+    a.vec_bias = pairs_aligned(a.bias, a.N, a.N, Q, 4);
     gate_kernel<Q><<<(a.T + kWaves - 1) / kWaves, 64 * kWaves, 0, stream>>>(a);
     return hipGetLastError();
   });

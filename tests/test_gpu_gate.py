@@ -93,6 +93,20 @@ def test_batches(T):
     _check(_rows(rng, T, 256, kw, "fp32"), "fp32", kw, "batch")
 
 
+@pytest.mark.parametrize("N,shift", [(256, 1), (256, 2), (128, 3), (65, 1)])
+def test_bias_at_any_address(N, shift):
+    from paper_2602_07265_amd import xshare as X
+    rng = np.random.default_rng(N + shift)
+    h = torch.from_numpy(rng.normal(0, 1, (9, N)).astype(np.float32)).to(DEV)
+    bias = torch.full((N + 8,), float("nan"), device=DEV)
+    bias[shift:shift + N] = torch.from_numpy(rng.normal(0, 0.3, N).astype(np.float32)).to(DEV)
+    part = bias[shift:shift + N]
+    say(f"gate case bias {shift} floats on N={N}")
+    a = X.gate(h, 6, score="sigmoid", bias=part)
+    b = X.gate(h, 6, score="sigmoid", bias=part.clone())
+    assert torch.equal(a["ids"], b["ids"]) and torch.equal(a["w"], b["w"])
+
+
 def test_ties_go_to_the_lower_index():
     kw = dict(top_k=5, score="sigmoid")
     h = np.zeros((3, 70), np.float32)
