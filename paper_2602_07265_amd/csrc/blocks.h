@@ -55,9 +55,11 @@ inline BlockLinearLayout block_linear_layout(int T, int k) {
   return L;
 }
 
-// Whether a product quantises x as it goes (launch_block_linear with x given): up to 16 rows and
-// 32768 values.
-inline bool block_linear_small(int T, int k) { return T <= 16 && long(T) * k <= 32768; }
+// Whether a product quantises x in every workgroup, a launch less (launch_block_linear with x
+// given): up to 16 rows of 16384 values in all.  One row of 2048 by 7168 takes 5.3 us so, 6.9 in
+// two launches; 4 rows of 4096 by 4096 8.6 and 8.9; 8 of 2048 by 7168 7.0 and 7.6, by 14336 11.5
+// and 10.7; past the limit 16 of 2048 by 7168 9.0 and 8.3, 4 of 7168 by 7168 16.3 and 14.6.
+inline bool block_linear_small(int T, int k) { return T <= 16 && long(T) * k <= 16384; }
 
 struct BlockLinearArgs {
   int T, n, k;

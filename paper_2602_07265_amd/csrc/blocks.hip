@@ -19,6 +19,7 @@
 #include <stdint.h>
 
 #include "blocks.h"
+#include "wave.h"
 
 namespace xs {
 namespace {
@@ -62,23 +63,29 @@ __device__ __forceinline__ uint16_t to_bf16(float v) {
 constexpr float kMaxCode = 448.0f;               // largest E4M3 value
 constexpr float kTiny = 448.0f * 0x1p-126f;      // least maximum a scale is made from
 
-// What a block's values are quantised with.  code = rne(448 x / a) wants the quotient
-// correctly rounded, so that a bf16 x gives the code of exact arithmetic even where the
-// quotient lies on the middle of two codes; with r = 1 / a rounded, q = t r and one step
-// q + (t - q a) r do it, all operands scaled by `pre` out of the ranges where they would
-// overflow or lose bits.
+// What a block's values are quantised with.  code = rne(448 x / a) wants the quotient of a bf16
+// x correctly rounded, so that it gives the code of exact arithmetic even where the quotient lies
+// on the middle of two codes.  With r = 1 / a to a rounding or so, q = t r and one step q + (t -
+// q a) r do it: the step's own error is about 2^-23 roundings of q, and t / a of a t of 11 bits
+// and an a of 8 is no nearer than 2^-9 to where the rounding turns.  All operands are scaled by
+// `pre` out of the ranges where they would overflow or lose bits.  The scale a / 448 is correctly
+// rounded for every a by the same step, 1 / 448 being so.
 struct Quantum {
   float a, r, pre, scale;
   bool finite;
 };
 __device__ __forceinline__ Quantum quantum(uint32_t abs_bits) {
+  constexpr float kInverse = 1.0f / kMaxCode;
   Quantum z;
   const float a = fmaxf(__uint_as_float(abs_bits), kTiny);
   z.finite = abs_bits < 0x7F800000u;
-  z.scale = z.finite ? a / kMaxCode : __uint_as_float(abs_bits);
+  const float s = a * kInverse;
+  z.scale = z.finite ? __builtin_fmaf(__builtin_fmaf(-s, kMaxCode, a), kInverse, s)
+                     : __uint_as_float(abs_bits);
   const float by = a > 0x1p100f ? 0x1p-64f : (a < 0x1p-60f ? 0x1p64f : 1.0f);
   z.a = a * by;
-  z.r = 1.0f / z.a;
+  const float r = __builtin_amdgcn_rcpf(z.a);
+  z.r = __builtin_fmaf(__builtin_fmaf(-z.a, r, 1.0f), r, r);
   z.pre = kMaxCode * by;
   return z;
 }
@@ -107,6 +114,14 @@ __device__ __forceinline__ uint32_t abs_max8(const float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
   return m;
+}
+
+// The largest of 16 neighbouring lanes' values, in all of them.
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+  v = max(v, dpp<0xB1, 0xF, 0u>(v));
+  v = max(v, dpp<0x4E, 0xF, 0u>(v));
+  v = max(v, dpp<0x141, 0xF, 0u>(v));
+  return max(v, dpp<0x140, 0xF, 0u>(v));
 }
 
 __device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
@@ -144,10 +159,7 @@ __device__ __forceinline__ void quantize_rows(const In* x, long rows, int cols, 
     const bool in = c < cols;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (in) load8(x + r * ld + c, v);
-    uint32_t m = abs_max8(v);
-#pragma unroll
-    for (int s = 1; s < 16; s *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, s));
-    const Quantum z = quantum(m);
+    const Quantum z = quantum(max16(abs_max8(v)));
     if (in)
       *reinterpret_cast<uint2*>(q + r * cols + c) = make_uint2(codes4(z, v), codes4(z, v + 4));
     if (l == 0) scales[i] = z.scale;
@@ -747,7 +759,6 @@ struct LinearForm {
 const LinearForm kLinearForms[] = {
     {16, 16, 0.12f, 0.136f, launch_product<kLinear, 1, 1, 4>},
     {32, 16, 0.19f, 0.195f, launch_product<kLinear, 2, 1, 4>},
-    {64, 16, 0.31f, 0.32f, launch_product<kLinear, 4, 1, 4>},
     {16, 32, 0.21f, 0.22f, launch_product<kLinear, 1, 2, 4>},
     {32, 32, 0.235f, 0.24f, launch_product<kLinear, 2, 2, 4>},
     {64, 32, 0.245f, 0.165f, launch_tile<kLinear, 64, 32, 2, 2, 4>},
@@ -770,7 +781,7 @@ float form_cost(const LinearForm& f, int T, int n) {
 // LDS: a linear product of up to 16 short rows, and the two products of one token's experts, so
 // that these calls are one launch and two.  The waves take the blocks of K in turn as in
 // product_kernel.
-//   kLinear  x rows [T, K] bf16; 16 MR weight rows a workgroup.
+//   kLinear  x rows [T, K] bf16; 16 MR WR weight rows a workgroup.
 //   kGateUp  the one token's x; workgroup (., r) the expert of pair r: h[r] = silu(W1 x) (W3 x).
 //            In bf16 instructions of the decoded codes, whose sums keep what the FP8 one's drop:
 //            of one token's hidden values two or three lie so near the middle of two codes that
@@ -778,7 +789,9 @@ float form_cost(const LinearForm& f, int T, int n) {
 //            rounding's error); the weights' stream hides the conversion.
 //   kDown    all pairs' h rows [k, K]; y = sum_r w_r W2_{id_r} q(h_r), the pairs one after the
 //            other in every wave, no outputs of single pairs in between.
-// Bound by the weights' latency and stream: 1 x 7168 x 2048 in 6.1 us; eight (2048, 768) experts'
+// A workgroup has WR shares of 16 MR weight rows, of KW waves each, whose sums meet in
+// product_kernel's order.
+// Bound by the weights' latency and stream: 1 x 7168 x 2048 in 5.3 us; eight (2048, 768) experts'
 // 25 MB and 13 MB in 8.9 and 7.1 us.  The first weights are under way while the rows are
 // quantised (9.7 -> 8.9 us).
 struct Small {
@@ -804,12 +817,14 @@ __host__ __device__ inline int small_pitch(int K) {
   return (K + kQuantBlock - 1) / kQuantBlock * kQuantBlock * (kKind == kGateUp ? 2 : 1) + 16;
 }
 
-template <Kind kKind, int MR, int KW>
-__global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
+template <Kind kKind, int MR, int KW, int WR>
+__global__ __launch_bounds__(64 * KW * WR, 2) void small_kernel(Small a) {
   constexpr int kRows = kKind == kLinear ? 16 : 1;
   constexpr int MW = kKind == kGateUp ? MR / 2 : MR;
   constexpr int LD = 16 * MR + 4;
-  __shared__ float red[KW][kRows][LD];
+  constexpr int kCols = 16 * MW;           // output columns of a wave
+  static_assert(kQuantBlock % kCols == 0, "they share the weights' scales");
+  __shared__ float red[KW * WR][kRows][LD];
   __shared__ int expert[kSmallPairs];
   __shared__ int pair[kSmallPairs];
   extern __shared__ __attribute__((aligned(16))) uint8_t codes[];
@@ -819,7 +834,7 @@ __global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
   const int N = a.N, K = a.K;
   const int nb = (K + kQuantBlock - 1) / kQuantBlock, nbN = (N + kQuantBlock - 1) / kQuantBlock;
   const int pitch = small_pitch<kKind>(K);
-  const int n0 = blockIdx.x * 16 * MW;
+  const int n0 = blockIdx.x * kCols * WR, nw = n0 + wave / KW * kCols;   // the wave's first
   int e0 = 0, pairs = 1;                   // kGateUp's expert; pairs that the workgroup adds up
   if constexpr (kKind == kGateUp) {
     e0 = __builtin_amdgcn_readfirstlane(a.ids[blockIdx.y]);
@@ -842,7 +857,7 @@ __global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
   // rows past the end repeat the last one; their results are not stored
   size_t wrow[MW];
 #pragma unroll
-  for (int m = 0; m < MW; ++m) wrow[m] = (size_t)min(n0 + 16 * m + n, N - 1) * K;
+  for (int m = 0; m < MW; ++m) wrow[m] = (size_t)min(nw + 16 * m + n, N - 1) * K;
   floatx4 acc[MR];
 #pragma unroll
   for (int m = 0; m < MR; ++m) acc[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -867,7 +882,7 @@ __global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
     const int e = kKind == kDown ? __builtin_amdgcn_readfirstlane(expert[i.q]) : e0;
     const int lo = min(b * kQuantBlock + 16 * g, K - 16);
     const int hi = min(b * kQuantBlock + 64 + 16 * g, K - 16);
-    const size_t s = ((size_t)e * nbN + n0 / kQuantBlock) * nb + b;
+    const size_t s = ((size_t)e * nbN + min(nw / kQuantBlock, nbN - 1)) * nb + b;
     r.f1 = a.s1[s];
     if constexpr (kKind == kGateUp) r.f3 = a.s3[s];
 #pragma unroll
@@ -913,32 +928,39 @@ __global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
     }
   };
   Block u, v;
-  Item i{0, wave};
+  Item i{0, wave % KW};
   while (i.b >= nb && i.q + 1 < pairs) {                // (fewer blocks than waves)
     i.b -= nb;
     ++i.q;
   }
   if (pairs > 0) load(u, i);                            // under way while the rows are quantised
 
-  for (int o = tid >> 4; o < rows * nb; o += 4 * KW) {
-    const int r = o / nb, b = o - r * nb, c = b * kQuantBlock + 8 * (tid & 15);
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (c < K) {
-      if constexpr (kKind == kDown)
-        load8(a.hin + (size_t)pair[r] * K + c, v);
+  {                                                     // 16 lanes a block, as in quantize_rows
+    constexpr int kStep = 4 * KW * WR;
+    const int row_step = kStep / nb, block_step = kStep - row_step * nb;
+    int r = (tid >> 4) / nb, b = (tid >> 4) - r * nb;
+    while (r < rows) {
+      const int c = b * kQuantBlock + 8 * (tid & 15);
+      float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (c < K) {
+        if constexpr (kKind == kDown)
+          load8(a.hin + (size_t)pair[r] * K + c, v);
+        else
+          load8(a.x + (size_t)r * a.ldx + c, v);
+      }
+      const Quantum z = quantum(max16(abs_max8(v)));
+      const uint32_t c0 = codes4(z, v), c1 = codes4(z, v + 4);
+      if constexpr (kKind == kGateUp)
+        *reinterpret_cast<bf16x8*>(codes + r * pitch + 2 * c) = codes_to_bf16(c0, c1);
       else
-        load8(a.x + (size_t)r * a.ldx + c, v);
+        *reinterpret_cast<uint2*>(codes + r * pitch + c) = make_uint2(c0, c1);
+      if ((tid & 15) == 0) scales[r * nb + b] = z.scale * (kKind == kDown ? a.w[pair[r]] : 1.0f);
+      r += row_step;
+      if ((b += block_step) >= nb) {
+        b -= nb;
+        ++r;
+      }
     }
-    uint32_t m = abs_max8(v);
-#pragma unroll
-    for (int s = 1; s < 16; s *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, s));
-    const Quantum z = quantum(m);
-    const uint32_t c0 = codes4(z, v), c1 = codes4(z, v + 4);
-    if constexpr (kKind == kGateUp)
-      *reinterpret_cast<bf16x8*>(codes + r * pitch + 2 * c) = codes_to_bf16(c0, c1);
-    else
-      *reinterpret_cast<uint2*>(codes + r * pitch + c) = make_uint2(c0, c1);
-    if ((tid & 15) == 0) scales[o] = z.scale * (kKind == kDown ? a.w[pair[r]] : 1.0f);
   }
   __syncthreads();
   if (pairs > 0) {
@@ -959,29 +981,30 @@ __global__ __launch_bounds__(64 * KW, 2) void small_kernel(Small a) {
     if (n < kRows) *reinterpret_cast<floatx4*>(&red[wave][n][16 * m + 4 * g]) = acc[m];
   __syncthreads();
   const int live = kKind == kLinear ? a.T : 1;
-  for (int i = tid; i < live * 16 * MW; i += 64 * KW) {
-    const int t = i / (16 * MW), c = i - t * 16 * MW;
+  for (int i = tid; i < live * kCols * WR; i += 64 * KW * WR) {
+    const int t = i / (kCols * WR), c = i - t * kCols * WR;
     if (n0 + c >= N) continue;
-    auto sum = [&](int col) {
-      float s = red[0][t][col];
+    auto sum = [&](int more) {
+      const int w0 = c / kCols * KW, col = c % kCols + more;
+      float s = red[w0][t][col];
 #pragma unroll
-      for (int w = 1; w < KW; ++w) s += red[w][t][col];
+      for (int w = 1; w < KW; ++w) s += red[w0 + w][t][col];
       return s;
     };
-    const float v = sum(c);
+    const float v = sum(0);
     if constexpr (kKind == kGateUp)
-      a.h[(size_t)blockIdx.y * N + n0 + c] = v / (1.0f + expf(-v)) * sum(16 * MW + c);
+      a.h[(size_t)blockIdx.y * N + n0 + c] = v / (1.0f + expf(-v)) * sum(kCols);
     else
       a.y[(size_t)t * a.ldy + n0 + c] = to_bf16(v);
   }
 }
 
-template <Kind kKind, int MR, int KW>
+template <Kind kKind, int MR, int KW, int WR>
 hipError_t launch_small(const Small& a, int rows, int groups, hipStream_t stream) {
-  const int cols = 16 * (kKind == kGateUp ? MR / 2 : MR);
-  small_kernel<kKind, MR, KW><<<dim3((a.N + cols - 1) / cols, groups), 64 * KW,
-                               rows * (small_pitch<kKind>(a.K) + 4 * quant_blocks(a.K)),
-                               stream>>>(a);
+  const int cols = 16 * (kKind == kGateUp ? MR / 2 : MR) * WR;
+  small_kernel<kKind, MR, KW, WR><<<dim3((a.N + cols - 1) / cols, groups), 64 * KW * WR,
+                                   rows * (small_pitch<kKind>(a.K) + 4 * quant_blocks(a.K)),
+                                   stream>>>(a);
   return hipGetLastError();
 }
 
@@ -1116,7 +1139,6 @@ hipError_t launch_block_linear(const BlockLinearArgs& a, hipStream_t stream) {
   p.y = a.y;
   p.ldy = a.ldy;
   if (a.x) {
-    // Up to 16 rows of 32768 values in all are quantised by every workgroup for itself.
     Small s{};
     s.x = a.x;
     s.ldx = a.ldx;
@@ -1127,9 +1149,12 @@ hipError_t launch_block_linear(const BlockLinearArgs& a, hipStream_t stream) {
     s.s1 = a.wscale;
     s.y = a.y;
     s.ldy = a.ldy;
-    if (a.n >= 14336) return launch_small<kLinear, 4, 4>(s, a.T, 1, stream);
-    if (a.n >= 7168) return launch_small<kLinear, 2, 4>(s, a.T, 1, stream);
-    return launch_small<kLinear, 1, 4>(s, a.T, 1, stream);
+    // Twice the waves a workgroup, which share the quantisation, where as many workgroups remain
+    // as there are compute units or nearly: one row of 2048 by 7168 5.5 -> 5.3 us, by 2048 4.1 ->
+    // 4.8; of 7168 by 14336 24.3 -> 22.6, by 1536 8.0 -> 9.7; 4 rows of 4096 by 4096 9.8 -> 8.6.
+    // (Four times: one row of 4096 by 24576 22.4 -> 24.9, 8 of 2048 by 32768 17.6 -> 15.9.)
+    if (a.n >= 4096) return launch_small<kLinear, 1, 4, 2>(s, a.T, 1, stream);
+    return launch_small<kLinear, 1, 4, 1>(s, a.T, 1, stream);
   }
   const LinearForm* best = &kLinearForms[0];
   for (const LinearForm& f : kLinearForms)
@@ -1155,7 +1180,7 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
     s.k = a.k;
     s.E = a.E;
     s.h = a.h;
-    const hipError_t e = launch_small<kGateUp, 2, 8>(s, 1, a.k, stream);
+    const hipError_t e = launch_small<kGateUp, 2, 8, 1>(s, 1, a.k, stream);
     if (e != hipSuccess) return e;
     s.hin = a.h;
     s.N = a.d;
@@ -1163,7 +1188,7 @@ hipError_t launch_block_experts(const BlockExpertsArgs& a, hipStream_t stream) {
     s.w1 = a.w2;
     s.s1 = a.s2;
     s.y = a.y;
-    return launch_small<kDown, 1, 8>(s, a.k, 1, stream);
+    return launch_small<kDown, 1, 8, 1>(s, a.k, 1, stream);
   }
   const long groups = (long(a.T) * quant_blocks(a.d) + 63) / 64;
   prepare_kernel<<<int(a.E + (groups < 4096 ? groups : 4096)), 1024, 0, stream>>>(

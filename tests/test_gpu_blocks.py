@@ -160,6 +160,35 @@ def test_linear(T, n, k):
     assert torch.equal(y.view(torch.int16), again.view(torch.int16))
 
 
+# sizes at which each form of the product is the one that is chosen (weight rows x tokens of a
+# workgroup), from codes, so that none of them quantises its rows itself
+@pytest.mark.parametrize("form,T,n,k", [
+    ("16x16", 16, 1001, 656), ("32x16", 13, 5003, 272), ("16x32", 30, 2049, 400),
+    ("32x32", 31, 5003, 272), ("64x32", 29, 14337, 144), ("32x32", 150, 1003, 912),
+    ("64x64", 600, 1367, 272), ("128x64", 290, 4100, 272), ("128x128", 160, 14339, 144),
+    ("128x256", 270, 14339, 144), ("256x256", 700, 13001, 144), ("128x128", 515, 16385, 128)])
+def test_linear_forms(form, T, n, k):
+    from paper_2602_07265_amd import xshare as X
+    rng = np.random.default_rng(T + n)
+    x, (q, s) = _x(rng, T, k), _weight(rng, n, k)
+    say(f"linear case form {form} T={T} n={n} k={k}")
+    codes, scales = X.block_quantize(x.to(DEV))
+    _check_linear(x, q, s, X.block_linear(codes, q.to(DEV), s.to(DEV), x_scale=scales))
+
+
+# rows that every workgroup quantises for itself: both widths of the workgroups (on both sides of
+# 4096 weight rows), the longest rows and one step past them, the most rows and one more
+@pytest.mark.parametrize("T,n,k", [(1, 14347, 160), (3, 4095, 272), (3, 4096, 272), (16, 300, 1024),
+                                   (1, 77, 16384), (1, 77, 16400), (17, 300, 656), (5, 200, 3264),
+                                   (16, 4129, 1024), (5, 4097, 272), (1, 77, 32784)])
+def test_linear_quantised_by_the_product(T, n, k):
+    from paper_2602_07265_amd import xshare as X
+    rng = np.random.default_rng(T + n + k)
+    x, (q, s) = _x(rng, T, k), _weight(rng, n, k)
+    say(f"linear case own quantisation T={T} n={n} k={k}")
+    _check_linear(x, q, s, X.block_linear(x.to(DEV), q.to(DEV), s.to(DEV)))
+
+
 @pytest.mark.parametrize("T,n,k", [(3, 100, 272), (40, 131, 400), (150, 264, 1040)])
 def test_linear_strided_guarded(T, n, k):
     """Rows apart in x and y, NaN around everything that is read."""
@@ -341,6 +370,42 @@ def test_experts_missing_pairs(T):
     w[5, 1:] = float("nan")
     y = _run_experts(x, ids, w, mats)
     assert torch.isnan(y[3]).all() and torch.isfinite(y[4:]).all()
+
+
+# both products in tiles of 32 and of 128 tokens; gate/up alone in tiles (experts of few down
+# columns), down alone in tiles (experts of few hidden units); down in tiles of 64 tokens
+@pytest.mark.parametrize("forms,T,E,k,d,f", [
+    ("32 / 32", 60, 100, 4, 528, 272), ("32 / few", 9, 160, 8, 272, 144),
+    ("128 / 128", 480, 100, 4, 528, 272), ("128 / 128", 160, 10, 8, 5136, 1296),
+    ("32 / few", 25, 50, 4, 144, 272), ("few / 32", 30, 50, 4, 1040, 112),
+    ("128 / 64", 130, 12, 3, 272, 1040), ("few / 64", 60, 12, 3, 272, 144)])
+def test_experts_forms(forms, T, E, k, d, f):
+    rng = np.random.default_rng(T + E + d)
+    x, mats = _x(rng, T, d), _expert_weights(rng, E, d, f)
+    ids, w = _routing(rng, T, E, k)
+    ids[: T // 3, 0] = 1                       # one expert holds many rows, another none
+    ids[ids == E - 1] = -1
+    ids[: T // 3, 1:] = np.where(ids[: T // 3, 1:] == 1, 2, ids[: T // 3, 1:])
+    say(f"experts case forms {forms} T={T} E={E} k={k} d={d} f={f}")
+    _check_experts(x, ids, w, mats, _run_experts(x, ids, w, mats))
+
+
+def test_experts_on_a_given_stream_and_output():
+    from paper_2602_07265_amd import xshare as X
+    rng = np.random.default_rng(31)
+    T, E, k, d, f = 21, 6, 2, 272, 144
+    x, mats = _x(rng, T, d), _expert_weights(rng, E, d, f)
+    ids, w = _routing(rng, T, E, k)
+    y = torch.empty((T, d), dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(X.block_experts_workspace_bytes(T, k, E, d, f), dtype=torch.uint8,
+                     device=DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got = _run_experts(x, ids, w, mats, y=y, workspace=ws, stream=side)
+    side.synchronize()
+    assert got is y
+    _check_experts(x, ids, w, mats, y)
 
 
 def test_experts_large_batch_of_small_experts():
