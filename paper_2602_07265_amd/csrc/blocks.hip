@@ -356,12 +356,20 @@ __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
   };
   Block u, v;
   int b = wave;
-  load(u, b);
-  while (b < nb) {
+  if (b < nb) load(u, b);
+  while (b < nb) {                                      // (no loads past the last block)
+    if (b + KW >= nb) {
+      add(u, b);
+      break;
+    }
     load(v, b + KW);
     __builtin_amdgcn_sched_barrier(0);                  // loads stay above the instructions
     add(u, b);
-    if ((b += KW) >= nb) break;
+    b += KW;
+    if (b + KW >= nb) {
+      add(v, b);
+      break;
+    }
     load(u, b + KW);
     __builtin_amdgcn_sched_barrier(0);
     add(v, b);
@@ -412,7 +420,8 @@ __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
 // falls to 1.5-2.0 GHz; the loads alone would take 88 us, the instructions and reads of LDS
 // alone 108.  Tried without gain: tiles ordered for the eight L2 caches, prefetching into
 // them, persistent workgroups that load the next tile's operands before they store, 16 waves,
-// reading the next block's operands under this one's instructions.
+// reading the next block's operands under this one's instructions, asking whether a block is left
+// to load (1000 x 4096 x 7168 44 -> 48 us).
 typedef const __attribute__((address_space(1))) void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
@@ -792,8 +801,9 @@ float form_cost(const LinearForm& f, int T, int n) {
 // A workgroup has WR shares of 16 MR weight rows, of KW waves each, whose sums meet in
 // product_kernel's order.
 // Bound by the weights' latency and stream: 1 x 7168 x 2048 in 5.3 us; eight (2048, 768) experts'
-// 25 MB and 13 MB in 8.9 and 7.1 us.  The first weights are under way while the rows are
-// quantised (9.7 -> 8.9 us).
+// 25 MB and 13 MB in 16.3 us together.  The first weights are under way while the rows are
+// quantised (gate/up 9.7 -> 8.9 us; two blocks of them: both products 17.6 -> 19.6), and nothing is
+// loaded past the last block (17.6 -> 16.3).
 struct Small {
   const uint16_t* x;           // kLinear, kGateUp
   long ldx;
@@ -966,11 +976,18 @@ __global__ __launch_bounds__(64 * KW * WR, 2) void small_kernel(Small a) {
   if (pairs > 0) {
     while (i.b < nb) {
       const Item j = next(i);
+      if (j.b >= nb) {                                  // (no loads past the last block)
+        add(u, i);
+        break;
+      }
       load(v, j);
       __builtin_amdgcn_sched_barrier(0);
       add(u, i);
-      if (j.b >= nb) break;
       i = next(j);
+      if (i.b >= nb) {
+        add(v, j);
+        break;
+      }
       load(u, i);
       __builtin_amdgcn_sched_barrier(0);
       add(v, j);
