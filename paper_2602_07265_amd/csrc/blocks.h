@@ -89,7 +89,7 @@ inline int pair_tiles(int pairs, int E, int tile_rows) {
 // of two (4096, 14336) experts has 32, 53 against 21 us; eight of them with 16 rows 128, 105 in
 // the form of 256 x 128 against 85 in that of 128 x 64.  One token's pairs, where their hidden
 // rows are short enough for every workgroup to quantise them, take two launches of their own
-// (one of eight (2048, 768) experts 34.7 -> 16.6 us a call).
+// (one of eight (2048, 768) experts 34.7 -> 15.4 us a call).
 struct BlockExpertsPlan {
   bool one;                    // one token: the launches without tiles
   bool few_up, few_down;       // few workgroups: gate/up in the few-row form; down in that or 128 x 64

