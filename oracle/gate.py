@@ -5,7 +5,7 @@ Experts rank by c_j = s_j + bias_j, or by h_j without a bias; a group's score is
 c_j of its N / G consecutive experts, or the sum of its two largest s_j (+ bias_j); ties go to
 the lower index.  The k best experts of the top_groups best groups are taken, with weights
 w_r = s_{id_r}, divided by their sum if asked, times `scale`.  A logit of -inf masks its expert:
-score 0, ranked last, 0 in a sum of two.
+score 0, ranked last, no part in a sum of two; a group without any other expert ranks last.
 """
 from __future__ import annotations
 
@@ -46,16 +46,22 @@ def gate(h, top_k, score="softmax", bias=None, n_groups=1, top_groups=1, group_s
     if top_groups < n_groups:
         base = c
         if group_score == "top2":
-            base = np.where(masked, 0.0, s if bias is None else c)
+            base = np.where(masked, -np.inf, s if bias is None else c)
         per = -np.sort(-base.reshape(T, n_groups, -1), axis=2)
-        gs = per[:, :, 0] if group_score == "max" else per[:, :, 0] + per[:, :, 1]
+        gs = per[:, :, 0]
+        if group_score == "top2":
+            gs = gs + np.where(np.isneginf(per[:, :, 1]), 0.0, per[:, :, 1])
         order = _best(gs, n_groups)
         at = np.take_along_axis(gs, order[:, top_groups - 1:top_groups + 1], 1)
         margin = np.minimum(margin, gap(at))
         keep = np.zeros((T, n_groups), bool)
         np.put_along_axis(keep, order[:, :top_groups], True, 1)
-        c = np.where(np.repeat(keep, N // n_groups, axis=1), c, -np.inf)
-    order = _best(c, min(top_k + 1, N))
+        # experts outside the groups come after the masked ones inside
+        keep = np.repeat(keep, N // n_groups, axis=1)
+        order = np.lexsort((-c, ~keep), axis=1)[:, :min(top_k + 1, N)]
+        c = np.where(keep, c, -np.inf)
+    else:
+        order = _best(c, min(top_k + 1, N))
     ranked = np.take_along_axis(c, order, 1)
     margin = np.minimum(margin, gap(ranked))
     ids = order[:, :top_k]

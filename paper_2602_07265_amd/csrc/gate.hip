@@ -125,7 +125,7 @@ __device__ __forceinline__ void load_bias(const GateArgs& a, int lane, float (&b
   }
 }
 
-// The two best of a group, from its parts'.
+// The two best of a group, from its parts' (0: no live expert).
 struct Top2 {
   uint32_t b1, b2;
   __device__ __forceinline__ void add(uint32_t v) {
@@ -136,8 +136,10 @@ struct Top2 {
     b2 = max(min(b1, o.b1), max(b2, o.b2));
     b1 = max(b1, o.b1);
   }
+  // The sum of the live ones of two; 0, behind every other group, where there is none.
   __device__ __forceinline__ uint32_t score(bool top2) const {
-    return top2 ? ord((unord(b1) + unord(b2)) + 0.0f) : b1;
+    if (!top2 || b2 == 0u) return b1;
+    return ord((unord(b1) + unord(b2)) + 0.0f);
   }
 };
 
@@ -208,7 +210,8 @@ __global__ __launch_bounds__(64 * kWaves) void gate_kernel(GateArgs a) {
     const float c = a.bias ? s + b[q] : h[q];
     const bool masked = h[q] == -INFINITY;           // ranks last, whatever its bias
     key[q] = ord(masked ? -INFINITY : c);
-    base[q] = a.top2 ? ord(masked ? 0.0f : a.bias ? c : s) : key[q];
+    // (in a sum of two a masked expert has no part: live ones may add up to less than 0)
+    base[q] = !a.top2 ? key[q] : masked ? 0u : ord(a.bias ? c : s);
   }
   if (grouped) limit_groups<Q>(a, lane, copies[wave], base, key);
   int id = 0;   // lane r: the expert of rank r
