@@ -601,7 +601,8 @@ typedef struct {
  * The experts rank by c_j = s_j + bias_j, or by the logits where there is no bias (the same
  * order); the groups by their score; ties go to the lower index.  Of the top_groups best
  * groups the k best experts are taken, and w_r = s_{id_r}, renormalised and scaled as asked.
- * A logit of -inf masks its expert: score 0, ranked behind the others of the chosen groups
+ * A logit of -inf, or up to bf16's lowest value (-0x1.FEp127; fp32's lies below it), masks its
+ * expert: score 0, ranked behind the others of the chosen groups
  * whatever its bias, no part in its group's score; a group of nothing else ranks behind every
  * other.  A row of nothing else gets weights of 0.  Scores that all underflow do, too.
  * Scores, sums and weights are fp32.  One kernel, no workspace.

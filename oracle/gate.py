@@ -4,16 +4,20 @@ A token's scores are s_j = exp(h_j - max h) / sum (softmax) or 1 / (1 + exp(-h_j
 Experts rank by c_j = s_j + bias_j, or by h_j without a bias; a group's score is the largest
 c_j of its N / G consecutive experts, or the sum of its two largest s_j (+ bias_j); ties go to
 the lower index.  The k best experts of the top_groups best groups are taken, with weights
-w_r = s_{id_r}, divided by their sum if asked, times `scale`.  A logit of -inf masks its expert:
-score 0, ranked last, no part in a sum of two; a group without any other expert ranks last.
+w_r = s_{id_r}, divided by their sum if asked, times `scale`.  A logit of -inf, or up to the
+lowest value of bf16, masks its expert: score 0, ranked last, no part in a sum of two; a group
+without any other expert ranks last.
 """
 from __future__ import annotations
 
 import numpy as np
 
+MASK = -float.fromhex("0x1.FEp127")       # the largest logit that masks
+
 
 def scores(h, score):
     h = np.asarray(h, np.float64)
+    h = np.where(h <= MASK, -np.inf, h)
     if score == "sigmoid":
         with np.errstate(over="ignore"):
             return 1.0 / (1.0 + np.exp(-h))
@@ -34,7 +38,7 @@ def gate(h, top_k, score="softmax", bias=None, n_groups=1, top_groups=1, group_s
     h = np.asarray(h, np.float64)
     T, N = h.shape
     s = scores(h, score)
-    masked = np.isneginf(h)
+    masked = h <= MASK
     c = h if bias is None else np.where(masked, -np.inf, s + np.asarray(bias, np.float64))
     margin = np.full(T, np.inf)
 

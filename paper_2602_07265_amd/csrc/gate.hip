@@ -31,6 +31,9 @@ constexpr int kWaves = 4;   // tokens of a workgroup
 // Weights are divided by no less than this: sigmoid scores that all underflow give weights
 // (and a gradient) of zero, not NaN.
 constexpr float kLeastSum = 0x1p-126f;
+// Logits up to this mask their expert: -inf, and the lowest finite values of bf16 (which programs
+// put in fp32 logits too) and of fp32.
+constexpr float kMask = -0x1.FEp127f;
 
 __device__ __forceinline__ float from_bf16(uint32_t b) { return __uint_as_float(b << 16); }
 
@@ -96,7 +99,7 @@ __device__ __forceinline__ void load_row(const GateArgs& a, const void* row, int
 #pragma unroll
   for (int q = 1; q < Q; ++q) m = fmaxf(m, h[q]);
   m = wave_fmax(m);
-  m = m == -INFINITY ? 0.0f : m;         // a row of -inf: every score 0
+  m = m <= kMask ? 0.0f : m;             // a row of masked experts: every score 0
 #pragma unroll
   for (int q = 0; q < Q; ++q) z += expf(h[q] - m);
   z = fmaxf(wave_sum(z), kLeastSum);
@@ -208,8 +211,8 @@ __global__ __launch_bounds__(64 * kWaves) void gate_kernel(GateArgs a) {
     const bool plain = !a.bias && !(grouped && a.top2);
     const float s = plain ? 0.0f : score(a, h[q], m, z);
     const float c = a.bias ? s + b[q] : h[q];
-    const bool masked = h[q] == -INFINITY;           // ranks last, whatever its bias
-    key[q] = ord(masked ? -INFINITY : c);
+    const bool masked = h[q] <= kMask;
+    key[q] = ord(masked ? h[q] : c);                 // below any score plus a finite bias
     // (in a sum of two a masked expert has no part: live ones may add up to less than 0)
     base[q] = !a.top2 ? key[q] : masked ? 0u : ord(a.bias ? c : s);
   }

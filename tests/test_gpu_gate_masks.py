@@ -50,3 +50,37 @@ def test_a_group_of_masked_experts_beats_no_live_one():
         ids, w = _check(h, torch.from_numpy(h).to(DEV), 2, "sigmoid", np.full(4, -1.5, np.float32),
                         2, 1, group_score, np.isneginf(h))
         assert ids.tolist() == [[0, 1]] and w.tolist() == [[0.5, 0.5]]
+
+
+# ------------------------------------------------------------------ masks of the lowest value
+
+FORMS = [dict(score="softmax", renormalize=True), dict(score="softmax", renormalize=False),
+         dict(score="sigmoid", renormalize=True, scale=2.5),
+         dict(score="sigmoid", renormalize=False)]
+
+
+@pytest.mark.parametrize("form", range(4))
+@pytest.mark.parametrize("kind", ["fp32", "bf16", "bf16 in fp32"])
+def test_lowest_value_masks_as_infinity_does(kind, form):
+    """Logits masked with their type's lowest value, whatever the biases: the choice and weights
+    that -inf gives (no bias ranks by the logits, where both come last), and gradients of 0."""
+    from paper_2602_07265_amd import xshare as X
+    dtype = torch.bfloat16 if kind == "bf16" else torch.float32
+    value = torch.finfo(torch.float32 if kind == "fp32" else torch.bfloat16).min
+    rng = np.random.default_rng(5 + form)
+    f = FORMS[form]
+    for N, G, tg, k in ((64, 8, 2, 6), (60, 6, 5, 10), (40, 1, 1, 9)):
+        h = torch.from_numpy(masked_rows(rng, N, max(G, 4))).to(dtype).float()
+        masked = torch.isneginf(h)
+        low = torch.where(masked, torch.full_like(h, value), h).to(dtype)
+        for bias in (None, 2 * torch.randn(N, device=DEV), torch.full((N,), -3.0, device=DEV)):
+            for group_score in ("max", "top2"):
+                say(f"gate case lowest value {kind} N={N} G={G} {group_score} {f}")
+                kw = dict(bias=bias, n_groups=G, top_groups=tg, group_score=group_score, **f)
+                a = X.gate(h.to(DEV, dtype), k, **kw)
+                b = X.gate(low.to(DEV), k, **kw)
+                assert torch.equal(a["ids"], b["ids"]) and torch.equal(a["w"], b["w"])
+                hidden = masked.to(DEV).gather(1, b["ids"].long())
+                assert (b["w"][hidden] == 0).all() and torch.isfinite(b["w"]).all()
+                d = X.gate_backward(low.to(DEV), b["ids"], torch.randn(len(h), k, device=DEV), **f)
+                assert torch.isfinite(d).all() and (d[masked.to(DEV)] == 0).all()

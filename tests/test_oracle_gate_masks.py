@@ -8,7 +8,7 @@ import pytest
 
 from oracle import gate as OG
 
-LOWEST = -math.inf        # the largest logit that masks
+LOWEST = -(2 - 2.0 ** -7) * 2.0 ** 127     # of bf16: the largest logit that masks
 
 
 def brute_force(h, k, score, bias, G, tg, group_score):
@@ -69,3 +69,16 @@ def test_a_group_of_masked_experts_beats_no_live_one():
     for group_score in ("max", "top2"):
         ids, w, _ = OG.gate(h, 2, "sigmoid", np.full(4, -1.5), 2, 1, group_score)
         assert ids.tolist() == [[0, 1]] and w.tolist() == [[0.5, 0.5]]
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("group_score", ["max", "top2"])
+@pytest.mark.parametrize("value", [LOWEST, float(np.finfo(np.float32).min)])
+def test_lowest_value_masks_as_infinity_does(value, group_score, score):
+    for level in (-1.5, 0.3):
+        args = (10, score, level + np.random.default_rng(1).normal(0, 1, 60), 6, 5, group_score)
+        a = OG.gate(masked_rows(np.random.default_rng(2), 60, 6), *args)
+        b = OG.gate(masked_rows(np.random.default_rng(2), 60, 6, value), *args)
+        assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+    # the next value above bf16's lowest is a logit as others are
+    assert OG.gate([[np.nextafter(value, 0)]], 1)[1] == (1.0 if value == LOWEST else 0.0)
