@@ -106,5 +106,5 @@ def gradient(h, ids, dw, score, renormalize, scale):
             if ok[t, r]:
                 ds[t, ids[t, r]] += dp[t, r]
     if score == "sigmoid":
-        return ds * s * (1.0 - s)
+        return ds * s * scores(-h, score)      # 1 - s, with all its bits
     return s * (ds - (ds * s).sum(axis=1, keepdims=True))

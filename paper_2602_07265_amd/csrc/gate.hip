@@ -59,6 +59,13 @@ __device__ __forceinline__ float score(const GateArgs& a, float h, float m, floa
   return a.sigmoid ? 1.0f / (1.0f + expf(-h)) : expf(h - m) / z;
 }
 
+// d score / d logit of a sigmoid, s (1 - s): the subtraction would leave nothing of 1 - s from a
+// logit of 17 on.
+__device__ __forceinline__ float sigmoid_slope(float h) {
+  const float e = expf(-fabsf(h));
+  return e / ((1.0f + e) * (1.0f + e));
+}
+
 // The lane's logits (-inf past N) and, for softmax, the row's maximum and sum.  a.vec: the rows
 // are aligned for loads of Q logits at once, and N is a multiple of Q.
 template <int Q>
@@ -267,9 +274,9 @@ __global__ __launch_bounds__(64 * kWaves) void gate_backward_kernel(GateArgs a) 
   }
   // softmax's common term, sum of ds s, which renormalised weights make zero
   const float dot = a.sigmoid || a.renormalize ? 0.0f : wave_sum(ds * s);
-  float sj[Q];
+  float sj[Q];                             // scores; their slopes where they are sigmoids
 #pragma unroll
-  for (int q = 0; q < Q; ++q) sj[q] = score(a, h[q], m, z);
+  for (int q = 0; q < Q; ++q) sj[q] = a.sigmoid ? sigmoid_slope(h[q]) : score(a, h[q], m, z);
   lanes_meet();
   if (id >= 0) mine[id] = ds;
   lanes_meet();
@@ -278,7 +285,7 @@ __global__ __launch_bounds__(64 * kWaves) void gate_backward_kernel(GateArgs a) 
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
     const float dj = mine[Q * lane + q];
-    d[q] = a.sigmoid ? dj * sj[q] * (1.0f - sj[q]) : sj[q] * (dj - dot);
+    d[q] = a.sigmoid ? dj * sj[q] : sj[q] * (dj - dot);
   }
   if (Q > 1 && a.vec_out) {
     if (Q * lane < a.N)
