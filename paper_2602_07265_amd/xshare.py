@@ -4,10 +4,16 @@ Every computation runs in the HIP kernels behind the C ABI of include/xshare.h; 
 checks tensor devices/dtypes/shapes, carves nothing itself except the workspace tensor it
 allocates when none is passed, and forwards raw device pointers plus the current HIP stream.
 There is no fallback: if the library is not built or no GPU is present, calls raise.
+
+A call with ``stream=`` works on that stream, and what it allocates (workspace, outputs) comes from
+that stream's memory.  It does not wait for the current stream; tensors given to it must live
+until ``stream`` has passed the call (``Tensor.record_stream``), as for torch's own operations.
 """
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 import os
 
 import torch
@@ -24,6 +30,34 @@ SCORE = {"topk": 0, "dense": 1}
 N_STAGE_EVENTS = 5
 NOALLOC_SCRATCH_BYTES = 64 << 20     # XSHARE_NOALLOC_SCRATCH_BYTES
 STAGES = ("route", "gate_up", "down", "combine")
+
+
+def _stream_ordered(call):
+    """``call``, run with its ``stream`` argument as the current stream where it is another one:
+    what the call allocates or copies itself belongs to the stream that works on it, so that no
+    later allocation of the caller's stream gets memory that is still in use there.  What it
+    returns may be used and dropped on the caller's stream (after waiting for ``stream``)."""
+    names = list(inspect.signature(call).parameters)
+    at = names.index("stream")
+
+    @functools.wraps(call)
+    def ordered(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return call(*args, **kw)
+        if not isinstance(stream, torch.cuda.Stream):     # any object that holds a handle
+            stream = torch.cuda.ExternalStream(stream.cuda_stream)
+        own = torch.cuda.current_stream(stream.device)
+        if own.cuda_stream == stream.cuda_stream:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            res = call(*args, **kw)
+        for t in res.values() if isinstance(res, dict) else \
+                res if isinstance(res, tuple) else (res,):
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(own)
+        return res
+    return ordered
 
 
 class RouteParams(ctypes.Structure):
@@ -296,6 +330,7 @@ def _shared(shared, d, f, dev):
     return SharedExperts(int(ns), w1.data_ptr(), w3.data_ptr(), w2.data_ptr())
 
 
+@_stream_ordered
 def router_logits(x: torch.Tensor, w_gate: torch.Tensor, *, out=None, workspace=None,
                   stream=None) -> torch.Tensor:
     """h = W_g x on the GPU (fp32 [T, N])."""
@@ -417,6 +452,7 @@ def _route_impl(logits, p, req_offsets, out, workspace, stream):
     return dict(sel_mask=sel, ids=ids, w=w, stats=stats)
 
 
+@_stream_ordered
 def select_ep(logits: torch.Tensor, groups: GroupMap, top_k: int, warmup_k0: int,
               per_group_budget: int, score_mode="topk", *, ledger=None, out=None,
               workspace=None, stream=None) -> dict:
@@ -446,6 +482,7 @@ def select_ep(logits: torch.Tensor, groups: GroupMap, top_k: int, warmup_k0: int
     return dict(sel_mask=sel, ids=ids, w=w, stats=stats, group_load=load)
 
 
+@_stream_ordered
 def route(logits: torch.Tensor, top_k: int, warmup_k0: int, budget: int, budget_mode="total",
           score_mode="topk", *, tau: float = 0.0, ledger=None, out=None, workspace=None,
           stream=None) -> dict:
@@ -455,6 +492,7 @@ def route(logits: torch.Tensor, top_k: int, warmup_k0: int, budget: int, budget_
     return _route_impl(logits, p, None, out, workspace, stream)
 
 
+@_stream_ordered
 def select_hier(logits: torch.Tensor, req_offsets, top_k: int, warmup_k0: int,
                 per_request_budget: int, budget: int, budget_mode="total", score_mode="topk", *,
                 tau: float = 0.0, ledger=None, out=None, workspace=None, stream=None) -> dict:
@@ -464,6 +502,7 @@ def select_hier(logits: torch.Tensor, req_offsets, top_k: int, warmup_k0: int,
     return _route_impl(logits, p, req_offsets, out, workspace, stream)
 
 
+@_stream_ordered
 def moe_forward(x: torch.Tensor, logits: torch.Tensor, w1: torch.Tensor, w3: torch.Tensor,
                 w2: torch.Tensor, top_k: int, warmup_k0: int, budget: int, budget_mode="total",
                 score_mode="topk", *, req_offsets=None, per_request_budget: int = 0,
@@ -522,6 +561,7 @@ def moe_forward(x: torch.Tensor, logits: torch.Tensor, w1: torch.Tensor, w3: tor
     return res
 
 
+@_stream_ordered
 def moe_forward_noalloc(x: torch.Tensor, logits: torch.Tensor, w1: torch.Tensor,
                         w3: torch.Tensor, w2: torch.Tensor, top_k: int, warmup_k0: int,
                         budget: int, budget_mode="total", score_mode="topk", *, y=None,
@@ -563,6 +603,7 @@ def moe_forward_noalloc(x: torch.Tensor, logits: torch.Tensor, w1: torch.Tensor,
     return res
 
 
+@_stream_ordered
 def moe_forward_fp8(x: torch.Tensor, logits: torch.Tensor, q1: torch.Tensor, q3: torch.Tensor,
                     q2: torch.Tensor, s1: torch.Tensor, s3: torch.Tensor, s2: torch.Tensor,
                     top_k: int, warmup_k0: int, budget: int, budget_mode="total",
@@ -625,6 +666,7 @@ def mx_granules(k: int) -> int:
     return (k + 255) // 256
 
 
+@_stream_ordered
 def tile_mx_scales(scales: torch.Tensor, stream=None) -> torch.Tensor:
     """xshare_mx_scales_tile: E8M0 scales [n, rows, k/32] (row-major) -> the tiled layout
     the MXFP4 GEMMs read, [n, rows/16, ceil(k/256), 16, 8] uint8 (a new tensor)."""
@@ -647,6 +689,7 @@ def mx_tiled(weights):
     return q1, q3, q2, tile_mx_scales(e1), tile_mx_scales(e3), tile_mx_scales(e2)
 
 
+@_stream_ordered
 def moe_forward_mxfp4(x: torch.Tensor, logits: torch.Tensor, q1: torch.Tensor, q3: torch.Tensor,
                       q2: torch.Tensor, e1: torch.Tensor, e3: torch.Tensor, e2: torch.Tensor,
                       top_k: int, warmup_k0: int, budget: int, budget_mode="total",
@@ -705,6 +748,7 @@ def moe_forward_mxfp4(x: torch.Tensor, logits: torch.Tensor, q1: torch.Tensor, q
     return res
 
 
+@_stream_ordered
 def moe_layer(x: torch.Tensor, w_gate: torch.Tensor, w1: torch.Tensor, w3: torch.Tensor,
               w2: torch.Tensor, top_k: int, warmup_k0: int, budget: int, budget_mode="total",
               score_mode="topk", *, shared=None, req_offsets=None, per_request_budget: int = 0,
@@ -813,6 +857,7 @@ class HipEvent:
             pass
 
 
+@_stream_ordered
 def moe_forward_v2(x: torch.Tensor, top_k: int, warmup_k0: int, budget: int,
                    budget_mode="total", score_mode="topk", *, logits=None, w_gate=None,
                    weights=(), scales=(None, None, None), weight_format="bf16",
@@ -944,6 +989,7 @@ def _logits(logits):
     return int(logits.dtype == torch.bfloat16), _rows(logits, logits.dtype, "logits")
 
 
+@_stream_ordered
 def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_groups: int = 1,
          top_groups: int = 1, group_score="max", renormalize: bool = True, scale: float = 1.0,
          out=None, stream=None) -> dict:
@@ -972,6 +1018,7 @@ def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_grou
     return dict(ids=ids, w=w)
 
 
+@_stream_ordered
 def gate_backward(logits: torch.Tensor, ids: torch.Tensor, dw: torch.Tensor, *, score="softmax",
                   renormalize: bool = True, scale: float = 1.0, out=None,
                   stream=None) -> torch.Tensor:
@@ -997,6 +1044,7 @@ def _blocks(n):
     return (n + 127) // 128
 
 
+@_stream_ordered
 def block_quantize(x: torch.Tensor, block_rows: int = 1, *, out=None, stream=None) -> tuple:
     """(codes uint8 [rows, cols], scales fp32) of a bf16 matrix: E4M3FN with one scale for each
     block of block_rows x 128 (1: activations, 128: weights).  ``out``: the two to write."""
@@ -1023,6 +1071,7 @@ def block_linear_workspace_bytes(T: int, n: int, k: int) -> int:
     return int(lib().xshare_block_linear_workspace_bytes(int(T), int(n), int(k)))
 
 
+@_stream_ordered
 def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale=None, y=None,
                  workspace=None, stream=None) -> torch.Tensor:
     """y = x W^T (bf16 [T, n]) with W as codes wq uint8 [n, k] and scales ws of its 128 x 128
@@ -1070,6 +1119,7 @@ def block_experts_workspace_bytes(T: int, top_k: int, n_experts: int, d: int, f:
                                                           int(d), int(f)))
 
 
+@_stream_ordered
 def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch.Tensor,
                   q3: torch.Tensor, q2: torch.Tensor, s1: torch.Tensor, s3: torch.Tensor,
                   s2: torch.Tensor, *, y=None, workspace=None, stream=None) -> torch.Tensor:
@@ -1110,6 +1160,7 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
     return y
 
 
+@_stream_ordered
 def probe_stream_read(buf: torch.Tensor, blocks: int = 2048, mode: int = 0, sink=None,
                       stream=None):
     """Enqueues one streaming read of ``buf`` (a contiguous GPU tensor, 16-byte aligned,
@@ -1135,6 +1186,7 @@ def use_timeline_library() -> None:
     LIB_PATH = TIMELINE_LIB_PATH
 
 
+@_stream_ordered
 def block_times(clear: bool = True, stream=None) -> dict:
     """The block timeline of the last expert-GEMM launches (xshare_block_times; the profiling
     build only): uint64 arrays of 100 MHz clock stamps, "gate_up" and "down" [blocks, 2]
