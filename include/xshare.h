@@ -19,7 +19,8 @@
  *   pointer after returning; scratch memory comes from the caller's workspace `ws`
  *   (size from the matching *_workspace_bytes function, 256-byte aligned).
  * - Calls are asynchronous and stream-ordered on `stream` (a hipStream_t; NULL = the
- *   default stream).  Outputs are valid once the stream has reached the end of the call.
+ *   default stream) of the current device, where all buffers must lie too.  Outputs are valid
+ *   once the stream has reached the end of the call.
  *   Nothing is copied back to the host and the stream is never synchronised.  A call only
  *   launches kernels (no memset, copy or allocation), so it can be captured in a HIP graph
  *   and replayed with the same pointers; calls that share a workspace must be ordered.

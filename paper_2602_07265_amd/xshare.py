@@ -32,32 +32,50 @@ NOALLOC_SCRATCH_BYTES = 64 << 20     # XSHARE_NOALLOC_SCRATCH_BYTES
 STAGES = ("route", "gate_up", "down", "combine")
 
 
-def _stream_ordered(call):
-    """``call``, run with its ``stream`` argument as the current stream where it is another one:
-    what the call allocates or copies itself belongs to the stream that works on it, so that no
-    later allocation of the caller's stream gets memory that is still in use there.  What it
-    returns may be used and dropped on the caller's stream (after waiting for ``stream``)."""
+def _placed(call):
+    """``call``, run where it belongs.
+
+    The device of its first argument is made current for it: a kernel goes to the current device,
+    whatever its arguments' device is.  ``stream``, where it is another one than that device's current
+    stream, is made current too: what the call allocates or copies itself belongs to the stream
+    that works on it, so that no later allocation of the caller's stream gets memory that is
+    still in use there.  What it returns may be used and dropped on the caller's stream (after
+    waiting for ``stream``)."""
     names = list(inspect.signature(call).parameters)
-    at = names.index("stream")
+    first, at = names[0], names.index("stream")
+
+    def on_device(i, *args, **kw):
+        if i < 0 or i == torch._C._cuda_getDevice():
+            return call(*args, **kw)
+        with torch.cuda.device(i):
+            return call(*args, **kw)
 
     @functools.wraps(call)
-    def ordered(*args, **kw):
+    def placed(*args, **kw):
         stream = args[at] if len(args) > at else kw.get("stream")
+        try:
+            i = (args[0] if args else kw[first]).get_device()
+        except (AttributeError, KeyError):
+            i = -1                                        # not a GPU tensor: not for here to say
         if stream is None:
-            return call(*args, **kw)
+            if i < 0 or i == torch._C._cuda_getDevice():  # (nearly always, and at once)
+                return call(*args, **kw)
+            return on_device(i, *args, **kw)
         if not isinstance(stream, torch.cuda.Stream):     # any object that holds a handle
-            stream = torch.cuda.ExternalStream(stream.cuda_stream)
+            stream = torch.cuda.ExternalStream(stream.cuda_stream, None if i < 0 else i)
+        if 0 <= i != stream.device.index:
+            raise ValueError(f"{first} is on cuda:{i}, the stream on {stream.device}")
         own = torch.cuda.current_stream(stream.device)
         if own.cuda_stream == stream.cuda_stream:
-            return call(*args, **kw)
-        with torch.cuda.stream(stream):
+            return on_device(i, *args, **kw)
+        with torch.cuda.stream(stream):                   # (its device too)
             res = call(*args, **kw)
         for t in res.values() if isinstance(res, dict) else \
                 res if isinstance(res, tuple) else (res,):
             if isinstance(t, torch.Tensor) and t.is_cuda:
                 t.record_stream(own)
         return res
-    return ordered
+    return placed
 
 
 class RouteParams(ctypes.Structure):
@@ -330,7 +348,7 @@ def _shared(shared, d, f, dev):
     return SharedExperts(int(ns), w1.data_ptr(), w3.data_ptr(), w2.data_ptr())
 
 
-@_stream_ordered
+@_placed
 def router_logits(x: torch.Tensor, w_gate: torch.Tensor, *, out=None, workspace=None,
                   stream=None) -> torch.Tensor:
     """h = W_g x on the GPU (fp32 [T, N])."""
@@ -452,7 +470,7 @@ def _route_impl(logits, p, req_offsets, out, workspace, stream):
     return dict(sel_mask=sel, ids=ids, w=w, stats=stats)
 
 
-@_stream_ordered
+@_placed
 def select_ep(logits: torch.Tensor, groups: GroupMap, top_k: int, warmup_k0: int,
               per_group_budget: int, score_mode="topk", *, ledger=None, out=None,
               workspace=None, stream=None) -> dict:
@@ -482,7 +500,7 @@ def select_ep(logits: torch.Tensor, groups: GroupMap, top_k: int, warmup_k0: int
     return dict(sel_mask=sel, ids=ids, w=w, stats=stats, group_load=load)
 
 
-@_stream_ordered
+@_placed
 def route(logits: torch.Tensor, top_k: int, warmup_k0: int, budget: int, budget_mode="total",
           score_mode="topk", *, tau: float = 0.0, ledger=None, out=None, workspace=None,
           stream=None) -> dict:
@@ -492,7 +510,7 @@ def route(logits: torch.Tensor, top_k: int, warmup_k0: int, budget: int, budget_
     return _route_impl(logits, p, None, out, workspace, stream)
 
 
-@_stream_ordered
+@_placed
 def select_hier(logits: torch.Tensor, req_offsets, top_k: int, warmup_k0: int,
                 per_request_budget: int, budget: int, budget_mode="total", score_mode="topk", *,
                 tau: float = 0.0, ledger=None, out=None, workspace=None, stream=None) -> dict:
@@ -502,7 +520,7 @@ def select_hier(logits: torch.Tensor, req_offsets, top_k: int, warmup_k0: int,
     return _route_impl(logits, p, req_offsets, out, workspace, stream)
 
 
-@_stream_ordered
+@_placed
 def moe_forward(x: torch.Tensor, logits: torch.Tensor, w1: torch.Tensor, w3: torch.Tensor,
                 w2: torch.Tensor, top_k: int, warmup_k0: int, budget: int, budget_mode="total",
                 score_mode="topk", *, req_offsets=None, per_request_budget: int = 0,
@@ -561,7 +579,7 @@ def moe_forward(x: torch.Tensor, logits: torch.Tensor, w1: torch.Tensor, w3: tor
     return res
 
 
-@_stream_ordered
+@_placed
 def moe_forward_noalloc(x: torch.Tensor, logits: torch.Tensor, w1: torch.Tensor,
                         w3: torch.Tensor, w2: torch.Tensor, top_k: int, warmup_k0: int,
                         budget: int, budget_mode="total", score_mode="topk", *, y=None,
@@ -603,7 +621,7 @@ def moe_forward_noalloc(x: torch.Tensor, logits: torch.Tensor, w1: torch.Tensor,
     return res
 
 
-@_stream_ordered
+@_placed
 def moe_forward_fp8(x: torch.Tensor, logits: torch.Tensor, q1: torch.Tensor, q3: torch.Tensor,
                     q2: torch.Tensor, s1: torch.Tensor, s3: torch.Tensor, s2: torch.Tensor,
                     top_k: int, warmup_k0: int, budget: int, budget_mode="total",
@@ -666,7 +684,7 @@ def mx_granules(k: int) -> int:
     return (k + 255) // 256
 
 
-@_stream_ordered
+@_placed
 def tile_mx_scales(scales: torch.Tensor, stream=None) -> torch.Tensor:
     """xshare_mx_scales_tile: E8M0 scales [n, rows, k/32] (row-major) -> the tiled layout
     the MXFP4 GEMMs read, [n, rows/16, ceil(k/256), 16, 8] uint8 (a new tensor)."""
@@ -689,7 +707,7 @@ def mx_tiled(weights):
     return q1, q3, q2, tile_mx_scales(e1), tile_mx_scales(e3), tile_mx_scales(e2)
 
 
-@_stream_ordered
+@_placed
 def moe_forward_mxfp4(x: torch.Tensor, logits: torch.Tensor, q1: torch.Tensor, q3: torch.Tensor,
                       q2: torch.Tensor, e1: torch.Tensor, e3: torch.Tensor, e2: torch.Tensor,
                       top_k: int, warmup_k0: int, budget: int, budget_mode="total",
@@ -748,7 +766,7 @@ def moe_forward_mxfp4(x: torch.Tensor, logits: torch.Tensor, q1: torch.Tensor, q
     return res
 
 
-@_stream_ordered
+@_placed
 def moe_layer(x: torch.Tensor, w_gate: torch.Tensor, w1: torch.Tensor, w3: torch.Tensor,
               w2: torch.Tensor, top_k: int, warmup_k0: int, budget: int, budget_mode="total",
               score_mode="topk", *, shared=None, req_offsets=None, per_request_budget: int = 0,
@@ -857,7 +875,7 @@ class HipEvent:
             pass
 
 
-@_stream_ordered
+@_placed
 def moe_forward_v2(x: torch.Tensor, top_k: int, warmup_k0: int, budget: int,
                    budget_mode="total", score_mode="topk", *, logits=None, w_gate=None,
                    weights=(), scales=(None, None, None), weight_format="bf16",
@@ -940,13 +958,16 @@ def _rows(t, dtype, name, cols=None):
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or (cols is not None and t.shape[1] != cols):
+    shape = t.shape
+    if len(shape) != 2 or (cols is not None and shape[1] != cols):
         raise ValueError(f"{name} must be a matrix" + ("" if cols is None else f" of {cols} columns")
-                         + f", got {tuple(t.shape)}")
-    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if t.shape[1] > 1 and t.stride(1) != 1:
+                         + f", got {tuple(shape)}")
+    if t.is_contiguous():
+        return shape[1]
+    ld, step = t.stride()
+    if shape[1] > 1 and step != 1:
         raise ValueError(f"{name}: the elements of a row must be neighbours")
-    return ld
+    return ld if shape[0] > 1 else shape[1]
 
 
 def _fit(device, *wanted):
@@ -969,10 +990,10 @@ def _stream_of(x, stream):
     (3 us less a call, of about 10 that the shortest of these calls take)."""
     if stream is not None:
         return stream.cuda_stream
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is None:
+    try:
+        return torch._C._cuda_getCurrentRawStream(x.get_device())
+    except AttributeError:
         return torch.cuda.current_stream(x.device).cuda_stream
-    return raw(x.device.index)
 
 
 def _gate_params(N, top_k, score, n_groups, top_groups, group_score, renormalize, scale):
@@ -989,7 +1010,7 @@ def _logits(logits):
     return int(logits.dtype == torch.bfloat16), _rows(logits, logits.dtype, "logits")
 
 
-@_stream_ordered
+@_placed
 def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_groups: int = 1,
          top_groups: int = 1, group_score="max", renormalize: bool = True, scale: float = 1.0,
          out=None, stream=None) -> dict:
@@ -1018,7 +1039,7 @@ def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_grou
     return dict(ids=ids, w=w)
 
 
-@_stream_ordered
+@_placed
 def gate_backward(logits: torch.Tensor, ids: torch.Tensor, dw: torch.Tensor, *, score="softmax",
                   renormalize: bool = True, scale: float = 1.0, out=None,
                   stream=None) -> torch.Tensor:
@@ -1044,7 +1065,7 @@ def _blocks(n):
     return (n + 127) // 128
 
 
-@_stream_ordered
+@_placed
 def block_quantize(x: torch.Tensor, block_rows: int = 1, *, out=None, stream=None) -> tuple:
     """(codes uint8 [rows, cols], scales fp32) of a bf16 matrix: E4M3FN with one scale for each
     block of block_rows x 128 (1: activations, 128: weights).  ``out``: the two to write."""
@@ -1071,7 +1092,7 @@ def block_linear_workspace_bytes(T: int, n: int, k: int) -> int:
     return int(lib().xshare_block_linear_workspace_bytes(int(T), int(n), int(k)))
 
 
-@_stream_ordered
+@_placed
 def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale=None, y=None,
                  workspace=None, stream=None) -> torch.Tensor:
     """y = x W^T (bf16 [T, n]) with W as codes wq uint8 [n, k] and scales ws of its 128 x 128
@@ -1119,7 +1140,7 @@ def block_experts_workspace_bytes(T: int, top_k: int, n_experts: int, d: int, f:
                                                           int(d), int(f)))
 
 
-@_stream_ordered
+@_placed
 def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch.Tensor,
                   q3: torch.Tensor, q2: torch.Tensor, s1: torch.Tensor, s3: torch.Tensor,
                   s2: torch.Tensor, *, y=None, workspace=None, stream=None) -> torch.Tensor:
@@ -1160,7 +1181,7 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
     return y
 
 
-@_stream_ordered
+@_placed
 def probe_stream_read(buf: torch.Tensor, blocks: int = 2048, mode: int = 0, sink=None,
                       stream=None):
     """Enqueues one streaming read of ``buf`` (a contiguous GPU tensor, 16-byte aligned,
@@ -1186,7 +1207,7 @@ def use_timeline_library() -> None:
     LIB_PATH = TIMELINE_LIB_PATH
 
 
-@_stream_ordered
+@_placed
 def block_times(clear: bool = True, stream=None) -> dict:
     """The block timeline of the last expert-GEMM launches (xshare_block_times; the profiling
     build only): uint64 arrays of 100 MHz clock stamps, "gate_up" and "down" [blocks, 2]
