@@ -643,7 +643,8 @@ xshare_status xshare_block_quantize(const uint16_t* x, int32_t rows, int32_t col
                                     int32_t block_rows, uint8_t* q, float* scales,
                                     hipStream_t stream);
 
-/* Workspace of xshare_block_linear (bytes, 256-aligned); 0 for invalid sizes.             */
+/* Workspace of xshare_block_linear (bytes, 256-aligned); 0 for invalid sizes.  That of T tokens
+ * serves any smaller T too.                                                                */
 size_t xshare_block_linear_workspace_bytes(int32_t T, int32_t n, int32_t k);
 
 /*
@@ -705,7 +706,8 @@ typedef struct {
   hipStream_t stream;
 } xshare_block_experts_args;
 
-/* Workspace of xshare_block_experts (bytes, 256-aligned); 0 for invalid sizes.            */
+/* Workspace of xshare_block_experts (bytes, 256-aligned); 0 for invalid sizes.  That of T tokens
+ * serves any smaller T too.                                                                */
 size_t xshare_block_experts_workspace_bytes(int32_t T, int32_t top_k, int32_t n_experts,
                                             int32_t d, int32_t f);
 

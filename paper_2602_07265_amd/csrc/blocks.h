@@ -90,23 +90,29 @@ inline int pair_tiles(int pairs, int E, int tile_rows) {
 // the form of 256 x 128 against 85 in that of 128 x 64.  One token's pairs, where their hidden
 // rows are short enough for every workgroup to quantise them, take two launches of their own
 // (one of eight (2048, 768) experts 34.7 -> 15.4 us a call).
+constexpr int kFewMean = 16;    // gate/up in the few-row form: rows of an expert at most
+constexpr int kFewGroups = 96;  // and fewer workgroups than this in the tiled one
+constexpr int kLeastTile = 16;  // the least rows of a tile of any plan
 struct BlockExpertsPlan {
   bool one;                    // one token: the launches without tiles
   bool few_up, few_down;       // few workgroups: gate/up in the few-row form; down in that or 128 x 64
   int wide;                    // tokens of the tiled form's tiles
   int up_rows, down_rows;      // rows of a tile of either product
 };
+inline bool one_token_form(int k, int d, int f) {   // (their rows in LDS: 38 KB at most)
+  return long(k) * f <= 32768 && d <= 16384;
+}
 inline BlockExpertsPlan block_experts_plan(int T, int k, int E, int d, int f) {
   BlockExpertsPlan p{};
   const int pairs = T > 0 ? T * k : k;
   const int expect = pairs < E ? pairs : E, mean = pairs / expect;
-  p.one = T == 1 && long(k) * f <= 32768 && d <= 16384;   // (their rows in LDS: 38 KB at most)
+  p.one = T == 1 && one_token_form(k, d, f);
   p.wide = mean >= 12 ? 128 : 32;
   const long spans = (mean + p.wide - 1) / p.wide;
-  p.few_up = mean <= 16 && long(expect) * ((f + 127) / 128) < 96;
+  p.few_up = mean <= kFewMean && long(expect) * quant_blocks(f) < kFewGroups;
   p.few_down = long(expect) * spans * ((d + 255) / 256) < 192;
-  p.up_rows = p.few_up ? 16 : p.wide;
-  p.down_rows = !p.few_down ? p.wide : mean <= 8 ? 16 : 64;
+  p.up_rows = p.few_up ? kLeastTile : p.wide;
+  p.down_rows = !p.few_down ? p.wide : mean <= 8 ? kLeastTile : 64;
   return p;
 }
 
@@ -116,12 +122,23 @@ struct BlockExpertsLayout {
   size_t perm;                 // int32 [T * k] pair (t * k + r) of each row in expert order
   size_t up_tiles;             // int4 [pair_tiles] {expert, first row, rows, 0} of gate/up
   size_t down_tiles;           // and of down
-  size_t h;                    // fp32 [T * k, f] hidden rows in expert order, where a plan
-                               //      quantises them after gate/up
+  size_t h;                    // fp32 [hidden_tokens * k, f] hidden rows in expert order, where a
+                               //      plan quantises them after gate/up
   size_t hq, hs;               // their codes [T * k, f] and scales [T * k, ceil(f / 128)]
   size_t o;                    // fp32 [T * k, d] the pairs' outputs, by pair
   size_t total;
 };
+// The most tokens, of up to T, whose plan quantises the hidden rows after gate/up (as those of all
+// smaller numbers do, but for one token's own form).
+inline int hidden_tokens(int T, int k, int E, int d, int f) {
+  const int blocks = quant_blocks(f);
+  const int pairs = long(E) * blocks < kFewGroups ? (kFewMean + 1) * E - 1   // by the mean
+                                                  : (kFewGroups - 1) / blocks;  // by the grid
+  const int one = one_token_form(k, d, f) ? 1 : 0, n = pairs / k > one ? pairs / k : one;
+  return n < T ? n : T;
+}
+// A workspace for T tokens serves any smaller number too: no region shrinks as T grows, whatever the
+// plans (the tiles are counted in the least rows a plan gives them).
 inline BlockExpertsLayout block_experts_layout(int T, int k, int E, int d, int f) {
   BlockExpertsLayout L{};
   const size_t rows = size_t(T) * k;
@@ -130,10 +147,10 @@ inline BlockExpertsLayout block_experts_layout(int T, int k, int E, int d, int f
   L.xs = o;     o += align256(sizeof(float) * size_t(T) * quant_blocks(d));
   L.counts = o; o += 256;
   L.perm = o;   o += align256(sizeof(int32_t) * rows);
-  const BlockExpertsPlan p = block_experts_plan(T, k, E, d, f);
-  L.up_tiles = o;   o += align256(16 * size_t(pair_tiles(int(rows), E, p.up_rows)));
-  L.down_tiles = o; o += align256(16 * size_t(pair_tiles(int(rows), E, p.down_rows)));
-  L.h = o;      o += p.one || p.few_up ? align256(sizeof(float) * rows * f) : 0;
+  const size_t tiles = align256(16 * size_t(pair_tiles(int(rows), E, kLeastTile)));
+  L.up_tiles = o;   o += tiles;
+  L.down_tiles = o; o += tiles;
+  L.h = o;      o += align256(sizeof(float) * size_t(hidden_tokens(T, k, E, d, f)) * k * f);
   L.hq = o;     o += align256(rows * f);
   L.hs = o;     o += align256(sizeof(float) * rows * quant_blocks(f));
   L.o = o;      o += align256(sizeof(float) * rows * d);
