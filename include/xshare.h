@@ -656,6 +656,7 @@ size_t xshare_block_linear_workspace_bytes(int32_t T, int32_t n, int32_t k);
  *   wq       [n, k] E4M3FN codes, 16-byte aligned, k a multiple of 16, n any.
  *   wscale   [ceil(n / 128), ceil(k / 128)] fp32.
  *   y        out [T, n] bf16, rows ldy >= n elements apart.
+ *   ws       with x: of xshare_block_linear_workspace_bytes, 16-byte aligned.
  *
  * y_tn = sum over blocks b of k of xs_tb wscale_{n/128,b} sum_{i in b} xq_ti wq_ni, summed in
  * fp32 and rounded once.  Inside a block the FP8 matrix instruction aligns the products of
@@ -684,7 +685,7 @@ xshare_status xshare_block_linear(const uint16_t* x, int64_t ldx, const uint8_t*
  *   d, f        multiples of 16.    n_experts <= 1024, top_k <= 32.
  *   y           out [T, d] bf16, rows ldy >= d elements apart, ldy a multiple of 8, 16-byte
  *               aligned; a token without pairs gets zeros.
- *   ws          of xshare_block_experts_workspace_bytes.
+ *   ws          of xshare_block_experts_workspace_bytes, 16-byte aligned.
  */
 typedef struct {
   size_t struct_size;

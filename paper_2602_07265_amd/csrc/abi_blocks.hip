@@ -144,6 +144,7 @@ xshare_status xshare_block_linear(const uint16_t* x, int64_t ldx, const uint8_t*
   if (x) {
     const xs::BlockLinearLayout L = xs::block_linear_layout(T, k);
     if (!ws || ws_bytes < L.total) return XSHARE_EWORKSPACE;
+    if (!aligned16(ws)) return XSHARE_EINVAL;
     if (xs::block_linear_small(T, k)) {
       a.x = x;
       a.ldx = ldx;
@@ -179,6 +180,7 @@ xshare_status xshare_block_experts(const xshare_block_experts_args* p) {
   const xs::BlockExpertsLayout L =
       xs::block_experts_layout(p->T, p->top_k, p->n_experts, p->d, p->f);
   if (!p->ws || p->ws_bytes < L.total) return XSHARE_EWORKSPACE;
+  if (!aligned16(p->ws)) return XSHARE_EINVAL;
   xs::BlockExpertsArgs a{};
   a.T = p->T;
   a.k = p->top_k;

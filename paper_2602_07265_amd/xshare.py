@@ -985,6 +985,14 @@ def _on(device, t, name):
         raise ValueError(f"{name} is on {t.device}, not {device}")
 
 
+def _workspace(device, t):
+    """The bytes of a given workspace, which have to be as many as its elements say."""
+    _on(device, t, "workspace")
+    if not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return t.numel() * t.element_size()
+
+
 def _stream_of(x, stream):
     """The handle of x's device's current stream, without a Stream object where torch gives it
     (3 us less a call, of about 10 that the shortest of these calls take)."""
@@ -1119,17 +1127,17 @@ def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale
         _on(dev, y, "y")
         if y.shape[0] != T:
             raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
+    size = 0
     if workspace is not None:
-        _on(dev, workspace, "workspace")
+        size = _workspace(dev, workspace)
     elif own:
-        workspace = x.new_empty(L.xshare_block_linear_workspace_bytes(T, n, k),
-                                dtype=torch.uint8)
+        size = L.xshare_block_linear_workspace_bytes(T, n, k)
+        workspace = x.new_empty(size, dtype=torch.uint8)
     px = x.data_ptr()
     st = L.xshare_block_linear(px if own else None, ldx, None if own else px,
                                    None if own else x_scale.data_ptr(), T, n, k, wq.data_ptr(),
                                    ws.data_ptr(), y.data_ptr(), ldy,
-                                   None if workspace is None else workspace.data_ptr(),
-                                   0 if workspace is None else workspace.numel(),
+                                   None if workspace is None else workspace.data_ptr(), size,
                                    _stream_of(x, stream))
     _check(st, "xshare_block_linear")
     return y
@@ -1168,14 +1176,14 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
         if y.shape[0] != T:
             raise ValueError(f"y must have {T} rows, got {y.shape[0]}")
     if workspace is None:
-        workspace = x.new_empty(L.xshare_block_experts_workspace_bytes(T, k, N, d, f),
-                                dtype=torch.uint8)
+        size = L.xshare_block_experts_workspace_bytes(T, k, N, d, f)
+        workspace = x.new_empty(size, dtype=torch.uint8)
     else:
-        _on(dev, workspace, "workspace")
+        size = _workspace(dev, workspace)
     a = BlockExpertsArgs(_EXPERTS_ARGS_BYTES, T, k, N, d, f, x.data_ptr(), ldx,
                          ids.data_ptr(), w.data_ptr(), q1.data_ptr(), q3.data_ptr(),
                          q2.data_ptr(), s1.data_ptr(), s3.data_ptr(), s2.data_ptr(),
-                         y.data_ptr(), ldy, workspace.data_ptr(), workspace.numel(),
+                         y.data_ptr(), ldy, workspace.data_ptr(), size,
                          _stream_of(x, stream))
     _check(L.xshare_block_experts(ctypes.byref(a)), "xshare_block_experts")
     return y
