@@ -980,6 +980,17 @@ def _fit(device, *wanted):
             raise ValueError(f"{name} is on {t.device}, not {device}")
 
 
+def _past_32_bits(sizes):
+    """Whether one of the sizes, or-ed together, is more than the library's 32 bits hold: it would
+    arrive as another, smaller one.  (Negative ones arrive as they are, and are refused there.)"""
+    return sizes >> 31 not in (0, -1)
+
+
+def _sizes(sizes, call):
+    if _past_32_bits(sizes):
+        raise XShareError(EUNSUPPORTED, call)
+
+
 def _on(device, t, name):
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not {device}")
@@ -1006,7 +1017,7 @@ def _stream_of(x, stream):
 
 def _gate_params(N, top_k, score, n_groups, top_groups, group_score, renormalize, scale):
     return GateParams(N, int(top_k), GATE[score] if isinstance(score, str) else int(score),
-                      int(n_groups), int(top_groups),
+                      n_groups, top_groups,
                       GROUP[group_score] if isinstance(group_score, str) else int(group_score),
                       int(bool(renormalize)), float(scale))
 
@@ -1027,7 +1038,8 @@ def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_grou
     come from the ``top_groups`` best groups (group_score "max" or "top2")."""
     dtype, ld = _logits(logits)
     T, N = logits.shape
-    k = int(top_k)
+    k, n_groups, top_groups = int(top_k), int(n_groups), int(top_groups)
+    _sizes(T | N | k | n_groups | top_groups, "xshare_gate")
     if bias is not None:
         _fit(logits.device, (bias, torch.float32, (N,), "bias"))
     ids, w = (None, None) if out is None else (out.get("ids"), out.get("w"))
@@ -1056,6 +1068,7 @@ def gate_backward(logits: torch.Tensor, ids: torch.Tensor, dw: torch.Tensor, *, 
     dtype, ld = _logits(logits)
     T, N = logits.shape
     k = ids.shape[1] if ids.dim() == 2 else -1
+    _sizes(T | N | k, "xshare_gate_backward")
     _fit(logits.device, (ids, torch.int32, (T, k), "ids"), (dw, torch.float32, (T, k), "dw"))
     if out is None:
         out = logits.new_empty((T, N), dtype=torch.float32)
@@ -1079,7 +1092,9 @@ def block_quantize(x: torch.Tensor, block_rows: int = 1, *, out=None, stream=Non
     block of block_rows x 128 (1: activations, 128: weights).  ``out``: the two to write."""
     ld = _rows(x, torch.bfloat16, "x")
     rows, cols = x.shape
-    step = max(int(block_rows), 1)
+    block_rows = int(block_rows)
+    _sizes(rows | cols | block_rows, "xshare_block_quantize")
+    step = max(block_rows, 1)
     shape = (-(-rows // step), _blocks(cols))
     q, s = (None, None) if out is None else out
     if q is None:
@@ -1090,14 +1105,17 @@ def block_quantize(x: torch.Tensor, block_rows: int = 1, *, out=None, stream=Non
         s = x.new_empty(shape, dtype=torch.float32)
     else:
         _fit(x.device, (s, torch.float32, shape, "scales"))
-    st = lib().xshare_block_quantize(x.data_ptr(), rows, cols, ld, int(block_rows), q.data_ptr(),
+    st = lib().xshare_block_quantize(x.data_ptr(), rows, cols, ld, block_rows, q.data_ptr(),
                                      s.data_ptr(), _stream_of(x, stream))
     _check(st, "xshare_block_quantize")
     return q, s
 
 
 def block_linear_workspace_bytes(T: int, n: int, k: int) -> int:
-    return int(lib().xshare_block_linear_workspace_bytes(int(T), int(n), int(k)))
+    T, n, k = int(T), int(n), int(k)
+    if _past_32_bits(T | n | k):
+        return 0                                  # as for other invalid sizes
+    return int(lib().xshare_block_linear_workspace_bytes(T, n, k))
 
 
 @_placed
@@ -1118,6 +1136,7 @@ def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale
         _dev(x, torch.uint8, (x.shape[0], k), "x codes")
         _fit(x.device, (x_scale, torch.float32, (x.shape[0], _blocks(k)), "x_scale"))
     dev, T, L = x.device, x.shape[0], lib()
+    _sizes(T | n | k, "xshare_block_linear")
     _fit(dev, (wq, torch.uint8, (n, k), "wq"),
          (ws, torch.float32, (_blocks(n), _blocks(k)), "ws"))
     if y is None:
@@ -1144,8 +1163,10 @@ def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale
 
 
 def block_experts_workspace_bytes(T: int, top_k: int, n_experts: int, d: int, f: int) -> int:
-    return int(lib().xshare_block_experts_workspace_bytes(int(T), int(top_k), int(n_experts),
-                                                          int(d), int(f)))
+    T, k, N, d, f = int(T), int(top_k), int(n_experts), int(d), int(f)
+    if _past_32_bits(T | k | N | d | f):
+        return 0
+    return int(lib().xshare_block_experts_workspace_bytes(T, k, N, d, f))
 
 
 @_placed
@@ -1163,6 +1184,7 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
     N, f = q1.shape[0], q1.shape[1]
     k = ids.shape[1]
     dev, L = x.device, lib()
+    _sizes(T | k | N | d | f, "xshare_block_experts")
     up, down = (N, _blocks(f), _blocks(d)), (N, _blocks(d), _blocks(f))
     _fit(dev, (ids, torch.int32, (T, k), "ids"), (w, torch.float32, (T, k), "w"),
          (q1, torch.uint8, (N, f, d), "w1 codes"), (q3, torch.uint8, (N, f, d), "w3 codes"),
