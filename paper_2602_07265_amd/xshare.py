@@ -956,7 +956,7 @@ def _rows(t, dtype, name, cols=None):
     """A GPU matrix of dtype whose rows may lie apart (its columns do not); its row stride."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     shape = t.shape
     if len(shape) != 2 or (cols is not None and shape[1] != cols):
@@ -1004,6 +1004,13 @@ def _workspace(device, t):
     return t.numel() * t.element_size()
 
 
+def _no_gradient(t, name, instead):
+    """Refuses a tensor whose gradient autograd would expect of this call, which records none."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which this call does not record: detach it or "
+                         f"call under torch.no_grad(); {instead}")
+
+
 def _stream_of(x, stream):
     """The handle of x's device's current stream, without a Stream object where torch gives it
     (3 us less a call, of about 10 that the shortest of these calls take)."""
@@ -1023,10 +1030,10 @@ def _gate_params(N, top_k, score, n_groups, top_groups, group_score, renormalize
 
 
 def _logits(logits):
-    if not isinstance(logits, torch.Tensor) or logits.dtype not in (torch.float32,
-                                                                    torch.bfloat16):
+    dtype = logits.dtype if isinstance(logits, torch.Tensor) else None
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
         raise ValueError("logits must be a float32 or bfloat16 GPU tensor")
-    return int(logits.dtype == torch.bfloat16), _rows(logits, logits.dtype, "logits")
+    return int(dtype is torch.bfloat16), _rows(logits, dtype, "logits")
 
 
 @_placed
@@ -1035,11 +1042,13 @@ def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_grou
          out=None, stream=None) -> dict:
     """A router's choice for each token of logits [T, N] (fp32 or bf16): dict(ids int32 [T, k],
     w fp32 [T, k]).  ``bias`` (fp32 [N]) enters the choice only; with ``n_groups`` the experts
-    come from the ``top_groups`` best groups (group_score "max" or "top2")."""
+    come from the ``top_groups`` best groups (group_score "max" or "top2").  Records no gradient
+    (``gate_backward`` gives the logits')."""
     dtype, ld = _logits(logits)
     T, N = logits.shape
     k, n_groups, top_groups = int(top_k), int(n_groups), int(top_groups)
     _sizes(T | N | k | n_groups | top_groups, "xshare_gate")
+    _no_gradient(logits, "logits", "gate_backward gives it")
     if bias is not None:
         _fit(logits.device, (bias, torch.float32, (N,), "bias"))
     ids, w = (None, None) if out is None else (out.get("ids"), out.get("w"))
@@ -1123,8 +1132,8 @@ def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale
                  workspace=None, stream=None) -> torch.Tensor:
     """y = x W^T (bf16 [T, n]) with W as codes wq uint8 [n, k] and scales ws of its 128 x 128
     blocks.  x is bf16, quantized here in 1 x 128 blocks, or with ``x_scale`` its codes
-    (``block_quantize``).  The input's gradient is this call on dy with ``wq.t().contiguous()``
-    and ``ws.t().contiguous()``."""
+    (``block_quantize``).  Records no gradient: the input's is this call on dy with
+    ``wq.t().contiguous()`` and ``ws.t().contiguous()``."""
     if wq.dim() != 2:
         raise ValueError("wq must be a matrix of codes")
     n, k = wq.shape
@@ -1137,6 +1146,8 @@ def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale
         _fit(x.device, (x_scale, torch.float32, (x.shape[0], _blocks(k)), "x_scale"))
     dev, T, L = x.device, x.shape[0], lib()
     _sizes(T | n | k, "xshare_block_linear")
+    if own:
+        _no_gradient(x, "x", "it is block_linear of y's on the transposed codes and scales")
     _fit(dev, (wq, torch.uint8, (n, k), "wq"),
          (ws, torch.float32, (_blocks(n), _blocks(k)), "ws"))
     if y is None:
@@ -1176,7 +1187,7 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
     """The routed SwiGLU experts of given pairs: y_i = sum_r w_ir E_{ids_ir}(x_i) (bf16 [T, d]),
     FP8 weights (codes uint8 [N, f, d], [N, f, d], [N, d, f]) with a scale for each 128 x 128
     block, activations quantized in 1 x 128 blocks.  ids and w [T, k] as ``gate`` or the set
-    selections return them; a pair whose id is not in [0, N) is left out."""
+    selections return them; a pair whose id is not in [0, N) is left out.  Records no gradient."""
     ldx = _rows(x, torch.bfloat16, "x")
     T, d = x.shape
     if q1.dim() != 3 or ids.dim() != 2:
@@ -1185,6 +1196,8 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
     k = ids.shape[1]
     dev, L = x.device, lib()
     _sizes(T | k | N | d | f, "xshare_block_experts")
+    _no_gradient(x, "x", "there is no backward call")
+    _no_gradient(w, "w", "there is no backward call")
     up, down = (N, _blocks(f), _blocks(d)), (N, _blocks(d), _blocks(f))
     _fit(dev, (ids, torch.int32, (T, k), "ids"), (w, torch.float32, (T, k), "w"),
          (q1, torch.uint8, (N, f, d), "w1 codes"), (q3, torch.uint8, (N, f, d), "w3 codes"),
