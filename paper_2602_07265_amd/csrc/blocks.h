@@ -93,10 +93,16 @@ inline int pair_tiles(int pairs, int E, int tile_rows) {
 constexpr int kFewMean = 16;    // gate/up in the few-row form: rows of an expert at most
 constexpr int kFewGroups = 96;  // and fewer workgroups than this in the tiled one
 constexpr int kLeastTile = 16;  // the least rows of a tile of any plan
+// Gate/up in bf16 instructions (blocks.hip says what for) up to 32 rows an expert: 96 tokens of
+// two of eight (4096, 14336) experts take 322 us a call so and 316 in FP8 ones, 512 of eight of 256
+// (7168, 2048) 2018 and 2051, 200 of eight of 128 (2048, 768) 144 and 142; past it the
+// instructions show: 1000 of those 208 and 195, 777 of the first 656 and 484, one (4096, 4096)
+// expert's 512 96 and 68.
 struct BlockExpertsPlan {
   bool one;                    // one token: the launches without tiles
   bool few_up, few_down;       // few workgroups: gate/up in the few-row form; down in that or 128 x 64
   int wide;                    // tokens of the tiled form's tiles
+  bool bf16_up;                // gate/up in bf16 instructions
   int up_rows, down_rows;      // rows of a tile of either product
 };
 inline bool one_token_form(int k, int d, int f) {   // (their rows in LDS: 38 KB at most)
@@ -108,6 +114,7 @@ inline BlockExpertsPlan block_experts_plan(int T, int k, int E, int d, int f) {
   const int expect = pairs < E ? pairs : E, mean = pairs / expect;
   p.one = T == 1 && one_token_form(k, d, f);
   p.wide = mean >= 12 ? 128 : 32;
+  p.bf16_up = mean <= 32;
   const long spans = (mean + p.wide - 1) / p.wide;
   p.few_up = mean <= kFewMean && long(expect) * quant_blocks(f) < kFewGroups;
   p.few_down = long(expect) * spans * ((d + 255) / 256) < 192;
