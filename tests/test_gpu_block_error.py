@@ -18,7 +18,7 @@ pytestmark = pytest.mark.gpu
     ("one token", 1, 64, 8, 2048, 1024), ("few / few", 6, 4, 2, 1040, 2320),
     ("few / 64", 16, 1, 1, 4096, 4096), ("few / 64", 60, 12, 3, 272, 528),
     ("few / 32", 130, 50, 4, 1040, 112), ("32 / 32", 60, 100, 4, 528, 272),
-    ("32 / few", 16, 128, 8, 144, 784), ("32 / few", 16, 128, 8, 2048, 768),
+    ("32 / few", 16, 128, 8, 144, 784), ("32 / 32", 16, 128, 8, 2048, 768),
     ("128 / 64", 130, 12, 3, 272, 1040), ("128 / 128", 480, 100, 4, 528, 272),
     ("128 in FP8 / 64", 200, 12, 3, 272, 1040), ("128 in FP8 / 128", 1100, 24, 4, 1040, 272)])
 def test_error_of_the_whole_output(forms, T, E, k, d, f):
