@@ -1047,8 +1047,10 @@ def gate(logits: torch.Tensor, top_k: int, *, score="softmax", bias=None, n_grou
     dtype, ld = _logits(logits)
     T, N = logits.shape
     k, n_groups, top_groups = int(top_k), int(n_groups), int(top_groups)
-    _sizes(T | N | k | n_groups | top_groups, "xshare_gate")
-    _no_gradient(logits, "logits", "gate_backward gives it")
+    if (T | N | k | n_groups | top_groups) >> 31:
+        _sizes(T | N | k | n_groups | top_groups, "xshare_gate")
+    if logits.requires_grad:
+        _no_gradient(logits, "logits", "gate_backward gives it")
     if bias is not None:
         _fit(logits.device, (bias, torch.float32, (N,), "bias"))
     ids, w = (None, None) if out is None else (out.get("ids"), out.get("w"))
@@ -1077,7 +1079,8 @@ def gate_backward(logits: torch.Tensor, ids: torch.Tensor, dw: torch.Tensor, *, 
     dtype, ld = _logits(logits)
     T, N = logits.shape
     k = ids.shape[1] if ids.dim() == 2 else -1
-    _sizes(T | N | k, "xshare_gate_backward")
+    if (T | N | k) >> 31:
+        _sizes(T | N | k, "xshare_gate_backward")
     _fit(logits.device, (ids, torch.int32, (T, k), "ids"), (dw, torch.float32, (T, k), "dw"))
     if out is None:
         out = logits.new_empty((T, N), dtype=torch.float32)
@@ -1102,7 +1105,8 @@ def block_quantize(x: torch.Tensor, block_rows: int = 1, *, out=None, stream=Non
     ld = _rows(x, torch.bfloat16, "x")
     rows, cols = x.shape
     block_rows = int(block_rows)
-    _sizes(rows | cols | block_rows, "xshare_block_quantize")
+    if (rows | cols | block_rows) >> 31:
+        _sizes(rows | cols | block_rows, "xshare_block_quantize")
     step = max(block_rows, 1)
     shape = (-(-rows // step), _blocks(cols))
     q, s = (None, None) if out is None else out
@@ -1145,8 +1149,9 @@ def block_linear(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, *, x_scale
         _dev(x, torch.uint8, (x.shape[0], k), "x codes")
         _fit(x.device, (x_scale, torch.float32, (x.shape[0], _blocks(k)), "x_scale"))
     dev, T, L = x.device, x.shape[0], lib()
-    _sizes(T | n | k, "xshare_block_linear")
-    if own:
+    if (T | n | k) >> 31:
+        _sizes(T | n | k, "xshare_block_linear")
+    if own and x.requires_grad:
         _no_gradient(x, "x", "it is block_linear of y's on the transposed codes and scales")
     _fit(dev, (wq, torch.uint8, (n, k), "wq"),
          (ws, torch.float32, (_blocks(n), _blocks(k)), "ws"))
@@ -1195,9 +1200,11 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
     N, f = q1.shape[0], q1.shape[1]
     k = ids.shape[1]
     dev, L = x.device, lib()
-    _sizes(T | k | N | d | f, "xshare_block_experts")
-    _no_gradient(x, "x", "there is no backward call")
-    _no_gradient(w, "w", "there is no backward call")
+    if (T | k | N | d | f) >> 31:
+        _sizes(T | k | N | d | f, "xshare_block_experts")
+    if x.requires_grad or w.requires_grad:
+        _no_gradient(x, "x", "there is no backward call")
+        _no_gradient(w, "w", "there is no backward call")
     up, down = (N, _blocks(f), _blocks(d)), (N, _blocks(d), _blocks(f))
     _fit(dev, (ids, torch.int32, (T, k), "ids"), (w, torch.float32, (T, k), "w"),
          (q1, torch.uint8, (N, f, d), "w1 codes"), (q3, torch.uint8, (N, f, d), "w3 codes"),
