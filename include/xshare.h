@@ -715,9 +715,10 @@ size_t xshare_block_experts_workspace_bytes(int32_t T, int32_t top_k, int32_t n_
 /*
  * xshare_block_experts -- the routed SwiGLU experts of given (token, expert, weight) triples:
  * y_i = sum_r w_ir E_{id_ir}(x_i) in rank order, E(x) = W2 q(silu(W1 q(x)) * (W3 q(x))), q the
- * quantisation in 1 x 128 blocks, products and sums as xshare_block_linear, SwiGLU, the
- * experts' outputs and their sum in fp32, rounded to bf16 once.  From one token to prefill
- * chunks; only weights of experts with a pair are read.
+ * quantisation in 1 x 128 blocks, products and sums as xshare_block_linear (W1 and W3 in exact
+ * products up to 32 rows an expert on average), SwiGLU, the experts' outputs and their sum in
+ * fp32, rounded to bf16 once.  From one token to prefill chunks; only weights of experts with a
+ * pair are read.
  */
 xshare_status xshare_block_experts(const xshare_block_experts_args* args);
 

@@ -849,7 +849,7 @@ float form_cost(const LinearForm& f, int T, int n) {
 // A workgroup has WR shares of 16 MR weight rows, of KW waves each, whose sums meet in
 // product_kernel's order.
 // Bound by the weights' latency and stream: 1 x 7168 x 2048 in 5.3 us; eight (2048, 768) experts'
-// 25 MB and 13 MB in 16.3 us together.  The first weights are under way while the rows are
+// 25 MB and 13 MB in 15.8 us together.  The first weights are under way while the rows are
 // quantised (gate/up 9.7 -> 8.9 us; two blocks of them: both products 17.6 -> 19.6), and nothing is
 // loaded past the last block (17.6 -> 16.3).
 struct Small {
