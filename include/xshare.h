@@ -722,6 +722,169 @@ size_t xshare_block_experts_workspace_bytes(int32_t T, int32_t top_k, int32_t n_
  */
 xshare_status xshare_block_experts(const xshare_block_experts_args* args);
 
+/* ---------------------------------------------------------------------------------------- *
+ * Tokens in expert order, products of groups of rows, and low-rank adapters, with gradients. *
+ * The pieces of a layer whose experts are a program's own or are trained: xshare_gate (or a  *
+ * set selection) -> xshare_expert_order -> xshare_dispatch -> xshare_grouped_linear ... ->    *
+ * xshare_combine, and back.  Adapters stand beside a shared projection (xshare_block_linear).*
+ * Limits: T * k and every other size at most 2^20, at most 1024 experts or adapters, k <= 32 *
+ * (XSHARE_EUNSUPPORTED beyond).  Every call gives the same bits again.                       *
+ * ---------------------------------------------------------------------------------------- */
+
+/* Workspace of xshare_expert_order (bytes, 256-aligned); 0 for invalid sizes.  That of T tokens
+ * serves any smaller T too.                                                                */
+size_t xshare_expert_order_workspace_bytes(int32_t T, int32_t top_k, int32_t n_experts);
+
+/*
+ * xshare_expert_order -- the (token, rank) pairs of a routing sorted by expert, ties by pair.
+ *
+ *   ids      [T, top_k] int32; a pair whose id lies outside [0, n_experts) has no row (an expert
+ *            of another GPU, a token of padding).  An id may be there twice in a row.
+ *   offsets  out [n_experts + 1] int32: expert e's rows are offsets[e] .. offsets[e + 1] - 1.
+ *   rows     out [T, top_k] int32: each pair's row, or -1.
+ *   pairs    out [T * top_k] int32: the pair t * top_k + r of each row; -1 from
+ *            offsets[n_experts] on.
+ *   ws       of xshare_expert_order_workspace_bytes, 16-byte aligned.
+ */
+xshare_status xshare_expert_order(const int32_t* ids, int32_t T, int32_t top_k, int32_t n_experts,
+                                  int32_t* offsets, int32_t* rows, int32_t* pairs, void* ws,
+                                  size_t ws_bytes, hipStream_t stream);
+
+/*
+ * xshare_dispatch -- each token to its pairs' rows: out[rows[t, r]] = x[t].
+ *
+ *   x, out   [T, d] and [T * top_k, d] of `dtype` (XSHARE_BF16, XSHARE_F32), rows ldx and ld_out
+ *            elements apart (at least d), any alignment of their elements; they do not overlap.
+ *   rows     as xshare_expert_order writes it: distinct; an entry outside [0, T * top_k) is no row.
+ *
+ * Rows that no pair has are left as they were.  The gradient of x is xshare_combine of out's
+ * without weights.
+ */
+xshare_status xshare_dispatch(const void* x, int64_t ldx, int32_t dtype, int32_t T, int32_t top_k,
+                              int32_t d, const int32_t* rows, void* out, int64_t ld_out,
+                              hipStream_t stream);
+
+/*
+ * xshare_combine -- rows back to their tokens: y[t] = sum over r of w[t, r] src[rows[t, r]], in
+ * rank order in fp32, rounded once; pairs without a row add nothing, whatever their weight.
+ *
+ *   src, y   [T * top_k, d] and [T, d] of `dtype`, as in xshare_dispatch.
+ *   w        [T, top_k] fp32, or NULL: every weight 1.
+ */
+xshare_status xshare_combine(const void* src, int64_t ld_src, int32_t dtype, int32_t T,
+                             int32_t top_k, int32_t d, const int32_t* rows, const float* w, void* y,
+                             int64_t ldy, hipStream_t stream);
+
+/*
+ * xshare_combine_backward -- the gradients of xshare_combine with weights:
+ * dsrc[rows[t, r]] = w[t, r] dy[t], rounded once, and dw[t, r] = dy[t] . src[rows[t, r]] in fp32
+ * (0 for a pair without a row).
+ *
+ *   dy, src, dsrc  [T, d], [T * top_k, d] and [T * top_k, d] of `dtype`; dsrc may be src.  Rows
+ *            that no pair has are left as they were.
+ *   dw       out [T, top_k] fp32.
+ */
+xshare_status xshare_combine_backward(const void* dy, int64_t lddy, const void* src, int64_t ld_src,
+                                      int32_t dtype, int32_t T, int32_t top_k, int32_t d,
+                                      const int32_t* rows, const float* w, void* dsrc,
+                                      int64_t ld_dsrc, float* dw, hipStream_t stream);
+
+/*
+ * xshare_grouped_linear -- y_p = W_e x_p for the rows p of each group e, in bf16 with fp32 sums,
+ * rounded once.
+ *
+ *   x        [P, k] bf16, rows ldx elements apart; 16-byte aligned, ldx >= k a multiple of 8, at
+ *            most 2^23 (so is the distance of every matrix of rows here).
+ *   w        [n_groups, n, k] bf16, 16-byte aligned; n and k multiples of 8.
+ *   offsets  DEVICE [n_groups + 1] int32, not decreasing, offsets[0] >= 0 and
+ *            offsets[n_groups] <= P: group e's rows are offsets[e] .. offsets[e + 1] - 1
+ *            (as xshare_expert_order writes them).  What is not so gives unspecified rows.
+ *   y        out [P, n] bf16, rows ldy >= n elements apart, ldy a multiple of 8, 16-byte aligned.
+ *            Rows outside the groups are left as they were, and x's are not read.
+ */
+xshare_status xshare_grouped_linear(const uint16_t* x, int64_t ldx, const uint16_t* w,
+                                    const int32_t* offsets, int32_t P, int32_t n_groups, int32_t n,
+                                    int32_t k, uint16_t* y, int64_t ldy, hipStream_t stream);
+
+/* xshare_grouped_linear_backward_x -- dx_p = W_e^T dy_p; dy [P, n] and dx [P, k] as y and x there. */
+xshare_status xshare_grouped_linear_backward_x(const uint16_t* dy, int64_t lddy, const uint16_t* w,
+                                               const int32_t* offsets, int32_t P, int32_t n_groups,
+                                               int32_t n, int32_t k, uint16_t* dx, int64_t lddx,
+                                               hipStream_t stream);
+
+/*
+ * xshare_grouped_linear_backward_w -- dW_e = sum over the group's rows of dy_p x_p^T.
+ *
+ *   dw        out [n_groups, n, k] of dw_dtype (XSHARE_F32, XSHARE_BF16), 16-byte aligned; zeros
+ *             for a group without rows.
+ *   accumulate  nonzero: dw += instead (XSHARE_F32 only, XSHARE_EUNSUPPORTED otherwise).
+ */
+xshare_status xshare_grouped_linear_backward_w(const uint16_t* dy, int64_t lddy, const uint16_t* x,
+                                               int64_t ldx, const int32_t* offsets, int32_t P,
+                                               int32_t n_groups, int32_t n, int32_t k, void* dw,
+                                               int32_t dw_dtype, int32_t accumulate,
+                                               hipStream_t stream);
+
+/*
+ * Arguments of xshare_adapters and xshare_adapters_backward.  Zero-initialise, set struct_size,
+ * fill.
+ *
+ *   T, n_adapters, rank, n, d   rank <= 128; rank, n and d multiples of 8.
+ *   x           [T, d] bf16, rows ldx elements apart; 16-byte aligned, ldx a multiple of 8 (so is
+ *               every matrix of rows here).
+ *   a, b        [n_adapters, rank, d] and [n_adapters, n, rank] bf16, 16-byte aligned.
+ *   ids         [T] int32: each token's adapter; outside [0, n_adapters): none.
+ *   scales      [n_adapters] fp32, or NULL: 1.
+ *   base, out   xshare_adapters: [T, n]; _backward: [T, d] bf16; base NULL: zeros.  out may be base;
+ *               otherwise they do not overlap.
+ *   dy          _backward only: [T, n] bf16, the gradient of xshare_adapters' out.
+ *   da, db      _backward only, out: [n_adapters, rank, d] and [n_adapters, n, rank] fp32, 16-byte
+ *               aligned; zeros for an adapter without tokens.
+ *   ws          of xshare_adapters_workspace_bytes, 16-byte aligned.
+ */
+typedef struct {
+  size_t struct_size;
+  int32_t T, n_adapters, rank, n, d;
+  const uint16_t* x;
+  int64_t ldx;
+  const uint16_t* a;
+  const uint16_t* b;
+  const int32_t* ids;
+  const float* scales;
+  const uint16_t* base;
+  int64_t ld_base;
+  uint16_t* out;
+  int64_t ld_out;
+  const uint16_t* dy;
+  int64_t lddy;
+  float* da;
+  float* db;
+  void* ws;
+  size_t ws_bytes;
+  hipStream_t stream;
+} xshare_adapters_args;
+
+/* Workspace of xshare_adapters, or with `backward` of xshare_adapters_backward (bytes,
+ * 256-aligned); 0 for invalid sizes.  That of T tokens serves any smaller T too.            */
+size_t xshare_adapters_workspace_bytes(int32_t T, int32_t n_adapters, int32_t rank, int32_t n,
+                                       int32_t d, int32_t backward);
+
+/*
+ * xshare_adapters -- low-rank adapters of many requests beside a shared projection:
+ * out_t = base_t + scales[e] B_e A_e x_t, e = ids[t]; out_t = base_t for a token without one (it
+ * has no part in anything else).  A_e x_t is held in fp32 (to 16 bits or more where it meets
+ * B_e), sums are fp32, and out is rounded once.
+ */
+xshare_status xshare_adapters(const xshare_adapters_args* args);
+
+/*
+ * xshare_adapters_backward -- its gradients: with h_t = A_e x_t and dh_t = scales[e] B_e^T dy_t,
+ * out_t = base_t + A_e^T dh_t (base: the part of x's gradient that the shared projection gives),
+ * da_e = sum over its tokens of dh_t x_t^T, db_e = scales[e] times the sum of dy_t h_t^T (base
+ * itself passes dy on).  The last two in fp32 throughout (h and dh to 24 bits).
+ */
+xshare_status xshare_adapters_backward(const xshare_adapters_args* args);
+
 /* Static description of a status code (never NULL).                                      */
 const char* xshare_status_string(int32_t status);
 

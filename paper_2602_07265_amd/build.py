@@ -10,6 +10,10 @@ Translation units:
 * gate.hip  -- routing by scores, bias and groups, and its backward pass; -ffp-contract=off;
 * blocks.hip -- FP8 products with a scale for each block of 128: quantiser, linear, experts;
 * abi_blocks.hip -- their extern "C" entry points;
+* order.hip, move.hip -- the pairs' expert order; rows into it and back, with gradients;
+* grouped.hip -- bf16 products of groups of rows and their gradients;
+* adapters.hip -- low-rank adapters of many requests and their gradients;
+* abi_groups.hip -- the entry points of these four;
 * probe.hip -- the streaming-read probe (measurement of the HBM read ceiling).
 Every HIP compile disables packed-fp32 instruction selection.  The same sources built with
 XS_BLOCK_TIMES=1 give libxshare_timeline.so, the profiling build whose expert GEMMs stamp
@@ -45,6 +49,11 @@ UNITS = {
                  "-fno-fast-math"],
     "blocks.hip": ["-fhip-fp32-correctly-rounded-divide-sqrt"],
     "abi_blocks.hip": [],
+    "order.hip": [],
+    "move.hip": [],
+    "grouped.hip": [],
+    "adapters.hip": [],
+    "abi_groups.hip": [],
     "probe.hip": [],
 }
 

@@ -1,0 +1,550 @@
+// Low-rank adapters of many requests beside a shared projection, and their gradients.
+//   y_t = base_t + s_e B_e A_e x_t          e the adapter of token t, A_e [r, d], B_e [n, r]
+//   dh_t = s_e B_e^T dy_t,  dx_t = base_t + A_e^T dh_t,
+//   dA_e = sum over its tokens of dh_t x_t^T,  dB_e = s_e sum of dy_t h_t^T,  h_t = A_e x_t
+//
+// Every product has one short side, r, so all are bound by reading and writing rows of d and n
+// values.  Up to kAdapterFew tokens are worked on one by one: a wave for each value of h, then a
+// lane for each of y.  More are put in adapters' order first, and tiles of tokens of one adapter
+// go through the matrix instructions.  h and dh are held as sums of three bf16 values (24 bits), so
+// that the products with them are as exact as those of fp32 values; y and dx, which are rounded
+// to bf16, take two of the three.  Going backward the factors are transposed first, which are
+// small beside the rows, and dh and dx are the two forward products on them.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "groups.h"
+#include "tiles.h"
+
+namespace xs {
+namespace {
+
+__device__ __forceinline__ float value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+__device__ __forceinline__ void values8(const uint4& v, float (&x)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ uint4 to_bf16x8(const float (&x)[8]) {
+  return make_uint4(to_bf16x2(x[0], x[1]), to_bf16x2(x[2], x[3]), to_bf16x2(x[4], x[5]),
+                    to_bf16x2(x[6], x[7]));
+}
+
+// ---------------------------------------------------------------------------- few tokens
+
+// h[t, j] = A_e[j] . x_t, a wave each.
+__global__ __launch_bounds__(256) void few_shrink_kernel(AdaptersArgs a, float* h) {
+  const int lane = threadIdx.x & 63;
+  const int t = blockIdx.y, j = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int e = a.ids[t];
+  if ((unsigned)e >= (unsigned)a.L || j >= a.r) return;
+  const uint16_t* const x = a.x + (size_t)t * a.ldx;
+  const uint16_t* const w = a.a + ((size_t)e * a.r + j) * a.d;
+  float sum = 0.0f;
+#pragma unroll 8
+  for (int c = 8 * lane; c < a.d; c += 512) {
+    float p[8], q[8];
+    values8(*reinterpret_cast<const uint4*>(x + c), p);
+    values8(*reinterpret_cast<const uint4*>(w + c), q);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(p[i], q[i], sum);
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) h[(size_t)t * a.r + j] = sum;
+}
+
+// y[t, c] = base + s B_e[c] . h_t, a lane each.
+__global__ __launch_bounds__(256) void few_expand_kernel(AdaptersArgs a, const float* h) {
+  __shared__ float hs[kMaxRank];
+  const int t = blockIdx.y, c = blockIdx.x * 256 + threadIdx.x;
+  const int e = a.ids[t];
+  const bool live = (unsigned)e < (unsigned)a.L;
+  if (live && (int)threadIdx.x < a.r) hs[threadIdx.x] = h[(size_t)t * a.r + threadIdx.x];
+  __syncthreads();
+  if (c >= a.n) return;
+  float y = 0.0f;
+  if (live) {
+    const uint16_t* const w = a.b + ((size_t)e * a.n + c) * a.r;
+#pragma unroll 4
+    for (int j = 0; j < a.r; j += 8) {
+      float q[8];
+      values8(*reinterpret_cast<const uint4*>(w + j), q);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y = __builtin_fmaf(q[i], hs[j + i], y);
+    }
+    if (a.scales) y *= a.scales[e];
+  }
+  if (a.base) {
+    const float b = value(a.base[(size_t)t * a.ld_base + c]);
+    y = live ? y + b : b;
+  }
+  a.out[(size_t)t * a.ld_out + c] = to_bf16(y);
+}
+
+// ---------------------------------------------------------------------------- many tokens
+
+// Tokens without an adapter: out = base, or zeros.
+__global__ __launch_bounds__(256) void rest_kernel(AdaptersArgs a, int columns) {
+  const int t = blockIdx.x;
+  if (a.rows[t] >= 0) return;
+  for (int c = 8 * threadIdx.x; c < columns; c += 8 * 256) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (a.base) v = *reinterpret_cast<const uint4*>(a.base + (size_t)t * a.ld_base + c);
+    *reinterpret_cast<uint4*>(a.out + (size_t)t * a.ld_out + c) = v;
+  }
+}
+
+// [rows, cols] of each adapter with tokens -> [cols, rows]; a thread takes eight rows of a column.
+__global__ __launch_bounds__(256) void transpose_kernel(const uint16_t* in, uint16_t* out, int rows,
+                                                        int cols, const int32_t* offsets) {
+  const int e = blockIdx.y;
+  if (offsets[e] == offsets[e + 1]) return;
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const int c = (int)(i % cols), r = (int)(i / cols) * 8;
+  if (r >= rows) return;
+  const size_t at = (size_t)e * rows * cols;
+  uint32_t v[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = in[at + (size_t)(r + q) * cols + c];
+  *reinterpret_cast<uint4*>(out + at + (size_t)c * rows + r) =
+      make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
+// v as three bf16 values that sum up to it (to 24 bits); infinities and NaN as one.
+__device__ __forceinline__ void split3(float v, uint16_t (&p)[3]) {
+  p[0] = to_bf16(v);
+  const float hi = value(p[0]);
+  const bool finite = fabsf(hi) < __builtin_inff();
+  const float rest = finite ? v - hi : 0.0f;
+  p[1] = to_bf16(rest);
+  p[2] = to_bf16(rest - value(p[1]));
+}
+
+struct Shrink {
+  const int32_t* offsets;
+  const int32_t* tokens;
+  int L, T, r, K;
+  const uint16_t* x;           // [T, K]
+  long ldx;
+  const uint16_t* w;           // [L, r, K]
+  const float* scales;         // [L], or null
+  uint16_t* h;                 // [T, 3, 16 JT]
+};
+
+// h of 16 MT tokens of one adapter: the waves take blocks of 64 of the reduction in turn, operands
+// straight from memory, and their sums meet in LDS.
+template <int MT, int JT>
+__global__ __launch_bounds__(512) void shrink_kernel(Shrink a) {
+  constexpr int kWaves = 8;
+  extern __shared__ floatx4 sums[];                    // [kWaves][MT JT][64]
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  Place p;
+  if (!find_place(a.offsets, a.L, a.T, 16 * MT, 1, p)) return;
+  const int e = __builtin_amdgcn_readfirstlane(p.e);
+  const int first = __builtin_amdgcn_readfirstlane(p.first);
+  const int live = __builtin_amdgcn_readfirstlane(p.live);
+  const uint16_t* x[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int token = a.tokens[first + min(16 * t + n, live - 1)];
+    x[t] = a.x + (size_t)token * a.ldx;
+  }
+  const uint16_t* w[JT];
+#pragma unroll
+  for (int j = 0; j < JT; ++j)
+    w[j] = a.w + ((size_t)e * a.r + min(16 * j + n, a.r - 1)) * a.K;
+  floatx4 acc[JT][MT];
+#pragma unroll
+  for (int j = 0; j < JT; ++j)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[j][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  for (int k0 = 64 * wave; k0 < a.K; k0 += 64 * kWaves) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int k = k0 + 32 * s + 8 * g;
+      const bool in = k < a.K;
+      uint4 fx[MT], fw[JT];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) fx[t] = in ? *reinterpret_cast<const uint4*>(x[t] + k) : zero;
+#pragma unroll
+      for (int j = 0; j < JT; ++j) fw[j] = in ? *reinterpret_cast<const uint4*>(w[j] + k) : zero;
+#pragma unroll
+      for (int j = 0; j < JT; ++j)
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+          acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(bf16x8, fw[j]), __builtin_bit_cast(bf16x8, fx[t]), acc[j][t], 0, 0,
+              0);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < JT; ++j)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) sums[(wave * MT * JT + j * MT + t) * 64 + lane] = acc[j][t];
+  __syncthreads();
+  const float s = a.scales ? a.scales[e] : 1.0f;
+  for (int i = wave; i < MT * JT; i += kWaves) {
+    const int j = i / MT, t = i % MT;
+    floatx4 v = sums[i * 64 + lane];
+#pragma unroll
+    for (int q = 1; q < kWaves; ++q) v += sums[(q * MT * JT + i) * 64 + lane];
+    if (16 * t + n >= live) continue;
+    uint16_t parts[4][3];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)                        // (past the rank: zeros)
+      split3(16 * j + 4 * g + c < a.r ? v[c] * s : 0.0f, parts[c]);
+    uint16_t* const out = a.h + (size_t)(first + 16 * t + n) * (48 * JT) + 16 * j + 4 * g;
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+      *reinterpret_cast<uint2*>(out + q * 16 * JT) =
+          make_uint2(parts[0][q] | (uint32_t)parts[1][q] << 16,
+                     parts[2][q] | (uint32_t)parts[3][q] << 16);
+  }
+}
+
+struct Expand {
+  const int32_t* offsets;
+  const int32_t* tokens;
+  int L, T, r, N;
+  const uint16_t* h;           // [T, 3, 16 JT]
+  const uint16_t* w;           // [L, N, r]
+  const float* scales;         // [L], or null
+  const uint16_t* base;        // [T, N], or null
+  long ld_base;
+  uint16_t* out;
+  long ld_out;
+};
+constexpr int kExpandColumns = 512;    // of a workgroup
+
+// out of 16 MT tokens of one adapter and kExpandColumns columns: each wave takes 32 of these at a
+// time, dealt so that a lane's eight results are neighbours.
+template <int MT, int JT>
+__global__ __launch_bounds__(256) void expand_kernel(Expand a) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  Place p;
+  const int columns = (a.N + kExpandColumns - 1) / kExpandColumns;
+  if (!find_place(a.offsets, a.L, a.T, 16 * MT, columns, p)) return;
+  const int e = __builtin_amdgcn_readfirstlane(p.e);
+  const int first = __builtin_amdgcn_readfirstlane(p.first);
+  const int live = __builtin_amdgcn_readfirstlane(p.live);
+  const int c0 = __builtin_amdgcn_readfirstlane(p.column) * kExpandColumns;
+  long token[MT];
+  bf16x8 fh[MT][JT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int row = first + min(16 * t + n, live - 1);
+    token[t] = a.tokens[row];
+#pragma unroll
+    for (int s = 0; s < JT; ++s)
+      fh[t][s] = *reinterpret_cast<const bf16x8*>(a.h + (size_t)row * (48 * JT) + 32 * s + 8 * g);
+  }
+  const float scale = a.scales ? a.scales[e] : 1.0f;
+  const uint16_t* const w = a.w + (size_t)e * a.N * a.r;
+  const int end = min(c0 + kExpandColumns, a.N);
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  for (int c = c0 + 32 * wave; c < end; c += 128) {
+    floatx4 acc[2][MT];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int col = min(c + 8 * (n >> 2) + 4 * m + (n & 3), a.N - 1);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) acc[m][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < JT; ++s) {
+        // the first two parts of h lie one behind the other: W's row goes with both
+        const int j = (32 * s + 8 * g) % (16 * JT);
+        const uint4 v =
+            j < a.r ? *reinterpret_cast<const uint4*>(w + (size_t)col * a.r + j) : zero;
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+          acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v),
+                                                              fh[t][s], acc[m][t], 0, 0, 0);
+      }
+    }
+    const int to = c + 8 * g;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      if (16 * t + n >= live || to >= a.N) continue;
+      float v[8] = {};
+      if (a.base)
+        values8(*reinterpret_cast<const uint4*>(a.base + token[t] * a.ld_base + to), v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(scale, acc[i / 4][t][i % 4], v[i]);
+      *reinterpret_cast<uint4*>(a.out + token[t] * a.ld_out + to) = to_bf16x8(v);
+    }
+  }
+}
+
+struct Factors {
+  const int32_t* offsets;
+  const int32_t* tokens;
+  int L, T, r, n, d, splits;
+  const uint16_t *x, *dy;
+  long ldx, lddy;
+  const uint16_t *h, *dh;      // [T, 3, 16 JT]
+  const float* scales;
+  float *da, *db;              // [L, r, d] and [L, n, r]; where splits > 1 a part's of the workspace
+};
+
+// The gradients of kGradColumns columns of a factor's long side: dA from x and dh, dB from dy and
+// h, both operands across the reduction, which runs over the adapter's tokens in blocks of 64.
+// Workgroup (column tile: dA's, then dB's; part of the tokens; adapter).
+template <int JT>
+__global__ __launch_bounds__(256) void factors_kernel(Factors a) {
+  constexpr int kThreads = 256, kRank = 16 * JT;
+  using Wide = Operand<true, false, kGradColumns, kThreads>;
+  constexpr int kHPieces = 3 * kRank / 8;              // 16-byte pieces of a row of h
+  constexpr int kHLoads = (kBlock * kHPieces + kThreads - 1) / kThreads;
+  constexpr int kStage = kBlock * (kGradColumns + 3 * kRank);
+  extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  const int tiles_a = (a.d + kGradColumns - 1) / kGradColumns;
+  const bool is_a = (int)blockIdx.x < tiles_a;
+  const int c0 = (is_a ? blockIdx.x : blockIdx.x - tiles_a) * kGradColumns;
+  const int width = is_a ? a.d : a.n;
+  const int e = blockIdx.z;
+  int lo, hi;
+  group_rows(a.offsets, e, a.T, lo, hi);
+  {  // this part of the adapter's tokens, in whole blocks
+    const int blocks = (hi - lo + kBlock - 1) / kBlock;
+    const int from = (int)((long)blocks * blockIdx.y / a.splits) * kBlock;
+    const int upto = (int)((long)blocks * (blockIdx.y + 1) / a.splits) * kBlock;
+    hi = min(hi, lo + upto);
+    lo += from;
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  const int rows = __builtin_amdgcn_readfirstlane(hi) - lo;
+  const uint16_t* const wide = is_a ? a.x : a.dy;
+  const long ld = is_a ? a.ldx : a.lddy;
+  const uint16_t* const skinny = is_a ? a.dh : a.h;
+  const uint16_t* const zeros = reinterpret_cast<const uint16_t*>(kZeros);
+
+  // lane's piece of load j of the wide rows: row j * kStep + tid / 16, columns off[j] ..
+  Wide ow;
+  ow.init(wide + c0, 0, min(kGradColumns, width - c0), 0, tid);
+  int token[Wide::kLoads];
+  auto fetch = [&](int b) {
+#pragma unroll
+    for (int j = 0; j < Wide::kLoads; ++j) {
+      const int q = b * kBlock + j * Wide::kStep + ow.row;
+      token[j] = q < rows ? a.tokens[lo + q] : -1;
+    }
+  };
+  // h's rows: LDS [3][64][kRank], each part an operand of its own
+  using Rank = Operand<true, false, kRank, kBlock * kRank / 8>;
+  auto load = [&](int b, uint16_t* stage) {
+#pragma unroll
+    for (int j = 0; j < Wide::kLoads; ++j)
+      to_lds(token[j] >= 0 ? wide + c0 + (size_t)token[j] * ld + ow.off[j] : zeros,
+             stage + j * kThreads * 8 + wave * 512);
+    uint16_t* const hl = stage + kBlock * kGradColumns;
+#pragma unroll
+    for (int j = 0; j < kHLoads; ++j) {
+      const int i = j * kThreads + tid;                // piece of the stage's [3][64][kRank / 8]
+      if (kBlock * kHPieces % kThreads != 0 && j * kThreads + wave * 64 >= kBlock * kHPieces)
+        break;                                         // (whole waves)
+      const int part = i / (kBlock * kRank / 8), in = i % (kBlock * kRank / 8);
+      const int q = in / (kRank / 8), slot = in % (kRank / 8);
+      const int c = 8 * (slot ^ Rank::swap(q) << 1);
+      const int row = b * kBlock + q;
+      to_lds(row < rows ? skinny + (size_t)(lo + row) * (3 * kRank) + part * kRank + c : zeros,
+             hl + (j * kThreads + wave * 64) * 8);
+    }
+  };
+  constexpr int kTiles = kGradColumns / 16 / 4;        // column tiles of a wave
+  floatx4 acc[kTiles][JT];
+#pragma unroll
+  for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+    for (int j = 0; j < JT; ++j) acc[m][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  auto step = [&](const uint16_t* __restrict__ stage) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      bf16x8 fw[kTiles];
+#pragma unroll
+      for (int m = 0; m < kTiles; ++m)
+        fw[m] = Wide::read_across(stage, (wave * kTiles + m) * 16, s, n, g);
+#pragma unroll
+      for (int part = 0; part < 3; ++part) {
+        const uint16_t* const hl = stage + kBlock * kGradColumns + part * kBlock * kRank;
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+          const bf16x8 fh = Rank::read_across(hl, 16 * j, s, n, g);
+#pragma unroll
+          for (int m = 0; m < kTiles; ++m)
+            acc[m][j] = is_a ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[m], fh, acc[m][j], 0, 0, 0)
+                             : __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, fw[m], acc[m][j], 0, 0, 0);
+        }
+      }
+    }
+  };
+  const int blocks = (rows + kBlock - 1) / kBlock;
+  if (blocks > 0) {
+    fetch(0);
+    load(0, lds);
+    if (blocks > 1) fetch(1);
+    for (int b = 0; b < blocks; ++b) {
+      uint16_t* const here = lds + (b & 1) * kStage;
+      wait_loads<0>();
+      if (b + 1 < blocks) {
+        load(b + 1, lds + (~b & 1) * kStage);
+        if (b + 2 < blocks) fetch(b + 2);
+      }
+      step(here);
+    }
+  }
+  const size_t plane = (size_t)blockIdx.y * a.L * a.r * ((size_t)a.n + a.d);
+  const float scale = is_a || !a.scales ? 1.0f : a.scales[e];   // (dh has its own in it)
+#pragma unroll
+  for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+      const int wide0 = c0 + (wave * kTiles + m) * 16;
+      if (is_a) {                                      // lane: rank n, columns 4 g ..
+        const int rank = 16 * j + n, c = wide0 + 4 * g;
+        if (rank < a.r && c < a.d)
+          *reinterpret_cast<floatx4*>(a.da + plane + ((size_t)e * a.r + rank) * a.d + c) = acc[m][j];
+      } else {                                         // lane: column n, ranks 4 g ..
+        const int rank = 16 * j + 4 * g, c = wide0 + n;
+        if (rank < a.r && c < a.n)
+          *reinterpret_cast<floatx4*>(a.db + plane + ((size_t)e * a.n + c) * a.r + rank) =
+              acc[m][j] * scale;
+      }
+    }
+}
+
+// The parts of the factors' gradients, [splits][da's, then db's values], in order.
+__global__ __launch_bounds__(256) void sum_parts_kernel(const float* part, int splits, size_t na,
+                                                        size_t nb, float* da, float* db) {
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= na + nb) return;
+  floatx4 v = *reinterpret_cast<const floatx4*>(part + i);
+  for (int s = 1; s < splits; ++s)
+    v += *reinterpret_cast<const floatx4*>(part + (size_t)s * (na + nb) + i);
+  *reinterpret_cast<floatx4*>(i < na ? da + i : db + (i - na)) = v;
+}
+
+template <typename F>
+hipError_t by_rank(int r, F launch) {
+  if (r <= 16) return launch(std::integral_constant<int, 1>());
+  if (r <= 32) return launch(std::integral_constant<int, 2>());
+  if (r <= 64) return launch(std::integral_constant<int, 4>());
+  return launch(std::integral_constant<int, 8>());
+}
+
+// Row tiles of `tile` tokens at most, for the eight XCDs.
+long most_tiles(int T, int L, int tile, long columns) {
+  const long some = T < L ? T : L;
+  return ((some + (T - some) / tile) * columns + 7) / 8 * 8;
+}
+
+template <typename K>
+hipError_t allow_lds(K kernel, int bytes) {
+  if (bytes <= 64 * 1024) return hipSuccess;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+hipError_t launch_shrink(const Shrink& s, hipStream_t stream) {
+  return by_rank(s.r, [&](auto j) {
+    constexpr int JT = decltype(j)::value, MT = JT >= 4 ? 2 : 1;
+    constexpr int kBytes = 8 * MT * JT * 64 * 16;
+    const auto kernel = shrink_kernel<MT, JT>;
+    const hipError_t e = allow_lds(kernel, kBytes);
+    if (e != hipSuccess) return e;
+    kernel<<<(unsigned)most_tiles(s.T, s.L, 16 * MT, 1), 512, kBytes, stream>>>(s);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_expand(const Expand& x, hipStream_t stream) {
+  return by_rank(x.r, [&](auto j) {
+    constexpr int JT = decltype(j)::value, MT = 2;
+    const long columns = (x.N + kExpandColumns - 1) / kExpandColumns;
+    const long grid = most_tiles(x.T, x.L, 16 * MT, columns);
+    if (grid * 256 > 0xFFFFFFFFl) return hipErrorInvalidConfiguration;
+    expand_kernel<MT, JT><<<(unsigned)grid, 256, 0, stream>>>(x);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_factors(const Factors& f, hipStream_t stream) {
+  return by_rank(f.r, [&](auto j) {
+    constexpr int JT = decltype(j)::value;
+    constexpr int kBytes = 2 * kBlock * (kGradColumns + 48 * JT) * 2;
+    static_assert(kBytes <= 160 * 1024, "LDS of a compute unit");
+    const auto kernel = factors_kernel<JT>;
+    const hipError_t e = allow_lds(kernel, kBytes);
+    if (e != hipSuccess) return e;
+    const int tiles = (f.n + kGradColumns - 1) / kGradColumns +
+                      (f.d + kGradColumns - 1) / kGradColumns;
+    kernel<<<dim3(tiles, f.splits, f.L), 256, kBytes, stream>>>(f);
+    return hipGetLastError();
+  });
+}
+
+hipError_t in_order(const AdaptersArgs& a, hipStream_t stream) {
+  OrderArgs o{a.ids, a.T, a.L, a.offsets, a.rows, a.tokens, a.counts};
+  return launch_order(o, stream);
+}
+
+}  // namespace
+
+hipError_t launch_adapters(const AdaptersArgs& a, hipStream_t stream) {
+  if (a.T <= kAdapterFew) {
+    float* const h = reinterpret_cast<float*>(a.h);    // (fp32 [T, r] in the place of three parts)
+    few_shrink_kernel<<<dim3((a.r + 3) / 4, a.T), 256, 0, stream>>>(a, h);
+    few_expand_kernel<<<dim3((a.n + 255) / 256, a.T), 256, 0, stream>>>(a, h);
+    return hipGetLastError();
+  }
+  hipError_t e = in_order(a, stream);
+  if (e != hipSuccess) return e;
+  const Shrink s{a.offsets, a.tokens, a.L, a.T, a.r, a.d, a.x, a.ldx, a.a, nullptr, a.h};
+  if ((e = launch_shrink(s, stream)) != hipSuccess) return e;
+  if (a.out != a.base) rest_kernel<<<a.T, 256, 0, stream>>>(a, a.n);
+  const Expand x{a.offsets, a.tokens, a.L, a.T, a.r, a.n, a.h, a.b, a.scales,
+                 a.base, a.ld_base, a.out, a.ld_out};
+  return launch_expand(x, stream);
+}
+
+hipError_t launch_adapters_backward(const AdaptersArgs& a, hipStream_t stream) {
+  hipError_t e = in_order(a, stream);
+  if (e != hipSuccess) return e;
+  transpose_kernel<<<dim3((unsigned)(((size_t)a.r / 8 * a.d + 255) / 256), a.L), 256, 0, stream>>>(
+      a.a, a.at, a.r, a.d, a.offsets);
+  transpose_kernel<<<dim3((unsigned)(((size_t)a.n / 8 * a.r + 255) / 256), a.L), 256, 0, stream>>>(
+      a.b, a.bt, a.n, a.r, a.offsets);
+  if (a.T > 0) {
+    const Shrink s{a.offsets, a.tokens, a.L, a.T, a.r, a.d, a.x, a.ldx, a.a, nullptr, a.h};
+    if ((e = launch_shrink(s, stream)) != hipSuccess) return e;
+    const Shrink g{a.offsets, a.tokens, a.L, a.T, a.r, a.n, a.dy, a.lddy, a.bt, a.scales, a.dh};
+    if ((e = launch_shrink(g, stream)) != hipSuccess) return e;
+    if (a.out != a.base) rest_kernel<<<a.T, 256, 0, stream>>>(a, a.d);
+    const Expand x{a.offsets, a.tokens, a.L, a.T, a.r, a.d, a.dh, a.at, nullptr,
+                   a.base, a.ld_base, a.out, a.ld_out};
+    if ((e = launch_expand(x, stream)) != hipSuccess) return e;
+  }
+  const size_t na = (size_t)a.L * a.r * a.d, nb = (size_t)a.L * a.r * a.n;
+  const bool parts = a.splits > 1;
+  const Factors f{a.offsets, a.tokens, a.L, a.T, a.r, a.n, a.d, a.splits, a.x, a.dy, a.ldx, a.lddy,
+                  a.h, a.dh, a.scales, parts ? a.part : a.da, parts ? a.part + na : a.db};
+  if ((e = launch_factors(f, stream)) != hipSuccess) return e;
+  if (parts)
+    sum_parts_kernel<<<(unsigned)((na + nb) / 4 / 256 + 1), 256, 0, stream>>>(a.part, a.splits, na,
+                                                                             nb, a.da, a.db);
+  return hipGetLastError();
+}
+
+}  // namespace xs

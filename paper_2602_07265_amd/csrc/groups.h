@@ -1,0 +1,149 @@
+// Launchers of the pairs' expert order (order.hip), the moves of rows into it and back (move.hip),
+// the products of groups of rows (grouped.hip) and the low-rank adapters (adapters.hip), and
+// the workspace layouts of those that need one.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "internal.h"
+
+namespace xs {
+
+constexpr int kMaxGroupSize = 1 << 20;   // every size of these calls, and T * k
+constexpr int kMaxRank = 128;            // of an adapter
+
+// ---------------------------------------------------------------------------- order
+
+struct OrderArgs {
+  const int32_t* ids;          // [pairs]
+  int pairs, E;
+  int32_t* offsets;            // [E + 1]
+  int32_t* rows;               // [pairs]
+  int32_t* pair_of;            // [pairs]
+  int32_t* counts;             // [order_parts(pairs), E], unused by one workgroup
+};
+constexpr int kOrderOne = 8192;     // pairs that one workgroup sorts by itself
+constexpr int kOrderPart = 4096;    // pairs of a workgroup where there are several
+inline int order_parts(int pairs) {
+  return pairs <= kOrderOne ? 0 : (pairs + kOrderPart - 1) / kOrderPart;
+}
+inline size_t order_bytes(int pairs, int E) {
+  const size_t b = align256(sizeof(int32_t) * size_t(order_parts(pairs)) * E);
+  return b > 0 ? b : 256;
+}
+hipError_t launch_order(const OrderArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------------------- moves
+
+struct MoveArgs {
+  int fp32;                    // 0: bf16 elements
+  int T, k, d;
+  const int32_t* rows;         // [T, k]
+  const void* token;           // [T, d] x, dy
+  long ld_token;
+  const void* row;             // [T k, d] rows read
+  long ld_row;
+  const float* w;              // [T, k], or null: 1
+  void* out_token;             // [T, d]
+  long ld_out_token;
+  void* out_row;               // [T k, d]
+  long ld_out_row;
+  float* dw;                   // [T, k]
+};
+hipError_t launch_dispatch(const MoveArgs& a, hipStream_t stream);
+hipError_t launch_combine(const MoveArgs& a, hipStream_t stream);
+hipError_t launch_combine_backward(const MoveArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------------------- products
+
+struct GroupedArgs {
+  int P, E, n, k;
+  const int32_t* offsets;      // [E + 1]
+  const uint16_t* x;           // [P, k]
+  long ldx;
+  const uint16_t* dy;          // [P, n]
+  long lddy;
+  const uint16_t* w;           // [E, n, k]
+  uint16_t* out;               // y [P, n] or dx [P, k]
+  long ldo;
+  void* dw;                    // [E, n, k], bf16 or fp32
+  int dw_fp32, accumulate;
+};
+hipError_t launch_grouped_linear(const GroupedArgs& a, hipStream_t stream);
+hipError_t launch_grouped_backward_x(const GroupedArgs& a, hipStream_t stream);
+hipError_t launch_grouped_backward_w(const GroupedArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------------------- adapters
+
+// Tokens up to which an adapters call goes token by token in two launches, without an order.
+constexpr int kAdapterFew = 64;
+inline int rank16(int r) { return (r + 15) / 16 * 16; }
+
+// Parts that the rows of an adapter are summed in for its factors' gradients.
+constexpr int kGradColumns = 128;      // columns of x or dy of a workgroup
+inline int adapter_splits(int T, int L, int n, int d) {
+  const long groups = long(L) * ((n + kGradColumns - 1) / kGradColumns +
+                                 (d + kGradColumns - 1) / kGradColumns);
+  const long want = 768 / groups, most = (T + 255) / 256;
+  const long n_parts = want < most ? want : most;
+  return n_parts < 1 ? 1 : int(n_parts);
+}
+
+struct AdaptersLayout {
+  size_t offsets, rows, tokens;  // the tokens in adapters' order
+  size_t counts;                 // of the sort
+  size_t h, dh;                  // bf16 [T, 3, rank16]: A x and s B^T dy, as three parts that sum up
+  size_t at, bt;                 // [L, d, r] and [L, r, n]: the factors transposed (backward)
+  size_t part;                   // fp32 [splits, L (n + d) r] where splits > 1 (backward)
+  size_t total;
+};
+inline AdaptersLayout adapters_layout(int T, int L, int r, int n, int d, bool backward) {
+  AdaptersLayout A{};
+  size_t o = 0;
+  A.offsets = o; o += align256(sizeof(int32_t) * (size_t(L) + 1));
+  A.rows = o;    o += align256(sizeof(int32_t) * size_t(T));
+  A.tokens = o;  o += align256(sizeof(int32_t) * size_t(T));
+  A.counts = o;  o += order_bytes(T, L);
+  A.h = o;       o += align256(6 * size_t(T) * rank16(r));
+  A.dh = o;
+  A.at = A.bt = A.part = o;
+  if (backward) {
+    o += align256(6 * size_t(T) * rank16(r));
+    A.at = o;    o += align256(2 * size_t(L) * d * r);
+    A.bt = o;    o += align256(2 * size_t(L) * n * r);
+    A.part = o;
+    // (of any number of tokens up to T: the parts grow with them)
+    const int splits = adapter_splits(T, L, n, d);
+    if (splits > 1) o += align256(4 * size_t(splits) * L * r * (size_t(n) + d));
+  }
+  A.total = o > 0 ? o : 256;
+  return A;
+}
+
+struct AdaptersArgs {
+  int T, L, r, n, d;
+  const uint16_t* x;           // [T, d]
+  long ldx;
+  const uint16_t* a;           // [L, r, d]
+  const uint16_t* b;           // [L, n, r]
+  const int32_t* ids;          // [T]
+  const float* scales;         // [L], or null: 1
+  const uint16_t* base;        // [T, n] or, backward, [T, d]; or null: 0
+  long ld_base;
+  uint16_t* out;               // [T, n] or, backward, [T, d]
+  long ld_out;
+  const uint16_t* dy;          // [T, n] (backward)
+  long lddy;
+  float* da;                   // [L, r, d] (backward)
+  float* db;                   // [L, n, r]
+  int32_t *offsets, *rows, *tokens, *counts;
+  uint16_t *h, *dh, *at, *bt;
+  float* part;
+  int splits;
+};
+hipError_t launch_adapters(const AdaptersArgs& a, hipStream_t stream);
+hipError_t launch_adapters_backward(const AdaptersArgs& a, hipStream_t stream);
+
+}  // namespace xs

@@ -1,0 +1,180 @@
+// The (token, rank) pairs of a routing in expert order: sorted by expert, ties by pair.
+//
+// A stable counting sort: the row of a pair is the number of pairs of lower experts plus the number
+// of earlier pairs of its own.  A wave takes a run of consecutive pairs, 64 at a time; the
+// lanes that hold the same expert find each other by one ballot for each bit of the id, so that
+// a lane's place among them is a count of lower lanes and nothing depends on the order of
+// atomics.  One workgroup sorts up to kOrderOne pairs in one launch; more go in two: the counts
+// of each workgroup's part, then every workgroup sums the parts before its own.
+//
+// A call reads and writes 12 bytes a pair, 1.6 MB at 131072 pairs: the launches and the waves'
+// chains over their runs bound it.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "groups.h"
+#include "wave.h"
+
+namespace xs {
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+
+// The lanes whose key (of `bits` bits) is this lane's.
+__device__ __forceinline__ uint64_t same_key(int key, int bits) {
+  uint64_t m = ~0ull;
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (key >> b) & 1;
+    const uint64_t s = __ballot(one);
+    m &= one ? s : ~s;
+  }
+  return m;
+}
+
+__device__ __forceinline__ int lower_lanes(uint64_t m) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32),
+                                   __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+
+// Pairs first .. first + len - 1 of the workgroup, dealt to its waves in runs: next[w][e] becomes
+// the row of the first pair of expert e in run w.  before: per expert, the pairs of earlier
+// workgroups (already added to the experts' first rows), or null.
+struct Runs {
+  int first, last, step;       // of this wave
+  __device__ __forceinline__ Runs(int begin, int end, int wave) {
+    step = ((end - begin + kWaves - 1) / kWaves + 63) / 64 * 64;
+    first = min(begin + wave * step, end);
+    last = min(first + step, end);
+  }
+};
+
+__device__ __forceinline__ int key_of(const OrderArgs& a, int i, int end) {
+  const int id = i < end ? a.ids[i] : -1;
+  return (unsigned)id < (unsigned)a.E ? id : a.E;      // E: no expert
+}
+
+// Per expert and wave the number of pairs in the wave's run.
+__device__ __forceinline__ void count_runs(const OrderArgs& a, const Runs& run, int* mine,
+                                           int lane) {
+  for (int e = lane; e < a.E; e += 64) mine[e] = 0;
+  for (int i = run.first; i < run.last; i += 64) {
+    const int key = key_of(a, i + lane, run.last);
+    if (key < a.E) atomicAdd(&mine[key], 1);           // (sums of ones: in any order)
+  }
+}
+
+// Exclusive sum of v over the threads of the workgroup; `total` the sum of all.
+__device__ __forceinline__ int block_scan(int v, int* part, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int upto = wave_scan(v);
+  if (lane == 63) part[wave] = upto;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    before += w < wave ? part[w] : 0;
+    total += part[w];
+  }
+  __syncthreads();
+  return before + upto - v;
+}
+
+// Places the wave's run; next[e]: the row of its next pair of expert e.
+__device__ __forceinline__ void place_runs(const OrderArgs& a, const Runs& run, int* next, int bits,
+                                           int lane) {
+  for (int i = run.first; i < run.last; i += 64) {
+    const int p = i + lane;
+    const int key = key_of(a, p, run.last);
+    const uint64_t same = same_key(key, bits);
+    const int rank = lower_lanes(same);
+    const bool live = key < a.E;
+    const int row = live ? next[key] + rank : -1;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // all lanes read before one writes
+    __builtin_amdgcn_wave_barrier();
+    if (live && rank == 0) next[key] = row + __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (p < run.last) a.rows[p] = row;
+    if (live) a.pair_of[row] = p;
+  }
+}
+
+// The whole sort (kParts false), or the second launch of two: part blockIdx.x of the pairs, whose
+// counts[part][e] the first launch wrote.
+template <bool kParts>
+__global__ __launch_bounds__(kThreads) void order_kernel(OrderArgs a, int part_size, int bits) {
+  extern __shared__ int lds[];                         // [kWaves][E] and [kWaves]
+  int* const part = lds + kWaves * a.E;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int begin = kParts ? blockIdx.x * part_size : 0;
+  const int end = kParts ? min(begin + part_size, a.pairs) : a.pairs;
+  const Runs run(begin, end, wave);
+  int* const mine = lds + wave * a.E;
+  count_runs(a, run, mine, lane);
+  // thread e: expert e's pairs in all parts and in those before this one
+  int all = 0, before = 0;
+  if (kParts && tid < a.E) {
+    const int parts = gridDim.x;
+#pragma unroll 8
+    for (int b = 0; b < parts; ++b) {
+      const int c = a.counts[(size_t)b * a.E + tid];
+      all += c;
+      before += b < (int)blockIdx.x ? c : 0;
+    }
+  }
+  __syncthreads();
+  if (!kParts && tid < a.E)
+    for (int w = 0; w < kWaves; ++w) all += lds[w * a.E + tid];
+  int total;
+  const int first = block_scan(tid < a.E ? all : 0, part, total);
+  if (tid < a.E) {
+    int at = first + before;
+    for (int w = 0; w < kWaves; ++w) {
+      const int c = lds[w * a.E + tid];
+      lds[w * a.E + tid] = at;
+      at += c;
+    }
+    if (!kParts || blockIdx.x == 0) a.offsets[tid] = first;
+  }
+  if (tid == 0 && (!kParts || blockIdx.x == 0)) a.offsets[a.E] = total;
+  __syncthreads();
+  place_runs(a, run, mine, bits, lane);
+  // rows past the last expert's hold no pair
+  for (int p = max(total, begin) + tid; p < end; p += kThreads) a.pair_of[p] = -1;
+}
+
+__global__ __launch_bounds__(kThreads) void order_count_kernel(OrderArgs a, int part_size) {
+  extern __shared__ int lds[];                         // [E]
+  const int begin = blockIdx.x * part_size, end = min(begin + part_size, a.pairs);
+  for (int e = threadIdx.x; e < a.E; e += kThreads) lds[e] = 0;
+  __syncthreads();
+  for (int i = begin + threadIdx.x; i < end; i += kThreads) {
+    const int key = key_of(a, i, end);
+    if (key < a.E) atomicAdd(&lds[key], 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += kThreads)
+    a.counts[(size_t)blockIdx.x * a.E + e] = lds[e];
+}
+
+}  // namespace
+
+hipError_t launch_order(const OrderArgs& a, hipStream_t stream) {
+  int bits = 1;
+  while ((1 << bits) <= a.E) ++bits;                   // keys 0 .. E
+  const size_t lds = sizeof(int) * (size_t(kWaves) * a.E + kWaves);
+  const int parts = order_parts(a.pairs);
+  const auto kernel = parts ? order_kernel<true> : order_kernel<false>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  if (parts)
+    order_count_kernel<<<parts, kThreads, sizeof(int) * a.E, stream>>>(a, kOrderPart);
+  kernel<<<parts ? parts : 1, kThreads, lds, stream>>>(a, kOrderPart, bits);
+  return hipGetLastError();
+}
+
+}  // namespace xs

@@ -47,6 +47,17 @@ __device__ __forceinline__ uint32_t wave_min(uint32_t v) {
   return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
+// Inclusive sum over the lanes of a wave.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += (int)dpp<0x111, 0xF, 0u>((uint32_t)v);   // row_shr:1
+  v += (int)dpp<0x112, 0xF, 0u>((uint32_t)v);
+  v += (int)dpp<0x114, 0xF, 0u>((uint32_t)v);
+  v += (int)dpp<0x118, 0xF, 0u>((uint32_t)v);
+  v += (int)dpp<0x142, 0xA, 0u>((uint32_t)v);   // row_bcast:15
+  v += (int)dpp<0x143, 0xC, 0u>((uint32_t)v);   // row_bcast:31
+  return v;
+}
+
 // Wave-wide sum and maximum of a float, in the same steps.
 template <int Ctrl, int RowMask>
 __device__ __forceinline__ float dpp_or(float old, float v) {

@@ -159,8 +159,27 @@ class BlockExpertsArgs(ctypes.Structure):
     ]
 
 
+class AdaptersArgs(ctypes.Structure):
+    """xshare_adapters_args (include/xshare.h)."""
+    _fields_ = [
+        ("struct_size", ctypes.c_size_t),
+        ("T", ctypes.c_int32), ("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32),
+        ("n", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+        ("a", ctypes.c_void_p), ("b", ctypes.c_void_p),
+        ("ids", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+        ("base", ctypes.c_void_p), ("ld_base", ctypes.c_int64),
+        ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64),
+        ("dy", ctypes.c_void_p), ("lddy", ctypes.c_int64),
+        ("da", ctypes.c_void_p), ("db", ctypes.c_void_p),
+        ("ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
 WEIGHTS = {"bf16": 0, "fp8": 1, "mxfp4": 2}
 _EXPERTS_ARGS_BYTES = ctypes.sizeof(BlockExpertsArgs)
+_ADAPTERS_ARGS_BYTES = ctypes.sizeof(AdaptersArgs)
 GATE = {"softmax": 0, "sigmoid": 1}
 GROUP = {"max": 0, "top2": 1}
 
@@ -263,6 +282,28 @@ def lib() -> ctypes.CDLL:
         L.xshare_block_experts_workspace_bytes.restype = _SZ
         L.xshare_block_experts.argtypes = [ctypes.POINTER(BlockExpertsArgs)]
         L.xshare_block_experts.restype = ctypes.c_int
+        L.xshare_expert_order_workspace_bytes.argtypes = [_I32, _I32, _I32]
+        L.xshare_expert_order_workspace_bytes.restype = _SZ
+        L.xshare_expert_order.argtypes = [_P, _I32, _I32, _I32, _P, _P, _P, _P, _SZ, _P]
+        L.xshare_expert_order.restype = ctypes.c_int
+        L.xshare_dispatch.argtypes = [_P, _I64, _I32, _I32, _I32, _I32, _P, _P, _I64, _P]
+        L.xshare_dispatch.restype = ctypes.c_int
+        L.xshare_combine.argtypes = [_P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _I64, _P]
+        L.xshare_combine.restype = ctypes.c_int
+        L.xshare_combine_backward.argtypes = [_P, _I64, _P, _I64, _I32, _I32, _I32, _I32, _P, _P,
+                                              _P, _I64, _P, _P]
+        L.xshare_combine_backward.restype = ctypes.c_int
+        for call in (L.xshare_grouped_linear, L.xshare_grouped_linear_backward_x):
+            call.argtypes = [_P, _I64, _P, _P, _I32, _I32, _I32, _I32, _P, _I64, _P]
+            call.restype = ctypes.c_int
+        L.xshare_grouped_linear_backward_w.argtypes = [_P, _I64, _P, _I64, _P, _I32, _I32, _I32,
+                                                       _I32, _P, _I32, _I32, _P]
+        L.xshare_grouped_linear_backward_w.restype = ctypes.c_int
+        L.xshare_adapters_workspace_bytes.argtypes = [_I32] * 6
+        L.xshare_adapters_workspace_bytes.restype = _SZ
+        for call in (L.xshare_adapters, L.xshare_adapters_backward):
+            call.argtypes = [ctypes.POINTER(AdaptersArgs)]
+            call.restype = ctypes.c_int
         L.xshare_probe_stream_read.argtypes = [_P, _SZ, _I32, _I32, _P, _P]
         L.xshare_probe_stream_read.restype = ctypes.c_int
         L.xshare_block_times.argtypes = [_P, _P, _P, _I32, _P]
@@ -1229,6 +1270,334 @@ def block_experts(x: torch.Tensor, ids: torch.Tensor, w: torch.Tensor, q1: torch
                          _stream_of(x, stream))
     _check(L.xshare_block_experts(ctypes.byref(a)), "xshare_block_experts")
     return y
+
+
+# ------------------------- tokens in expert order, products of groups of rows, adapters
+
+def _movable(t, name):
+    """The library's type and the row stride of a bf16 or fp32 matrix."""
+    dtype = t.dtype if isinstance(t, torch.Tensor) else None
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise ValueError(f"{name} must be a float32 or bfloat16 GPU tensor")
+    return int(dtype is torch.bfloat16), _rows(t, dtype, name)
+
+
+def _order_rows(order, device):
+    """rows [T, k] of an expert order, checked, and T, k."""
+    rows = order["rows"]
+    if rows.dim() != 2:
+        raise ValueError("an order's rows are [T, k]")
+    T, k = rows.shape
+    _fit(device, (rows, torch.int32, (T, k), "order's rows"))
+    return rows, T, k
+
+
+def _matrix_out(t, like, shape, name):
+    """A given output or a new one of shape, of like's type and device; and its row stride."""
+    if t is None:
+        return like.new_empty(shape), shape[1]
+    ld = _rows(t, like.dtype, name, shape[1])
+    _on(like.device, t, name)
+    if t.shape[0] != shape[0]:
+        raise ValueError(f"{name} must have {shape[0]} rows, got {t.shape[0]}")
+    return t, ld
+
+
+def _matrix_in(t, like, shape, name):
+    """The row stride of an input of shape, of like's type and device."""
+    ld = _rows(t, like.dtype, name, shape[1])
+    _on(like.device, t, name)
+    if t.shape[0] != shape[0]:
+        raise ValueError(f"{name} must have {shape[0]} rows, got {t.shape[0]}")
+    return ld
+
+
+def expert_order_workspace_bytes(T: int, top_k: int, n_experts: int) -> int:
+    T, k, N = int(T), int(top_k), int(n_experts)
+    if _past_32_bits(T | k | N):
+        return 0
+    return int(lib().xshare_expert_order_workspace_bytes(T, k, N))
+
+
+@_placed
+def expert_order(ids: torch.Tensor, n_experts: int, *, out=None, workspace=None,
+                 stream=None) -> dict:
+    """The (token, rank) pairs of ids [T, k] (``gate``'s or a set selection's) sorted by expert, ties
+    by pair: dict(offsets int32 [n_experts + 1], each expert's first row; rows int32 [T, k], each
+    pair's row; pairs int32 [T k], each row's pair t k + r).  A pair whose id is not in
+    [0, n_experts) has row -1; pairs is -1 from offsets[n_experts] on."""
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise ValueError("ids are [T, k]")
+    T, k = ids.shape
+    N, dev, L = int(n_experts), ids.device, lib()
+    if (T | k | N) >> 31:
+        _sizes(T | k | N, "xshare_expert_order")
+    _dev(ids, torch.int32, (T, k), "ids")
+    out = {} if out is None else out
+    res = dict(offsets=out.get("offsets"), rows=out.get("rows"), pairs=out.get("pairs"))
+    for name, shape in (("offsets", (max(N, 0) + 1,)), ("rows", (T, k)), ("pairs", (T * k,))):
+        if res[name] is None:
+            res[name] = ids.new_empty(shape)
+        else:
+            _fit(dev, (res[name], torch.int32, shape, name))
+    if workspace is None:
+        size = L.xshare_expert_order_workspace_bytes(T, k, N)
+        workspace = ids.new_empty(size, dtype=torch.uint8)
+    else:
+        size = _workspace(dev, workspace)
+    st = L.xshare_expert_order(ids.data_ptr(), T, k, N, res["offsets"].data_ptr(),
+                               res["rows"].data_ptr(), res["pairs"].data_ptr(),
+                               workspace.data_ptr(), size, _stream_of(ids, stream))
+    _check(st, "xshare_expert_order")
+    return res
+
+
+@_placed
+def dispatch(x: torch.Tensor, order: dict, *, out=None, stream=None) -> torch.Tensor:
+    """x [T, d] (bf16 or fp32) in the order of ``expert_order``: [T k, d], row rows[t, r] is x[t].
+    Rows from offsets[n_experts] on are left as they were (``out``) or hold nothing.  Records no
+    gradient (``dispatch_backward`` gives x's)."""
+    dtype, ldx = _movable(x, "x")
+    rows, T, k = _order_rows(order, x.device)
+    d = x.shape[1]
+    if (T | k | d) >> 31:
+        _sizes(T | k | d, "xshare_dispatch")
+    if x.shape[0] != T:
+        raise ValueError(f"x must have {T} rows, got {x.shape[0]}")
+    if x.requires_grad:
+        _no_gradient(x, "x", "dispatch_backward gives it")
+    out, ldo = _matrix_out(out, x, (T * k, d), "out")
+    st = lib().xshare_dispatch(x.data_ptr(), ldx, dtype, T, k, d, rows.data_ptr(), out.data_ptr(),
+                               ldo, _stream_of(x, stream))
+    _check(st, "xshare_dispatch")
+    return out
+
+
+def _combine(src, w, order, out, stream, name):
+    dtype, ld = _movable(src, name)
+    rows, T, k = _order_rows(order, src.device)
+    d = src.shape[1]
+    if (T | k | d) >> 31:
+        _sizes(T | k | d, "xshare_combine")
+    if src.shape[0] != T * k:
+        raise ValueError(f"{name} must have {T * k} rows, got {src.shape[0]}")
+    if w is not None:
+        _fit(src.device, (w, torch.float32, (T, k), "w"))
+    y, ldy = _matrix_out(out, src, (T, d), "out")
+    st = lib().xshare_combine(src.data_ptr(), ld, dtype, T, k, d, rows.data_ptr(),
+                              None if w is None else w.data_ptr(), y.data_ptr(), ldy,
+                              _stream_of(src, stream))
+    _check(st, "xshare_combine")
+    return y
+
+
+@_placed
+def dispatch_backward(drows: torch.Tensor, order: dict, *, out=None, stream=None) -> torch.Tensor:
+    """The gradient of ``dispatch``'s x [T, d] from that of its rows [T k, d]: each token's rows,
+    summed in fp32 and rounded once."""
+    return _combine(drows, None, order, out, stream, "drows")
+
+
+@_placed
+def combine(rows: torch.Tensor, w: torch.Tensor, order: dict, *, out=None,
+            stream=None) -> torch.Tensor:
+    """y[t] = sum_r w[t, r] rows[order rows[t, r]] ([T, d], in rows' type, bf16 or fp32), w fp32
+    [T, k]; pairs without a row add nothing.  Records no gradient (``combine_backward``)."""
+    if w is None:
+        raise ValueError("w must be a GPU tensor")
+    if rows.requires_grad or w.requires_grad:
+        _no_gradient(rows, "rows", "combine_backward gives it")
+        _no_gradient(w, "w", "combine_backward gives it")
+    return _combine(rows, w, order, out, stream, "rows")
+
+
+@_placed
+def combine_backward(dy: torch.Tensor, rows: torch.Tensor, w: torch.Tensor, order: dict, *, out=None,
+                     stream=None) -> dict:
+    """The gradients of ``combine`` from dy [T, d]: dict(drows [T k, d], dw fp32 [T, k]).  drows
+    outside the order's rows is left as it was (``out``) or holds nothing; dw is 0 there."""
+    dtype, lddy = _movable(dy, "dy")
+    at, T, k = _order_rows(order, dy.device)
+    d = dy.shape[1]
+    if (T | k | d) >> 31:
+        _sizes(T | k | d, "xshare_combine_backward")
+    if dy.shape[0] != T:
+        raise ValueError(f"dy must have {T} rows, got {dy.shape[0]}")
+    ld = _matrix_in(rows, dy, (T * k, d), "rows")
+    _fit(dy.device, (w, torch.float32, (T, k), "w"))
+    drows, dw = (None, None) if out is None else (out.get("drows"), out.get("dw"))
+    drows, ldd = _matrix_out(drows, dy, (T * k, d), "drows")
+    if dw is None:
+        dw = w.new_empty((T, k))
+    else:
+        _fit(dy.device, (dw, torch.float32, (T, k), "dw"))
+    st = lib().xshare_combine_backward(dy.data_ptr(), lddy, rows.data_ptr(), ld, dtype, T, k, d,
+                                       at.data_ptr(), w.data_ptr(), drows.data_ptr(), ldd,
+                                       dw.data_ptr(), _stream_of(dy, stream))
+    _check(st, "xshare_combine_backward")
+    return dict(drows=drows, dw=dw)
+
+
+def _grouped(rows, w, offsets, cols, name, call):
+    """Checks the rows [P, cols'] and weights [E, n, k] of a product of groups: (ld, P, E, n, k)."""
+    if not isinstance(w, torch.Tensor) or w.dim() != 3:
+        raise ValueError("w must be [groups, n, k]")
+    E, n, k = w.shape
+    ld = _rows(rows, torch.bfloat16, name, (n, k)[cols])
+    P = rows.shape[0]
+    if (P | E | n | k) >> 31:
+        _sizes(P | E | n | k, call)
+    _fit(rows.device, (w, torch.bfloat16, (E, n, k), "w"),
+         (offsets, torch.int32, (E + 1,), "offsets"))
+    return ld, P, E, n, k
+
+
+@_placed
+def grouped_linear(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, *, y=None,
+                   stream=None) -> torch.Tensor:
+    """y_p = W_e x_p (bf16 [P, n]) for the rows p = offsets[e] .. offsets[e + 1] - 1 of each group e
+    (int32 [E + 1], as ``expert_order`` gives them), W bf16 [E, n, k], n and k multiples of 8.  Rows
+    of no group are left as they were (``y``) or hold nothing.  Records no gradient:
+    ``grouped_linear_backward_x`` and ``_w`` give them."""
+    ldx, P, E, n, k = _grouped(x, w, offsets, 1, "x", "xshare_grouped_linear")
+    if x.requires_grad or w.requires_grad:
+        _no_gradient(x, "x", "grouped_linear_backward_x gives it")
+        _no_gradient(w, "w", "grouped_linear_backward_w gives it")
+    y, ldy = _matrix_out(y, x, (P, n), "y")
+    st = lib().xshare_grouped_linear(x.data_ptr(), ldx, w.data_ptr(), offsets.data_ptr(), P, E, n, k,
+                                     y.data_ptr(), ldy, _stream_of(x, stream))
+    _check(st, "xshare_grouped_linear")
+    return y
+
+
+@_placed
+def grouped_linear_backward_x(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, *, out=None,
+                              stream=None) -> torch.Tensor:
+    """The gradient of ``grouped_linear``'s x: dx_p = W_e^T dy_p (bf16 [P, k])."""
+    lddy, P, E, n, k = _grouped(dy, w, offsets, 0, "dy", "xshare_grouped_linear_backward_x")
+    out, ldo = _matrix_out(out, dy, (P, k), "out")
+    st = lib().xshare_grouped_linear_backward_x(dy.data_ptr(), lddy, w.data_ptr(),
+                                                offsets.data_ptr(), P, E, n, k, out.data_ptr(), ldo,
+                                                _stream_of(dy, stream))
+    _check(st, "xshare_grouped_linear_backward_x")
+    return out
+
+
+@_placed
+def grouped_linear_backward_w(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, *, out=None,
+                              accumulate: bool = False, stream=None) -> torch.Tensor:
+    """The gradient of ``grouped_linear``'s weights: dW_e = sum over the group's rows of
+    dy_p x_p^T, fp32 [E, n, k] (or of ``out``'s type, fp32 or bf16); zeros for a group without
+    rows.  ``accumulate``: added to an fp32 ``out`` instead."""
+    lddy = _rows(dy, torch.bfloat16, "dy")
+    ldx = _rows(x, torch.bfloat16, "x")
+    P, n = dy.shape
+    k = x.shape[1]
+    E = offsets.shape[0] - 1 if offsets.dim() == 1 else -1
+    if (P | n | k | E) >> 31:
+        _sizes(P | n | k | E, "xshare_grouped_linear_backward_w")
+    if x.shape[0] != P:
+        raise ValueError(f"x must have {P} rows, got {x.shape[0]}")
+    _on(dy.device, x, "x")
+    _fit(dy.device, (offsets, torch.int32, (E + 1,), "offsets"))
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs an out to add to")
+        out = dy.new_empty((max(E, 0), n, k), dtype=torch.float32)
+    elif out.dtype is torch.float32 or out.dtype is torch.bfloat16:
+        _fit(dy.device, (out, out.dtype, (E, n, k), "out"))
+    else:
+        raise ValueError("out must be float32 or bfloat16")
+    st = lib().xshare_grouped_linear_backward_w(
+        dy.data_ptr(), lddy, x.data_ptr(), ldx, offsets.data_ptr(), P, E, n, k, out.data_ptr(),
+        int(out.dtype is torch.bfloat16), int(bool(accumulate)), _stream_of(dy, stream))
+    _check(st, "xshare_grouped_linear_backward_w")
+    return out
+
+
+def adapters_workspace_bytes(T: int, n_adapters: int, rank: int, n: int, d: int,
+                             backward: bool = False) -> int:
+    T, N, r, n, d = int(T), int(n_adapters), int(rank), int(n), int(d)
+    if _past_32_bits(T | N | r | n | d):
+        return 0
+    return int(lib().xshare_adapters_workspace_bytes(T, N, r, n, d, int(bool(backward))))
+
+
+def _adapters_args(x, a, b, ids, scales, base, out, workspace, stream, backward):
+    """The arguments that both directions share, and the tensor that they write."""
+    if a.dim() != 3 or b.dim() != 3:
+        raise ValueError("a is [adapters, rank, d], b [adapters, n, rank]")
+    N, r, d = a.shape
+    n = b.shape[1]
+    ldx = _rows(x, torch.bfloat16, "x", d)
+    T, dev, L = x.shape[0], x.device, lib()
+    call = "xshare_adapters_backward" if backward else "xshare_adapters"
+    if (T | N | r | n | d) >> 31:
+        _sizes(T | N | r | n | d, call)
+    _fit(dev, (a, torch.bfloat16, (N, r, d), "a"), (b, torch.bfloat16, (N, n, r), "b"),
+         (ids, torch.int32, (T,), "ids"))
+    if scales is not None:
+        _fit(dev, (scales, torch.float32, (N,), "scales"))
+    shape = (T, d if backward else n)
+    ld_base = 0 if base is None else _matrix_in(base, x, shape, "base")
+    out, ld_out = _matrix_out(out, x, shape, "out")
+    if workspace is None:
+        size = L.xshare_adapters_workspace_bytes(T, N, r, n, d, int(backward))
+        workspace = x.new_empty(size, dtype=torch.uint8)
+    else:
+        size = _workspace(dev, workspace)
+    p = AdaptersArgs(_ADAPTERS_ARGS_BYTES, T, N, r, n, d, x.data_ptr(), ldx, a.data_ptr(),
+                     b.data_ptr(), ids.data_ptr(), None if scales is None else scales.data_ptr(),
+                     None if base is None else base.data_ptr(), ld_base, out.data_ptr(), ld_out,
+                     None, 0, None, None, workspace.data_ptr(), size, _stream_of(x, stream))
+    return p, out, workspace
+
+
+@_placed
+def adapters(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor, *, scales=None,
+             base=None, out=None, workspace=None, stream=None) -> torch.Tensor:
+    """Low-rank adapters beside a shared projection: base_t + scales[e] B_e A_e x_t for e = ids[t]
+    (bf16 [T, n]); base_t for a token whose id is not in [0, adapters).  x bf16 [T, d], a bf16
+    [adapters, rank, d], b bf16 [adapters, n, rank], ids int32 [T], scales fp32 [adapters] (none: 1),
+    base bf16 [T, n] (none: 0), such as ``block_linear``'s y; ``out`` may be base.  rank, n and d
+    are multiples of 8, rank at most 128.  Records no gradient (``adapters_backward``)."""
+    if x.requires_grad or a.requires_grad or b.requires_grad \
+            or (base is not None and base.requires_grad):
+        _no_gradient(x, "x", "adapters_backward gives it")
+        _no_gradient(a, "a", "adapters_backward gives it")
+        _no_gradient(b, "b", "adapters_backward gives it")
+        if base is not None:
+            _no_gradient(base, "base", "it is that of what adapters returns")
+    if scales is not None and scales.requires_grad:
+        _no_gradient(scales, "scales", "there is no call for it")
+    p, out, _ws = _adapters_args(x, a, b, ids, scales, base, out, workspace, stream, False)
+    _check(lib().xshare_adapters(ctypes.byref(p)), "xshare_adapters")
+    return out
+
+
+@_placed
+def adapters_backward(dy: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                      ids: torch.Tensor, *, scales=None, base=None, out=None, workspace=None,
+                      stream=None) -> dict:
+    """The gradients of ``adapters`` from dy [T, n]: dict(dx bf16 [T, d], da fp32 [adapters, rank, d],
+    db fp32 [adapters, n, rank]).  ``base`` [T, d]: what dx is added to (the shared projection's
+    part; ``out["dx"]`` may be it); zeros in da and db for adapters without tokens."""
+    dx, da, db = (None, None, None) if out is None else (out.get("dx"), out.get("da"),
+                                                         out.get("db"))
+    p, dx, _ws = _adapters_args(x, a, b, ids, scales, base, dx, workspace, stream, True)
+    p.lddy = _matrix_in(dy, x, (x.shape[0], b.shape[1]), "dy")
+    p.dy = dy.data_ptr()
+    if da is None:
+        da = x.new_empty(a.shape, dtype=torch.float32)
+    else:
+        _fit(x.device, (da, torch.float32, a.shape, "da"))
+    if db is None:
+        db = x.new_empty(b.shape, dtype=torch.float32)
+    else:
+        _fit(x.device, (db, torch.float32, b.shape, "db"))
+    p.da, p.db = da.data_ptr(), db.data_ptr()
+    _check(lib().xshare_adapters_backward(ctypes.byref(p)), "xshare_adapters_backward")
+    return dict(dx=dx, da=da, db=db)
 
 
 @_placed
