@@ -79,7 +79,8 @@ hipError_t launch_grouped_backward_w(const GroupedArgs& a, hipStream_t stream);
 
 // Tokens up to which an adapters call goes token by token in two launches, without an order.
 constexpr int kAdapterFew = 64;
-inline int rank16(int r) { return (r + 15) / 16 * 16; }
+// Values of a row of h: the ranks of the kernels' instances, which have 1, 2, 4 or 8 tiles of 16.
+inline int padded_rank(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
 
 // Parts that the rows of an adapter are summed in for its factors' gradients.
 constexpr int kGradColumns = 128;      // columns of x or dy of a workgroup
@@ -94,7 +95,7 @@ inline int adapter_splits(int T, int L, int n, int d) {
 struct AdaptersLayout {
   size_t offsets, rows, tokens;  // the tokens in adapters' order
   size_t counts;                 // of the sort
-  size_t h, dh;                  // bf16 [T, 3, rank16]: A x and s B^T dy, as three parts that sum up
+  size_t h, dh;                  // bf16 [T, 3, padded_rank]: A x and s B^T dy, as three parts that sum up
   size_t at, bt;                 // [L, d, r] and [L, r, n]: the factors transposed (backward)
   size_t part;                   // fp32 [splits, L (n + d) r] where splits > 1 (backward)
   size_t total;
@@ -106,11 +107,11 @@ inline AdaptersLayout adapters_layout(int T, int L, int r, int n, int d, bool ba
   A.rows = o;    o += align256(sizeof(int32_t) * size_t(T));
   A.tokens = o;  o += align256(sizeof(int32_t) * size_t(T));
   A.counts = o;  o += order_bytes(T, L);
-  A.h = o;       o += align256(6 * size_t(T) * rank16(r));
+  A.h = o;       o += align256(6 * size_t(T) * padded_rank(r));
   A.dh = o;
   A.at = A.bt = A.part = o;
   if (backward) {
-    o += align256(6 * size_t(T) * rank16(r));
+    o += align256(6 * size_t(T) * padded_rank(r));
     A.at = o;    o += align256(2 * size_t(L) * d * r);
     A.bt = o;    o += align256(2 * size_t(L) * n * r);
     A.part = o;

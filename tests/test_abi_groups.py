@@ -148,6 +148,14 @@ def test_workspaces_serve_smaller_batches():
     o = [X.expert_order_workspace_bytes(T, 8, 300) for T in range(0, 9000, 37)]
     for sizes in (a, o):
         assert all(s > 0 and s % 256 == 0 for s in sizes) and sizes == sorted(sizes)
+    # h and dh: three bf16 parts of 16, 32, 64 or 128 ranks a token
+    for r, wide in ((8, 16), (24, 32), (40, 64), (72, 128), (104, 128)):
+        T = 1 << 16
+        big, small = (X.adapters_workspace_bytes(n, 1, r, 64, 64, True) for n in (T, T // 2))
+        order = X.expert_order_workspace_bytes(T, 1, 1) - X.expert_order_workspace_bytes(T // 2, 1, 1)
+        parts = [min(max(768 // 2, 1), -(-n // 256)) for n in (T, T // 2)]
+        assert big - small == 2 * 6 * (T // 2) * wide + 8 * (T // 2) + order \
+            + 4 * r * 128 * (parts[0] - parts[1])
     assert X.adapters_workspace_bytes(8, 5, 12, 400, 4096) == 0
     assert X.expert_order_workspace_bytes(8, 33, 300) == 0
     assert X.adapters_workspace_bytes(PAST, 5, 16, 400, 4096) == 0

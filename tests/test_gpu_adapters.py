@@ -137,3 +137,22 @@ def test_one_workspace_and_the_same_bits_again():
             assert torch.equal(y[i], y[0])
             for name in ("dx", "da", "db"):
                 assert torch.equal(g[i][name], g[0][name]), name
+
+
+@pytest.mark.parametrize("r", [8, 24, 40, 48, 56, 72, 96, 104, 112, 120])
+def test_ranks_between_the_tiles_with_every_row_used(r):
+    from paper_2602_07265_amd import xshare as X
+    T, L, n, d = 257, 2, 136, 72
+    c = _case(T, L, r, n, d, r, none=0.0)
+    need = X.adapters_workspace_bytes(T, L, r, n, d, True)
+    ws = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    args = (c["x"], c["a"], c["b"], c["ids"])
+    y = X.adapters(*args, base=c["base"], workspace=ws[:need])
+    got = X.adapters_backward(c["dy"], *args, workspace=ws[:need])
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0xA5).all()
+    within(y, *OG.adapters(*args, None, c["base"]), adapter_rel(r, d), "y")
+    ref, mag = OG.adapters_backward(c["dy"], *args, None, None)
+    within(got["dx"], ref["dx"], mag["dx"], adapter_rel(r, n), "dx")
+    within(got["da"], ref["da"], mag["da"], factor_rel(T, n), "da")
+    within(got["db"], ref["db"], mag["db"], factor_rel(T, d), "db")
