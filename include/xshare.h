@@ -789,28 +789,34 @@ xshare_status xshare_combine_backward(const void* dy, int64_t lddy, const void* 
                                       const int32_t* rows, const float* w, void* dsrc,
                                       int64_t ld_dsrc, float* dw, hipStream_t stream);
 
+/* Workspace of xshare_grouped_linear and of both of its gradients (bytes, 256-aligned); 0 where they
+ * need none (fewer than 256 rows) and for invalid sizes.  That of P rows serves any fewer too. */
+size_t xshare_grouped_linear_workspace_bytes(int32_t P, int32_t n_groups, int32_t n, int32_t k);
+
 /*
  * xshare_grouped_linear -- y_p = W_e x_p for the rows p of each group e, in bf16 with fp32 sums,
  * rounded once.
  *
  *   x        [P, k] bf16, rows ldx elements apart; 16-byte aligned, ldx >= k a multiple of 8, at
- *            most 2^23 (so is the distance of every matrix of rows here).
+ *            most 2^22 (so is the distance of every matrix of rows here).
  *   w        [n_groups, n, k] bf16, 16-byte aligned; n and k multiples of 8.
  *   offsets  DEVICE [n_groups + 1] int32, not decreasing, offsets[0] >= 0 and
  *            offsets[n_groups] <= P: group e's rows are offsets[e] .. offsets[e + 1] - 1
  *            (as xshare_expert_order writes them).  What is not so gives unspecified rows.
  *   y        out [P, n] bf16, rows ldy >= n elements apart, ldy a multiple of 8, 16-byte aligned.
  *            Rows outside the groups are left as they were, and x's are not read.
+ *   ws       of xshare_grouped_linear_workspace_bytes, 16-byte aligned; may be NULL where that is 0.
  */
 xshare_status xshare_grouped_linear(const uint16_t* x, int64_t ldx, const uint16_t* w,
                                     const int32_t* offsets, int32_t P, int32_t n_groups, int32_t n,
-                                    int32_t k, uint16_t* y, int64_t ldy, hipStream_t stream);
+                                    int32_t k, uint16_t* y, int64_t ldy, void* ws,
+                                    size_t ws_bytes, hipStream_t stream);
 
 /* xshare_grouped_linear_backward_x -- dx_p = W_e^T dy_p; dy [P, n] and dx [P, k] as y and x there. */
 xshare_status xshare_grouped_linear_backward_x(const uint16_t* dy, int64_t lddy, const uint16_t* w,
                                                const int32_t* offsets, int32_t P, int32_t n_groups,
                                                int32_t n, int32_t k, uint16_t* dx, int64_t lddx,
-                                               hipStream_t stream);
+                                               void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
  * xshare_grouped_linear_backward_w -- dW_e = sum over the group's rows of dy_p x_p^T.
@@ -822,8 +828,8 @@ xshare_status xshare_grouped_linear_backward_x(const uint16_t* dy, int64_t lddy,
 xshare_status xshare_grouped_linear_backward_w(const uint16_t* dy, int64_t lddy, const uint16_t* x,
                                                int64_t ldx, const int32_t* offsets, int32_t P,
                                                int32_t n_groups, int32_t n, int32_t k, void* dw,
-                                               int32_t dw_dtype, int32_t accumulate,
-                                               hipStream_t stream);
+                                               int32_t dw_dtype, int32_t accumulate, void* ws,
+                                               size_t ws_bytes, hipStream_t stream);
 
 /*
  * Arguments of xshare_adapters and xshare_adapters_backward.  Zero-initialise, set struct_size,

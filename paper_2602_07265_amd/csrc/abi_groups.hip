@@ -69,10 +69,18 @@ xshare_status check_grouped(int32_t P, int32_t E, int32_t n, int32_t k) {
 }
 
 // Rows further apart than this would not fit the kernels' 32-bit offsets within a tile.
-constexpr int64_t kMaxRowStride = 1 << 23;
+constexpr int64_t kMaxRowStride = 1 << 22;
 
-xs::GroupedArgs grouped_args(int32_t P, int32_t E, int32_t n, int32_t k, const int32_t* offsets) {
+xshare_status check_sums(int32_t P, const void* ws, size_t ws_bytes) {
+  const size_t need = xs::grouped_bytes(P);
+  if (need > 0 && (!ws || ws_bytes < need)) return XSHARE_EWORKSPACE;
+  return need > 0 && !aligned(ws, 16) ? XSHARE_EINVAL : XSHARE_OK;
+}
+
+xs::GroupedArgs grouped_args(int32_t P, int32_t E, int32_t n, int32_t k, const int32_t* offsets,
+                             void* ws) {
   xs::GroupedArgs a{};
+  a.sums = xs::grouped_bytes(P) > 0 ? at<float>(ws, 0) : nullptr;
   a.P = P;
   a.E = E;
   a.n = n;
@@ -225,14 +233,16 @@ xshare_status xshare_combine_backward(const void* dy, int64_t lddy, const void* 
 
 xshare_status xshare_grouped_linear(const uint16_t* x, int64_t ldx, const uint16_t* w,
                                     const int32_t* offsets, int32_t P, int32_t n_groups, int32_t n,
-                                    int32_t k, uint16_t* y, int64_t ldy, hipStream_t stream) {
+                                    int32_t k, uint16_t* y, int64_t ldy, void* ws,
+                                    size_t ws_bytes, hipStream_t stream) {
   const xshare_status st = check_grouped(P, n_groups, n, k);
   if (st != XSHARE_OK || P == 0) return st;
   if (!valid_matrix(x, ldx, k) || !w || !aligned(w, 16) || !offsets || !aligned(offsets, 4) ||
       !valid_matrix(y, ldy, n))
     return XSHARE_EINVAL;
   if (ldx > kMaxRowStride) return XSHARE_EUNSUPPORTED;
-  xs::GroupedArgs a = grouped_args(P, n_groups, n, k, offsets);
+  if (const xshare_status bad = check_sums(P, ws, ws_bytes)) return bad;
+  xs::GroupedArgs a = grouped_args(P, n_groups, n, k, offsets, ws);
   a.x = x;
   a.ldx = ldx;
   a.w = w;
@@ -244,14 +254,15 @@ xshare_status xshare_grouped_linear(const uint16_t* x, int64_t ldx, const uint16
 xshare_status xshare_grouped_linear_backward_x(const uint16_t* dy, int64_t lddy, const uint16_t* w,
                                                const int32_t* offsets, int32_t P, int32_t n_groups,
                                                int32_t n, int32_t k, uint16_t* dx, int64_t lddx,
-                                               hipStream_t stream) {
+                                               void* ws, size_t ws_bytes, hipStream_t stream) {
   const xshare_status st = check_grouped(P, n_groups, n, k);
   if (st != XSHARE_OK || P == 0) return st;
   if (!valid_matrix(dy, lddy, n) || !w || !aligned(w, 16) || !offsets || !aligned(offsets, 4) ||
       !valid_matrix(dx, lddx, k))
     return XSHARE_EINVAL;
   if (lddy > kMaxRowStride) return XSHARE_EUNSUPPORTED;
-  xs::GroupedArgs a = grouped_args(P, n_groups, n, k, offsets);
+  if (const xshare_status bad = check_sums(P, ws, ws_bytes)) return bad;
+  xs::GroupedArgs a = grouped_args(P, n_groups, n, k, offsets, ws);
   a.dy = dy;
   a.lddy = lddy;
   a.w = w;
@@ -263,15 +274,17 @@ xshare_status xshare_grouped_linear_backward_x(const uint16_t* dy, int64_t lddy,
 xshare_status xshare_grouped_linear_backward_w(const uint16_t* dy, int64_t lddy, const uint16_t* x,
                                                int64_t ldx, const int32_t* offsets, int32_t P,
                                                int32_t n_groups, int32_t n, int32_t k, void* dw,
-                                               int32_t dw_dtype, int32_t accumulate,
-                                               hipStream_t stream) {
+                                               int32_t dw_dtype, int32_t accumulate, void* ws,
+                                               size_t ws_bytes, hipStream_t stream) {
   if (dw_dtype != XSHARE_F32 && dw_dtype != XSHARE_BF16) return XSHARE_EINVAL;
   const xshare_status st = check_grouped(P, n_groups, n, k);
   if (st != XSHARE_OK) return st;
   if (!offsets || !aligned(offsets, 4) || !dw || !aligned(dw, 16)) return XSHARE_EINVAL;
   if (P > 0 && (!valid_matrix(dy, lddy, n) || !valid_matrix(x, ldx, k))) return XSHARE_EINVAL;
-  if (accumulate && dw_dtype != XSHARE_F32) return XSHARE_EUNSUPPORTED;
-  xs::GroupedArgs a = grouped_args(P, n_groups, n, k, offsets);
+  if ((accumulate && dw_dtype != XSHARE_F32) || lddy > kMaxRowStride || ldx > kMaxRowStride)
+    return XSHARE_EUNSUPPORTED;
+  if (const xshare_status bad = check_sums(P, ws, ws_bytes)) return bad;
+  xs::GroupedArgs a = grouped_args(P, n_groups, n, k, offsets, ws);
   a.dy = dy;
   a.lddy = lddy;
   a.x = x;
@@ -280,6 +293,10 @@ xshare_status xshare_grouped_linear_backward_w(const uint16_t* dy, int64_t lddy,
   a.dw_fp32 = dw_dtype == XSHARE_F32;
   a.accumulate = accumulate != 0;
   return status_of(xs::launch_grouped_backward_w(a, stream));
+}
+
+size_t xshare_grouped_linear_workspace_bytes(int32_t P, int32_t n_groups, int32_t n, int32_t k) {
+  return check_grouped(P, n_groups, n, k) == XSHARE_OK ? xs::grouped_bytes(P) : 0;
 }
 
 size_t xshare_adapters_workspace_bytes(int32_t T, int32_t n_adapters, int32_t rank, int32_t n,

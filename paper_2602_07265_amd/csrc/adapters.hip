@@ -147,9 +147,7 @@ __global__ __launch_bounds__(512) void shrink_kernel(Shrink a) {
   const int n = lane & 15, g = lane >> 4;
   Place p;
   if (!find_place(a.offsets, a.L, a.T, 16 * MT, 1, p)) return;
-  const int e = __builtin_amdgcn_readfirstlane(p.e);
-  const int first = __builtin_amdgcn_readfirstlane(p.first);
-  const int live = __builtin_amdgcn_readfirstlane(p.live);
+  const int e = p.e, first = p.first, live = p.live;
   const uint16_t* x[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
@@ -234,10 +232,8 @@ __global__ __launch_bounds__(256) void expand_kernel(Expand a) {
   Place p;
   const int columns = (a.N + kExpandColumns - 1) / kExpandColumns;
   if (!find_place(a.offsets, a.L, a.T, 16 * MT, columns, p)) return;
-  const int e = __builtin_amdgcn_readfirstlane(p.e);
-  const int first = __builtin_amdgcn_readfirstlane(p.first);
-  const int live = __builtin_amdgcn_readfirstlane(p.live);
-  const int c0 = __builtin_amdgcn_readfirstlane(p.column) * kExpandColumns;
+  const int e = p.e, first = p.first, live = p.live;
+  const int c0 = p.column * kExpandColumns;
   long token[MT];
   bf16x8 fh[MT][JT];
 #pragma unroll
@@ -331,14 +327,14 @@ __global__ __launch_bounds__(256) void factors_kernel(Factors a) {
   const uint16_t* const skinny = is_a ? a.dh : a.h;
   const uint16_t* const zeros = reinterpret_cast<const uint16_t*>(kZeros);
 
-  // lane's piece of load j of the wide rows: row j * kStep + tid / 16, columns off[j] ..
-  Wide ow;
-  ow.init(wide + c0, 0, min(kGradColumns, width - c0), 0, tid);
+  // lane's piece of load j of the wide rows: row j * kStep + tid / kPieces, `column` on
   int token[Wide::kLoads];
+  static_assert(Wide::kStep % 16 == 0, "one column for every load");
+  const int column = min(Wide::column(tid, 0), width - c0 - 8);
   auto fetch = [&](int b) {
 #pragma unroll
     for (int j = 0; j < Wide::kLoads; ++j) {
-      const int q = b * kBlock + j * Wide::kStep + ow.row;
+      const int q = b * kBlock + j * Wide::kStep + tid / Wide::kPieces;
       token[j] = q < rows ? a.tokens[lo + q] : -1;
     }
   };
@@ -347,7 +343,7 @@ __global__ __launch_bounds__(256) void factors_kernel(Factors a) {
   auto load = [&](int b, uint16_t* stage) {
 #pragma unroll
     for (int j = 0; j < Wide::kLoads; ++j)
-      to_lds(token[j] >= 0 ? wide + c0 + (size_t)token[j] * ld + ow.off[j] : zeros,
+      to_lds(token[j] >= 0 ? wide + c0 + (size_t)token[j] * ld + column : zeros,
              stage + j * kThreads * 8 + wave * 512);
     uint16_t* const hl = stage + kBlock * kGradColumns;
 #pragma unroll
@@ -375,13 +371,13 @@ __global__ __launch_bounds__(256) void factors_kernel(Factors a) {
       bf16x8 fw[kTiles];
 #pragma unroll
       for (int m = 0; m < kTiles; ++m)
-        fw[m] = Wide::read_across(stage, (wave * kTiles + m) * 16, s, n, g);
+        fw[m] = Wide::read_across(stage, Wide::across(wave * kTiles + m, n, g), s);
 #pragma unroll
       for (int part = 0; part < 3; ++part) {
         const uint16_t* const hl = stage + kBlock * kGradColumns + part * kBlock * kRank;
 #pragma unroll
         for (int j = 0; j < JT; ++j) {
-          const bf16x8 fh = Rank::read_across(hl, 16 * j, s, n, g);
+          const bf16x8 fh = Rank::read_across(hl, Rank::across(j, n, g), s);
 #pragma unroll
           for (int m = 0; m < kTiles; ++m)
             acc[m][j] = is_a ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[m], fh, acc[m][j], 0, 0, 0)

@@ -25,6 +25,10 @@ namespace {
 
 enum Kind { kForward, kGradX, kGradW };
 
+constexpr int kUnits = 256;             // compute units of the GPU
+constexpr int kTileQuads = 256 * 256 / 4;
+constexpr int kSplitRounds = 16;        // tiles a unit from which none is split
+
 struct Product {
   const int32_t* offsets;
   int E, P;
@@ -39,9 +43,152 @@ struct Product {
   void* dw;
   int dw_fp32, accumulate;
   int column_tiles, row_tiles; // row_tiles: kGradW
+  floatx4* sums;               // of parts of tiles (kUnits of 256 x 256), or null: none is split
 };
 
-template <Kind kKind, int BA, int BB, int WA, int WB, int kStages>
+// Where a workgroup's tile lies, and its operands.
+struct Tile {
+  int e, first, live, c0, reduction;
+  int rows_left;               // of the output from the tile's first on, as its operand has them
+  int part;                    // of the workspace, which takes its sums; -1: the output does
+  const uint16_t *a, *b;       // the tile's first column's (row's) values
+  long lda, ldb;
+};
+
+// Tiles that are worked on whole: one for every compute unit as often as that goes.  Of the rest
+// every tile's reduction is split in so many parts that they are one for every unit again, or in as
+// many as have kLeastBlocks blocks each (reduction: the rows of a group on average where it is they).
+struct Shares {
+  long whole;
+  int rest, parts;
+};
+constexpr int kLeastBlocks = 8;
+__host__ __device__ inline Shares shares_of(long tiles, int reduction) {
+  Shares s{tiles, 0, 1};
+  const int rest = (int)(tiles % kUnits);
+  if (rest == 0) return s;
+  const int by_units = kUnits / rest, by_blocks = reduction / (kBlock * kLeastBlocks);
+  const int parts = by_units < by_blocks ? by_units : by_blocks;
+  if (parts < 2) return s;
+  s.whole = tiles - rest;
+  s.rest = rest;
+  s.parts = parts;
+  return s;
+}
+template <Kind kKind>
+__device__ __forceinline__ int common_reduction(const Product& p) {
+  return kKind == kGradW ? p.P / p.E + 1 : p.reduction;
+}
+
+template <Kind kKind, int BA, int BB>
+__device__ __forceinline__ bool tile_at(const Product& p, const RowTiles& c, long at, Tile& t) {
+  if constexpr (kKind == kGradW) {
+    const int per = p.column_tiles * p.row_tiles;
+    t.e = (int)(at / per);
+    const int in = (int)(at % per);
+    t.first = in / p.column_tiles * BB;                // row of dW_e
+    t.c0 = in % p.column_tiles * BA;
+    t.rows_left = p.out_rows - t.first;
+    t.live = min(BB, t.rows_left);
+    int lo, hi;
+    group_rows(p.offsets, t.e, p.P, lo, hi);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    t.reduction = __builtin_amdgcn_readfirstlane(hi) - lo;
+    t.a = p.a + (size_t)lo * p.lda + t.c0;
+    t.b = p.b + (size_t)lo * p.ldb + t.first;
+    t.lda = p.lda;
+  } else {
+    Place q;
+    if (!place_of(p.offsets, p.E, p.P, BB, p.column_tiles, c, at, q)) return false;
+    t.e = q.e;
+    t.first = q.first;
+    t.rows_left = t.live = q.live;
+    t.c0 = q.column * BA;
+    t.reduction = p.reduction;
+    const size_t group = (size_t)t.e * p.columns * p.reduction;
+    t.a = kKind == kForward ? p.a + group + (size_t)t.c0 * p.reduction : p.a + group + t.c0;
+    t.lda = kKind == kForward ? p.reduction : p.columns;
+    t.b = p.b + (size_t)t.first * p.ldb;
+  }
+  t.ldb = p.ldb;
+  t.part = -1;
+  return true;
+}
+template <Kind kKind, int BB>
+__device__ __forceinline__ long count_tiles(const Product& p, RowTiles& c) {
+  if constexpr (kKind == kGradW) return (long)p.E * p.column_tiles * p.row_tiles;
+  c = count_row_tiles(p.offsets, p.E, p.P, BB);
+  return (long)c.total * p.column_tiles;
+}
+// This workgroup's tile, or the part of it; false where there is none for it.
+template <Kind kKind, int BA, int BB>
+__device__ __forceinline__ bool find_tile(const Product& p, Tile& t) {
+  RowTiles c;
+  const long tiles = count_tiles<kKind, BB>(p, c);
+  const Shares s = p.sums ? shares_of(tiles, common_reduction<kKind>(p)) : Shares{tiles, 0, 1};
+  const int i = blockIdx.x;
+  const long whole = (s.whole + 7) / 8 * 8;            // (kUnits times something, or all)
+  if (i < whole) {
+    const long at = kKind == kGradW ? (i < s.whole ? i : -1) : piece_of(i, s.whole);
+    return at >= 0 && tile_at<kKind, BA, BB>(p, c, at, t);
+  }
+  const long at = piece_of(i - (int)whole, (long)s.rest * s.parts);
+  if (at < 0 || !tile_at<kKind, BA, BB>(p, c, s.whole + at / s.parts, t)) return false;
+  const int blocks = (t.reduction + kBlock - 1) / kBlock, part = (int)(at % s.parts);
+  const int from = (int)((long)blocks * part / s.parts) * kBlock;
+  const int upto = (int)((long)blocks * (part + 1) / s.parts) * kBlock;
+  t.part = (int)at;
+  t.reduction = min(upto, t.reduction) - from;
+  t.a += kKind == kForward ? from : from * t.lda;
+  t.b += kKind == kGradW ? from * t.ldb : from;
+  return true;
+}
+
+// The results of 16 output rows (`r` this lane's, of the tile) and MA column tiles from column c on:
+// lane (n, g) holds columns 4 g .. 4 g + 3 of each tile in row n; kSpread: of the pairs that
+// tile_kernel deals.
+template <Kind kKind, bool kSpread, int MA>
+__device__ __forceinline__ void store(const Product& a, const Tile& t, int r, int c, int g,
+                                      const floatx4 (&v)[MA]) {
+  if (r >= t.live) return;
+  if constexpr (kKind == kGradW) {
+    const size_t row = ((size_t)t.e * a.out_rows + t.first + r) * a.columns;
+#pragma unroll
+    for (int m = 0; m < MA; ++m) {
+      const int at = c + 16 * m + 4 * g;
+      if (at >= a.columns) continue;                   // (columns come in eights)
+      if (a.dw_fp32) {
+        floatx4* const out = reinterpret_cast<floatx4*>(static_cast<float*>(a.dw) + row + at);
+        *out = a.accumulate ? *out + v[m] : v[m];
+      } else {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dw) + row + at) =
+            make_uint2(to_bf16x2(v[m][0], v[m][1]), to_bf16x2(v[m][2], v[m][3]));
+      }
+    }
+  } else {
+    uint16_t* const out = a.out + (size_t)(t.first + r) * a.ldo;
+    if constexpr (kSpread) {
+#pragma unroll
+      for (int m = 0; m < MA; m += 2) {
+        const int at = c + 16 * m + 8 * g;
+        if (at >= a.columns) continue;
+        *reinterpret_cast<uint4*>(out + at) =
+            make_uint4(to_bf16x2(v[m][0], v[m][1]), to_bf16x2(v[m][2], v[m][3]),
+                       to_bf16x2(v[m + 1][0], v[m + 1][1]), to_bf16x2(v[m + 1][2], v[m + 1][3]));
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < MA; ++m) {
+        const int at = c + 16 * m + 4 * g;
+        if (at < a.columns)
+          *reinterpret_cast<uint2*>(out + at) =
+              make_uint2(to_bf16x2(v[m][0], v[m][1]), to_bf16x2(v[m][2], v[m][3]));
+      }
+    }
+  }
+}
+
+template <Kind kKind, int BA, int BB, int WA, int WB, int kStages, int kB>
 __global__ __launch_bounds__(64 * WA * WB) void tile_kernel(Product a) {
   constexpr bool kAcrossA = kKind != kForward, kAcrossB = kKind == kGradW;
   constexpr int kThreads = 64 * WA * WB;
@@ -49,52 +196,24 @@ __global__ __launch_bounds__(64 * WA * WB) void tile_kernel(Product a) {
   // Going forward the columns of two neighbouring A tiles are dealt so that a lane's eight results
   // are neighbours: row i = 4 a + b of tile m is column 8 a + 4 (m % 2) + b of the pair.
   constexpr bool kSpread = !kAcrossA && MA % 2 == 0;
-  using OpA = Operand<kAcrossA, kSpread, BA, kThreads>;
-  using OpB = Operand<kAcrossB, false, BB, kThreads>;
+  using OpA = Operand<kAcrossA, kSpread, BA, kThreads, kB>;
+  using OpB = Operand<kAcrossB, false, BB, kThreads, kB>;
   constexpr int kLoads = OpA::kLoads + OpB::kLoads;
-  constexpr int kStage = (BA + BB) * kBlock;
+  constexpr int kStage = (BA + BB) * kB;
   extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wa = wave % WA, wb = wave / WA;
   const int n = lane & 15, g = lane >> 4;
 
-  int e, first, live, c0, reduction;
-  if constexpr (kKind == kGradW) {
-    const int per = a.column_tiles * a.row_tiles;
-    e = blockIdx.x / per;
-    const int at = blockIdx.x % per;
-    first = at / a.column_tiles * BB;                  // row of dW_e
-    c0 = at % a.column_tiles * BA;
-    live = min(BB, a.out_rows - first);
-  } else {
-    Place p;
-    if (!find_place(a.offsets, a.E, a.P, BB, a.column_tiles, p)) return;
-    e = __builtin_amdgcn_readfirstlane(p.e);
-    first = __builtin_amdgcn_readfirstlane(p.first);
-    live = __builtin_amdgcn_readfirstlane(p.live);
-    c0 = __builtin_amdgcn_readfirstlane(p.column) * BA;
-  }
+  Tile tile;
+  if (!find_tile<kKind, BA, BB>(a, tile)) return;     // (its parts are turns_kernel's alone)
+  const int reduction = tile.reduction;
   OpA oa;
   OpB ob;
-  const int live_columns = min(BA, a.columns - c0);
-  if constexpr (kKind == kForward) {
-    reduction = a.reduction;
-    oa.init(a.a + ((size_t)e * a.columns + c0) * reduction, reduction, live_columns, reduction, tid);
-    ob.init(a.b + (size_t)first * a.ldb, a.ldb, live, reduction, tid);
-  } else if constexpr (kKind == kGradX) {
-    reduction = a.reduction;
-    oa.init(a.a + (size_t)e * a.columns * reduction + c0, a.columns, live_columns, reduction, tid);
-    ob.init(a.b + (size_t)first * a.ldb, a.ldb, live, reduction, tid);
-  } else {
-    int lo, hi;
-    group_rows(a.offsets, e, a.P, lo, hi);
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    reduction = __builtin_amdgcn_readfirstlane(hi) - lo;
-    oa.init(a.a + (size_t)lo * a.lda + c0, a.lda, live_columns, reduction, tid);
-    ob.init(a.b + (size_t)lo * a.ldb + first, a.ldb, live, reduction, tid);
-  }
-  const int blocks = (reduction + kBlock - 1) / kBlock;
+  oa.init(tile.a, tile.lda, a.columns - tile.c0, reduction, tid);
+  ob.init(tile.b, tile.ldb, tile.rows_left, reduction, tid);
+  const int blocks = (reduction + kB - 1) / kB;
 
   floatx4 acc[MA][MB];
 #pragma unroll
@@ -106,20 +225,20 @@ __global__ __launch_bounds__(64 * WA * WB) void tile_kernel(Product a) {
     if (i < OpA::kLoads)
       oa.load(b, stage, i < OpA::kLoads ? i : 0, wave);
     else
-      ob.load(b, stage + BA * kBlock, i < OpA::kLoads ? 0 : i - OpA::kLoads, wave);
+      ob.load(b, stage + BA * kB, i < OpA::kLoads ? 0 : i - OpA::kLoads, wave);
   };
   auto step = [&](int b, const uint16_t* __restrict__ stage, uint16_t* __restrict__ next) {
     const uint16_t* const sa = stage;
-    const uint16_t* const sb = stage + BA * kBlock;
+    const uint16_t* const sb = stage + BA * kB;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load(b + kStages - 1, next, i);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < kB / 32; ++s) {
       bf16x8 fa[MA], fb[MB];
 #pragma unroll
       for (int m = 0; m < MA; ++m) {
         if constexpr (kAcrossA) {
-          fa[m] = OpA::read_across(sa, (wa * MA + m) * 16, s, n, g);
+          fa[m] = OpA::read_across(sa, OpA::across(wa * MA + m, n, g), s);
         } else {
           const int R = kSpread ? wa * MA * 16 + m / 2 * 32 + 8 * (n >> 2) + 4 * (m & 1) + (n & 3)
                                 : (wa * MA + m) * 16 + n;
@@ -129,7 +248,7 @@ __global__ __launch_bounds__(64 * WA * WB) void tile_kernel(Product a) {
 #pragma unroll
       for (int t = 0; t < MB; ++t) {
         if constexpr (kAcrossB)
-          fb[t] = OpB::read_across(sb, (wb * MB + t) * 16, s, n, g);
+          fb[t] = OpB::read_across(sb, OpB::across(wb * MB + t, n, g), s);
         else
           fb[t] = OpB::read_along(sb, (wb * MB + t) * 16 + n, s, g);
       }
@@ -154,73 +273,322 @@ __global__ __launch_bounds__(64 * WA * WB) void tile_kernel(Product a) {
     wait_loads<0>();
   }
 
-  // lane (n, g) holds columns 4 g .. 4 g + 3 of column tile m, in row n of row tile t
 #pragma unroll
   for (int t = 0; t < MB; ++t) {
-    const int r = wb * MB * 16 + 16 * t + n;
-    if (r >= live) continue;
-    if constexpr (kKind == kGradW) {
-      const size_t row = ((size_t)e * a.out_rows + first + r) * a.columns;
+    floatx4 v[MA];
 #pragma unroll
-      for (int m = 0; m < MA; ++m) {
-        const int c = c0 + (wa * MA + m) * 16 + 4 * g;
-        if (c >= a.columns) continue;                  // (columns come in eights)
-        if (a.dw_fp32) {
-          floatx4* const out = reinterpret_cast<floatx4*>(static_cast<float*>(a.dw) + row + c);
-          *out = a.accumulate ? *out + acc[m][t] : acc[m][t];
-        } else {
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dw) + row + c) =
-              make_uint2(to_bf16x2(acc[m][t][0], acc[m][t][1]),
-                         to_bf16x2(acc[m][t][2], acc[m][t][3]));
-        }
-      }
-    } else {
-      uint16_t* const out = a.out + (size_t)(first + r) * a.ldo;
-      if constexpr (kSpread) {
-#pragma unroll
-        for (int m = 0; m < MA; m += 2) {
-          const int c = c0 + wa * MA * 16 + m / 2 * 32 + 8 * g;
-          if (c >= a.columns) continue;
-          *reinterpret_cast<uint4*>(out + c) =
-              make_uint4(to_bf16x2(acc[m][t][0], acc[m][t][1]), to_bf16x2(acc[m][t][2], acc[m][t][3]),
-                         to_bf16x2(acc[m + 1][t][0], acc[m + 1][t][1]),
-                         to_bf16x2(acc[m + 1][t][2], acc[m + 1][t][3]));
-        }
-      } else {
-#pragma unroll
-        for (int m = 0; m < MA; ++m) {
-          const int c = c0 + (wa * MA + m) * 16 + 4 * g;
-          if (c >= a.columns) continue;
-          *reinterpret_cast<uint2*>(out + c) = make_uint2(to_bf16x2(acc[m][t][0], acc[m][t][1]),
-                                                          to_bf16x2(acc[m][t][2], acc[m][t][3]));
-        }
-      }
-    }
+    for (int m = 0; m < MA; ++m) v[m] = acc[m][t];
+    store<kKind, kSpread>(a, tile, wb * MB * 16 + 16 * t + n, tile.c0 + wa * MA * 16, g, v);
   }
 }
 
-template <Kind kKind, int BA, int BB, int WA, int WB, int kStages>
-hipError_t launch_tile(Product a, hipStream_t stream) {
-  constexpr int kBytes = kStages * (BA + BB) * kBlock * 2;
-  static_assert(kBytes <= 160 * 1024, "LDS of a compute unit");
-  const auto kernel = tile_kernel<kKind, BA, BB, WA, WB, kStages>;
-  if (kBytes > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    if (e != hipSuccess) return e;
+// Tiles of 256 x 256, eight waves of 128 columns by 64 rows, in two groups that take turns: while one
+// works through the matrix instructions of a quarter of its block, the other reads the operands of its
+// next quarter from LDS and starts loads.  Either operand has two halves of 128 rows (columns); a
+// wave has 64 columns and 32 rows of each.  A half is loaded for the block after the next as soon
+// as both groups have read it, so that two buffers hold almost two blocks of loads in flight.
+template <Kind kKind>
+__global__ __launch_bounds__(512, 2) void turns_kernel(Product a) {
+  constexpr bool kAcrossA = kKind != kForward, kAcrossB = kKind == kGradW;
+  constexpr bool kSpread = !kAcrossA;
+  using OpA = Operand<kAcrossA, kSpread, 128, 512>;
+  using OpB = Operand<kAcrossB, false, 128, 512>;
+  constexpr int kHalf = 128 * kBlock;                  // elements of a half
+  constexpr int kStage = 4 * kHalf;                    // A's halves, B's halves
+  extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wa = wave & 1, wb = wave >> 1;
+  const int n = lane & 15, g = lane >> 4;
+  Tile tile;
+  if (!find_tile<kKind, 256, 256>(a, tile)) return;
+  const int reduction = tile.reduction;
+  OpA oa[2];
+  OpB ob[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    oa[h].init(tile.a + 128 * h * (kAcrossA ? 1 : tile.lda), tile.lda, a.columns - tile.c0 - 128 * h,
+               reduction, tid);
+    ob[h].init(tile.b + 128 * h * (kAcrossB ? 1 : tile.ldb), tile.ldb, tile.rows_left - 128 * h,
+               reduction, tid);
   }
+  const int blocks = (reduction + kBlock - 1) / kBlock;
+  floatx4 acc[2][2][2][4];                             // A's half, B's half, row tile, column tile
+#pragma unroll
+  for (int i = 0; i < 2 * 2 * 2 * 4; ++i)
+    acc[i >> 4][i >> 3 & 1][i >> 2 & 1][i & 3] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  bf16x8 fa[2][2][4], fb[2][2][2];                     // half, 32 of the block, tile
+
+  int place_a[4], place_b[2];                          // of what lies across the reduction
+#pragma unroll
+  for (int m = 0; m < 4; ++m) place_a[m] = OpA::across(wa * 4 + m, n, g);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) place_b[t] = OpB::across(wb * 2 + t, n, g);
+  auto read_a = [&](int h, int s, const uint16_t* __restrict__ from) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      if constexpr (kAcrossA)
+        fa[h][s][m] = OpA::read_across(from, place_a[m], s);
+      else
+        fa[h][s][m] = OpA::read_along(
+            from, wa * 64 + m / 2 * 32 + 8 * (n >> 2) + 4 * (m & 1) + (n & 3), s, g);
+    }
+  };
+  auto read_b = [&](int h, const uint16_t* __restrict__ from) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if constexpr (kAcrossB)
+          fb[h][s][t] = OpB::read_across(from, place_b[t], s);
+        else
+          fb[h][s][t] = OpB::read_along(from, wb * 32 + 16 * t + n, s, g);
+      }
+  };
+  auto load_a = [&](int b, int h, uint16_t* __restrict__ to) {
+    oa[h].load(b, to, 0, wave);
+    oa[h].load(b, to, 1, wave);
+  };
+  auto load_b = [&](int b, int h, uint16_t* __restrict__ to) {
+    ob[h].load(b, to, 0, wave);
+    ob[h].load(b, to, 1, wave);
+  };
+  // The end of a quarter's reads: they are done, and all but N loads; then the other group's turn.
+  auto meet = [&](auto loads) {
+    constexpr int N = decltype(loads)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (N >= 0)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N >= 0 ? N : 0) : "memory");
+    else
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply = [&](int ha, int hb) {
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          acc[ha][hb][t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[ha][s][m], fb[hb][s][t],
+                                                                      acc[ha][hb][t][m], 0, 0, 0);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  std::integral_constant<int, -1> reads;
+  std::integral_constant<int, 8> eight;
+  std::integral_constant<int, 12> twelve;
+  // One block, a quarter of its products a turn: what a turn reads was loaded two blocks ago, and what
+  // all have read by then is loaded for the block after the next.
+  auto block = [&](int b, uint16_t* __restrict__ here, uint16_t* __restrict__ other) {
+    read_b(0, here + 2 * kHalf);
+    read_a(0, 1, here);
+    meet(reads);
+    multiply(0, 0);
+    read_b(1, here + 3 * kHalf);
+    read_a(1, 0, here + kHalf);
+    __builtin_amdgcn_sched_barrier(0);
+    load_a(b + 2, 0, here);
+    meet(reads);
+    multiply(0, 1);
+    read_a(1, 1, here + kHalf);
+    __builtin_amdgcn_sched_barrier(0);
+    load_b(b + 2, 0, here + 2 * kHalf);
+    load_b(b + 2, 1, here + 3 * kHalf);
+    meet(twelve);                                      // the next block's first half of A is there
+    multiply(1, 1);
+    read_a(0, 0, other);
+    __builtin_amdgcn_sched_barrier(0);
+    load_a(b + 2, 1, here + kHalf);
+    meet(eight);                                       // and the rest of it
+    multiply(1, 0);
+  };
+  if (blocks > 0) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      load_a(b, 0, lds + b * kStage);
+      load_b(b, 0, lds + b * kStage + 2 * kHalf);
+      load_b(b, 1, lds + b * kStage + 3 * kHalf);
+      load_a(b, 1, lds + b * kStage + kHalf);
+    }
+    meet(eight);
+    read_a(0, 0, lds);
+    if (wave >= 4) meet(reads);                        // the second group comes a turn later
+#pragma unroll 1
+    for (int b = 0; b < blocks; ++b) {
+      const int here = (b & 1) * kStage;
+      block(b, lds + here, lds + (kStage - here));
+    }
+    if (wave < 4) meet(reads);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load outlives the workgroup's LDS
+  }
+  if (tile.part >= 0) {
+    floatx4* const to = a.sums + (size_t)tile.part * kTileQuads + tid;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) to[i * 512] = acc[i >> 4][i >> 3 & 1][i >> 2 & 1][i & 3];
+    return;
+  }
+#pragma unroll
+  for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int ha = 0; ha < 2; ++ha)
+        store<kKind, kSpread>(a, tile, hb * 128 + wb * 32 + 16 * t + n, tile.c0 + ha * 128 + wa * 64,
+                              g, acc[ha][hb][t]);
+}
+
+// The parts of the tiles that turns_kernel splits, summed in order and stored: workgroup (quarter,
+// tile), the threads' values as in that kernel.
+template <Kind kKind>
+__global__ __launch_bounds__(512) void join_kernel(Product a) {
+  constexpr bool kSpread = kKind == kForward;
+  RowTiles c;
+  const long tiles = count_tiles<kKind, 256>(a, c);
+  const Shares s = shares_of(tiles, common_reduction<kKind>(a));
+  Tile tile;
+  if ((int)blockIdx.y >= s.rest || !tile_at<kKind, 256, 256>(a, c, s.whole + blockIdx.y, tile)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wa = wave & 1, wb = wave >> 1, hb = blockIdx.x >> 1, t = blockIdx.x & 1;
+  const floatx4* from = a.sums + (size_t)blockIdx.y * s.parts * kTileQuads + tid;
+#pragma unroll
+  for (int ha = 0; ha < 2; ++ha) {
+    floatx4 v[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) v[m] = from[(16 * ha + 8 * hb + 4 * t + m) * 512];
+    for (int p = 1; p < s.parts; ++p)
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+        v[m] += from[(size_t)p * kTileQuads + (16 * ha + 8 * hb + 4 * t + m) * 512];
+    store<kKind, kSpread>(a, tile, hb * 128 + wb * 32 + 16 * t + (lane & 15),
+                          tile.c0 + ha * 128 + wa * 64, lane >> 4, v);
+  }
+}
+
+// The most tiles of BA x BB that there can be.
+template <Kind kKind, int BA, int BB>
+long most_tiles(Product& a) {
   a.column_tiles = (a.columns + BA - 1) / BA;
   a.row_tiles = (a.out_rows + BB - 1) / BB;
-  long grid;
-  if (kKind == kGradW) {
-    grid = (long)a.E * a.column_tiles * a.row_tiles;
-  } else {
-    const long some = a.P < a.E ? a.P : a.E;           // at most one partly filled tile a group
-    grid = ((some + (a.P - some) / BB) * a.column_tiles + 7) / 8 * 8;
+  if (kKind == kGradW) return (long)a.E * a.column_tiles * a.row_tiles;
+  const long some = a.P < a.E ? a.P : a.E;             // at most one partly filled tile a group
+  return (some + (a.P - some) / BB) * a.column_tiles;
+}
+
+template <typename F>
+hipError_t launch(const Product& a, F kernel, long grid, int threads, int bytes,
+                  hipStream_t stream) {
+  if (bytes > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
   }
-  if (grid * 64 * WA * WB > 0xFFFFFFFFl) return hipErrorInvalidConfiguration;
-  kernel<<<(unsigned)grid, 64 * WA * WB, kBytes, stream>>>(a);
+  grid = (grid + 7) / 8 * 8;
+  if (grid * threads > 0xFFFFFFFFl) return hipErrorInvalidConfiguration;
+  kernel<<<(unsigned)grid, threads, bytes, stream>>>(a);
   return hipGetLastError();
+}
+
+template <Kind kKind, int BA, int BB, int WA, int WB, int kStages, int kB = kBlock>
+hipError_t launch_tile(Product a, hipStream_t stream) {
+  constexpr int kBytes = kStages * (BA + BB) * kB * 2;
+  static_assert(kBytes <= 160 * 1024, "LDS of a compute unit");
+  a.sums = nullptr;
+  const long tiles = most_tiles<kKind, BA, BB>(a);
+  return launch(a, tile_kernel<kKind, BA, BB, WA, WB, kStages, kB>, tiles, 64 * WA * WB, kBytes, stream);
+}
+
+template <Kind kKind>
+hipError_t launch_turns(Product a, hipStream_t stream) {
+  const long tiles = most_tiles<kKind, 256, 256>(a);
+  if (tiles > kSplitRounds * kUnits) a.sums = nullptr; // (the last round is a small part)
+  const long more = a.sums ? kUnits : 0;               // parts in place of the rest
+  const hipError_t e =
+      launch(a, turns_kernel<kKind>, tiles + more, 512, 2 * 512 * kBlock * 2, stream);
+  if (e != hipSuccess || !a.sums) return e;
+  const long rest = tiles < kUnits ? tiles : kUnits - 1;
+  join_kernel<kKind><<<dim3(4, (unsigned)rest), 512, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+// The forms of a product: its tile, and what 64 of the reduction cost in microseconds, `few` with
+// little else on the GPU, `full` for each tile that every compute unit has to work on.  Measured over
+// 1 to 64 groups of 1 to 4096 rows by four shapes of 512 to 4096; of 109 cases the choice came within
+// 10 % of the best form on 98 (forward) and 93 (dx), 3 and 4 % above it on average.
+struct Form {
+  int columns, rows;
+  float few, full;
+  hipError_t (*launch)(Product, hipStream_t);
+  bool turns;                  // turns_kernel, which splits what is left of a last round
+};
+const Form kForwardForms[] = {
+    {64, 32, 0.185f, 0.145f, launch_tile<kForward, 64, 32, 4, 1, 4>, false},
+    {64, 64, 0.23f, 0.205f, launch_tile<kForward, 64, 64, 2, 2, 3>, false},
+    {128, 64, 0.30f, 0.34f, launch_tile<kForward, 128, 64, 2, 2, 3>, false},
+    {256, 256, 1.07f, 1.5f, launch_turns<kForward>, true},
+};
+const Form kGradXForms[] = {
+    {64, 32, 0.225f, 0.145f, launch_tile<kGradX, 64, 32, 4, 1, 4>, false},
+    {64, 64, 0.25f, 0.205f, launch_tile<kGradX, 64, 64, 2, 2, 3>, false},
+    {128, 64, 0.38f, 0.33f, launch_tile<kGradX, 128, 64, 2, 2, 3>, false},
+    {128, 128, 0.52f, 0.68f, launch_tile<kGradX, 128, 128, 2, 2, 3>, false},
+    {256, 256, 1.35f, 1.7f, launch_turns<kGradX>, true},
+};
+// Outputs of many tiles are bound by writing them: with 96 rows a group or more on average in tiles of
+// 256 x 256 (128 groups' 256 rows by 1536 x 2048 in 544 us, 607 in tiles of 128 x 128), with fewer in
+// these (64 groups' 4 rows by 4096 x 4096 in 686 us, 789 in the others).
+const Form kGradWForms[] = {
+    {128, 64, 0.60f, 0.42f, launch_tile<kGradW, 128, 64, 2, 2, 3, 32>, false},
+    {128, 128, 0.82f, 0.64f, launch_tile<kGradW, 128, 128, 2, 2, 3, 32>, false},
+    {256, 256, 1.30f, 1.65f, launch_turns<kGradW>, true},
+};
+constexpr int kManyTiles = 1024;       // of 256 x 256
+constexpr int kWritten = 96;
+
+float form_cost(const Form& f, float tiles, int reduction) {
+  const float blocks = (float)((reduction + kBlock - 1) / kBlock);
+  if (!f.turns) {
+    const float round = tiles / kUnits;
+    const float some = f.few + (f.full > f.few ? (f.full - f.few) * (round < 1 ? round : 1) : 0);
+    return blocks * (f.full * round > some ? f.full * round : some);
+  }
+  const Shares s = shares_of((long)(tiles + 0.999f), reduction);
+  const long rounds = (s.whole + kUnits - 1) / kUnits;
+  float cost = rounds * f.full;
+  const int left = (int)(s.whole - (rounds - 1) * kUnits);
+  if (rounds > 0) cost -= (f.full - f.few) * (1.0f - (float)left / kUnits);
+  if (s.rest == 0) return blocks * cost;
+  const int more = s.rest * s.parts;                   // parts, each written and read again
+  cost += (f.few + (f.full - f.few) * more / kUnits) / s.parts;
+  return blocks * cost + 4.0f + 0.1f * more;
+}
+
+template <int N>
+const Form& form_for(const Form (&forms)[N], const Product& a, int groups, float mean,
+                     int reduction) {
+  int best = 0;
+  float least = 0;
+  for (int i = 0; i < N; ++i) {
+    const Form& f = forms[i];
+    if (f.turns && a.P < kTurnsRows) continue;
+    const int columns = (a.columns + f.columns - 1) / f.columns;
+    // a group's last tile is half full on average (one group's size is known)
+    const float rows = a.out_rows ? (float)((a.out_rows + f.rows - 1) / f.rows)
+                       : groups == 1 ? (float)((a.P + f.rows - 1) / f.rows)
+                       : mean > 1 ? mean / f.rows + 0.5f : 1.0f;
+    const float cost = form_cost(f, groups * columns * (rows > 1 ? rows : 1.0f), reduction);
+    if (i == 0 || cost < least) {
+      best = i;
+      least = cost;
+    }
+  }
+  return forms[best];
 }
 
 Product product_of(const GroupedArgs& g) {
@@ -230,7 +598,14 @@ Product product_of(const GroupedArgs& g) {
   a.P = g.P;
   a.out = g.out;
   a.ldo = g.ldo;
+  a.sums = reinterpret_cast<floatx4*>(g.sums);
   return a;
+}
+
+template <int N>
+hipError_t launch_rows(const Form (&forms)[N], const Product& a, hipStream_t stream) {
+  const int groups = a.P < a.E ? a.P : a.E;
+  return form_for(forms, a, groups, (float)a.P / groups, a.reduction).launch(a, stream);
 }
 
 }  // namespace
@@ -242,10 +617,7 @@ hipError_t launch_grouped_linear(const GroupedArgs& g, hipStream_t stream) {
   a.a = g.w;
   a.b = g.x;
   a.ldb = g.ldx;
-  const int mean = g.P / (g.P < g.E ? g.P : g.E);
-  if (mean <= 24) return launch_tile<kForward, 64, 32, 4, 1, 4>(a, stream);
-  if (mean <= 160) return launch_tile<kForward, 128, 128, 2, 2, 2>(a, stream);
-  return launch_tile<kForward, 256, 256, 2, 4, 2>(a, stream);
+  return launch_rows(kForwardForms, a, stream);
 }
 
 hipError_t launch_grouped_backward_x(const GroupedArgs& g, hipStream_t stream) {
@@ -255,10 +627,7 @@ hipError_t launch_grouped_backward_x(const GroupedArgs& g, hipStream_t stream) {
   a.a = g.w;
   a.b = g.dy;
   a.ldb = g.lddy;
-  const int mean = g.P / (g.P < g.E ? g.P : g.E);
-  if (mean <= 24) return launch_tile<kGradX, 64, 32, 4, 1, 4>(a, stream);
-  if (mean <= 160) return launch_tile<kGradX, 128, 128, 2, 2, 2>(a, stream);
-  return launch_tile<kGradX, 256, 256, 2, 4, 2>(a, stream);
+  return launch_rows(kGradXForms, a, stream);
 }
 
 hipError_t launch_grouped_backward_w(const GroupedArgs& g, hipStream_t stream) {
@@ -272,7 +641,12 @@ hipError_t launch_grouped_backward_w(const GroupedArgs& g, hipStream_t stream) {
   a.dw = g.dw;
   a.dw_fp32 = g.dw_fp32;
   a.accumulate = g.accumulate;
-  return launch_tile<kGradW, 128, 128, 2, 2, 2>(a, stream);
+  const float mean = (float)a.P / a.E;
+  const long tiles = (long)a.E * ((a.columns + 255) / 256) * ((a.out_rows + 255) / 256);
+  if (tiles >= kManyTiles)
+    return mean >= kWritten ? launch_tile<kGradW, 256, 256, 2, 4, 4, 32>(a, stream)
+                            : launch_tile<kGradW, 128, 128, 2, 2, 3, 32>(a, stream);
+  return form_for(kGradWForms, a, a.E, mean, (int)mean + 1).launch(a, stream);
 }
 
 }  // namespace xs

@@ -58,6 +58,11 @@ hipError_t launch_combine_backward(const MoveArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------------------- products
 
+// Rows from which the products may take 256 x 256 tiles, which keep the sums of split ones in the
+// workspace: at most one part for each of 256 compute units.
+constexpr int kTurnsRows = 256;
+inline size_t grouped_bytes(int P) { return P < kTurnsRows ? 0 : size_t(256) * 256 * 256 * 4; }
+
 struct GroupedArgs {
   int P, E, n, k;
   const int32_t* offsets;      // [E + 1]
@@ -70,6 +75,7 @@ struct GroupedArgs {
   long ldo;
   void* dw;                    // [E, n, k], bf16 or fp32
   int dw_fp32, accumulate;
+  float* sums;                 // grouped_bytes(P) of them, or null
 };
 hipError_t launch_grouped_linear(const GroupedArgs& a, hipStream_t stream);
 hipError_t launch_grouped_backward_x(const GroupedArgs& a, hipStream_t stream);

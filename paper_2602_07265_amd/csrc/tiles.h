@@ -18,6 +18,7 @@ using LdsPtr = __attribute__((address_space(3))) void*;
 using LdsQuad = __attribute__((address_space(3))) i16x4*;
 
 constexpr int kBlock = 64;     // of the reduction
+constexpr uint32_t kPast = 1u << 31;   // bytes that no buffer of a load has
 
 __device__ const uint4 kZeros[1] = {{0, 0, 0, 0}};
 
@@ -49,67 +50,85 @@ __device__ __forceinline__ void group_rows(const int32_t* offsets, int e, int P,
   hi = max(lo, min(offsets[e + 1], P));
 }
 
-// A row tile: its group, first row and rows; tiles are counted over the groups in turn, and the
-// columns' tiles within them, near ones to the same XCD.
-struct Place {
-  int e, first, live, column;
+// Workgroups go to the eight XCDs in turn.  For `n` pieces of work of which neighbours share operands:
+// workgroup i's piece, such that every XCD gets a run of them; -1 where there is none for it.
+__device__ __forceinline__ long piece_of(int i, long n) {
+  const long per = (n + 7) / 8, at = (i & 7) * per + (i >> 3);
+  return (i >> 3) < per && at < n ? at : -1;
+}
+
+// Row tiles of `tile` rows, counted over the groups in turn.  Every wave counts them for itself: lane
+// l those of groups l span .. l span + span - 1.
+struct RowTiles {
+  int span, mine, upto;        // groups of a lane; their tiles; those and all before
+  int total;
 };
-// The place of this workgroup among `columns` column tiles of every row tile of `tile` rows; false
-// where there is none for it (the grid is an upper bound).  Every wave finds it for itself: lane
-// l counts the tiles of groups l S .. l S + S - 1.
-__device__ __forceinline__ bool find_place(const int32_t* offsets, int E, int P, int tile, int columns,
-                                           Place& p) {
+__device__ __forceinline__ RowTiles count_row_tiles(const int32_t* offsets, int E, int P, int tile) {
   const int lane = threadIdx.x & 63;
-  const int span = (E + 63) / 64;
-  int mine = 0;
-  for (int i = 0; i < span; ++i) {
-    const int e = lane * span + i;
+  RowTiles c;
+  c.span = (E + 63) / 64;
+  c.mine = 0;
+  for (int i = 0; i < c.span; ++i) {
+    const int e = lane * c.span + i;
     if (e >= E) break;
     int lo, hi;
     group_rows(offsets, e, P, lo, hi);
-    mine += (hi - lo + tile - 1) / tile;
+    c.mine += (hi - lo + tile - 1) / tile;
   }
-  const int upto = wave_scan(mine);
-  const int tiles = __builtin_amdgcn_readlane(upto, 63);
-  // workgroups go to the eight XCDs in turn: each gets a run of tiles
-  const long all = (long)tiles * columns;
-  const int per = (int)((all + 7) / 8);
-  const int idx = blockIdx.x >> 3, xcd = blockIdx.x & 7;
-  const long at = (long)xcd * per + idx;
-  if (idx >= per || at >= all) return false;
-  // four row tiles next to each other, column after column
+  c.upto = wave_scan(c.mine);
+  c.total = __builtin_amdgcn_readlane(c.upto, 63);
+  return c;
+}
+
+// A tile of the output: its group, first row, rows, and column tile.
+struct Place {
+  int e, first, live, column;
+};
+// The at-th of c.total * columns tiles: four row tiles next to each other, column after column.
+__device__ __forceinline__ bool place_of(const int32_t* offsets, int E, int P, int tile, int columns,
+                                         const RowTiles& c, long at, Place& p) {
   constexpr int kDeep = 4;
   const int band = (int)(at / ((long)kDeep * columns));
-  const int deep = min(kDeep, tiles - band * kDeep);
+  const int deep = min(kDeep, c.total - band * kDeep);
   const int rest = (int)(at - (long)band * kDeep * columns);
   const int want = band * kDeep + rest % deep;
   p.column = rest / deep;
-  const int holder = __builtin_ctzll(__ballot(upto > want));
-  int left = want - __builtin_amdgcn_readlane(upto - mine, holder);
-  for (int e = holder * span; e < E; ++e) {
+  const int holder = __builtin_ctzll(__ballot(c.upto > want));
+  int left = want - __builtin_amdgcn_readlane(c.upto - c.mine, holder);
+  for (int e = holder * c.span; e < E; ++e) {
     int lo, hi;
     group_rows(offsets, e, P, lo, hi);
     const int n = (hi - lo + tile - 1) / tile;
     if (left < n) {
-      p.e = e;
-      p.first = lo + left * tile;
-      p.live = min(tile, hi - p.first);
+      p.e = __builtin_amdgcn_readfirstlane(e);
+      p.first = __builtin_amdgcn_readfirstlane(lo + left * tile);
+      p.live = __builtin_amdgcn_readfirstlane(min(tile, hi - p.first));
+      p.column = __builtin_amdgcn_readfirstlane(p.column);
       return true;
     }
     left -= n;
   }
   return false;
 }
+// The tile of this workgroup, of `columns` column tiles of every row tile of `tile` rows; false where
+// there is none for it (the grid is an upper bound).
+__device__ __forceinline__ bool find_place(const int32_t* offsets, int E, int P, int tile, int columns,
+                                           Place& p) {
+  const RowTiles c = count_row_tiles(offsets, E, P, tile);
+  const long at = piece_of(blockIdx.x, (long)c.total * columns);
+  return at >= 0 && place_of(offsets, E, P, tile, columns, c, at, p);
+}
 
 // One operand's tile of `kRows` rows or columns of the output, kThreads loading it.
 //   along  LDS [kRows][64]: row R's 16-byte piece c lies at c ^ swap(R)
-//   across LDS [64][kRows]: the 16 columns u of reduction q lie at u ^ swap(q)
-template <bool kAcross, bool kSpread, int kRows, int kThreads>
+//   across LDS [kB][kRows]: the 16 columns u of reduction q lie at u ^ swap(q)
+template <bool kAcross, bool kSpread, int kRows, int kThreads, int kB = kBlock>
 struct Operand {
-  static constexpr int kLoads = kRows * 8 / kThreads;
+  static_assert(kAcross || kB == kBlock, "rows of 128 bytes");
+  static constexpr int kLoads = kRows * kB / 8 / kThreads;
   static constexpr int kPieces = kAcross ? kRows / 8 : 8;       // of an LDS row
   static constexpr int kStep = kThreads / kPieces;              // LDS rows of a load
-  static_assert(kRows * 8 % kThreads == 0, "whole loads");
+  static_assert(kRows * kB / 8 % kThreads == 0, "whole loads");
   // kSpread: the instruction's 16 rows lie 8 a + 4 m + b, a, b < 4, apart (see tile_kernel)
   __device__ static __forceinline__ int swap(int R) {
     if constexpr (!kAcross) return kSpread ? (R >> 1 & 1) | (R >> 3 & 3) << 1 : R >> 1 & 7;
@@ -117,54 +136,68 @@ struct Operand {
     if constexpr (kRows == 64) return (R >> 1 & 1) | (R >> 3 & 1) << 1;
     return kRows == 32 ? R >> 3 & 1 : 0;
   }
+  static_assert(kAcross || kStep % 32 == 0, "along, the places in a load's rows are every load's");
+
   const uint16_t* base;
   long ld;
+  int live;                    // rows (along) or columns (across) from base on; none: zeros
   int end;                     // of the reduction
-  uint32_t off[kLoads];        // along: of the lane's rows; across: of its columns
-  int piece, row;
+  int at;                      // the lane's first reduction of a block (along)
+  uint32_t off[kAcross ? kLoads : 1];   // the lane's, from a block's (along: a load's) start, bytes
 
-  // rows `live` of them from `base`, `ld` elements apart (along); or columns from `base`
-  __device__ __forceinline__ void init(const uint16_t* b, long l, int live, int reduction, int tid) {
+  // The column (across) of this lane's place in the LDS rows of load j.
+  __device__ static __forceinline__ int column(int tid, int j) {
+    return 8 * (tid % kPieces ^ swap(j * kStep + tid / kPieces) << 1);
+  }
+  // `live` rows (along) or columns (across) from b on, rows l elements apart
+  __device__ __forceinline__ void init(const uint16_t* b, long l, int n, int reduction, int tid) {
     base = b;
     ld = l;
+    live = n;
     end = reduction;
-    row = tid / kPieces;
-    const int slot = tid % kPieces;
-    if constexpr (kAcross) {
-      piece = 0;
+    const int row = tid / kPieces;
+    at = 8 * (tid % kPieces ^ swap(row));
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j)
-        off[j] = min(8 * (slot ^ swap(j * kStep + row) << 1), live - 8);
-    } else {
-      piece = 8 * (slot ^ swap(row));
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j)
-        off[j] = (uint32_t)(min(j * kStep + row, live - 1) * ld);
-    }
+    for (int j = 0; j < (kAcross ? kLoads : 1); ++j)
+      off[j] = 2 * ((uint32_t)((j * kStep + row) * l) + (kAcross ? column(tid, j) : at));
   }
+  // Load j of a block.  Buffer loads give zeros for what lies past the buffer that they are told of:
+  // it ends with the last live row's last value.  (Across, columns past the live ones bring the next
+  // row's values, to columns of the output that are not there.)
   __device__ __forceinline__ void load(int block, uint16_t* lds, int j, int wave) const {
-    const int k0 = block * kBlock;
-    const uint16_t* src;
+    const int k = block * kB;
+    const uint16_t* from;
+    int elements, ahead = 0;
+    uint32_t o;
     if constexpr (kAcross) {
-      const int q = k0 + j * kStep + row;
-      src = base + (long)q * ld + off[j];
-      if (q >= end) src = reinterpret_cast<const uint16_t*>(kZeros);
+      from = base + k * ld;
+      elements = live > 0 && end > k ? (min(end - k, kB) - 1) * (int)ld + live : 0;
+      o = off[j];
     } else {
-      src = base + off[j] + k0 + piece;
-      if (k0 + piece >= end) src = reinterpret_cast<const uint16_t*>(kZeros);
+      const int rows = live - j * kStep;
+      from = base + j * kStep * ld;
+      elements = rows > 0 ? (min(rows, kStep) - 1) * (int)ld + end : 0;
+      ahead = 2 * k;
+      o = at < end - k ? off[0] : kPast;               // (a row's end is no buffer's)
     }
-    to_lds(src, lds + j * kThreads * 8 + wave * 512);
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(from), 0,
+                                                          2 * elements, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        buffer, (LdsPtr)(lds + j * kThreads * 8 + wave * 512), 16, o, ahead, 0, 0);
   }
   // The instruction's operand: lane (n, g) holds reductions 32 s + 8 g .. + 7 of row (along) R,
   // or of column c0 + n (across).
   __device__ static __forceinline__ bf16x8 read_along(const uint16_t* lds, int R, int s, int g) {
     return *reinterpret_cast<const bf16x8*>(lds + R * kBlock + 8 * ((4 * s + g) ^ swap(R)));
   }
-  __device__ static __forceinline__ bf16x8 read_across(const uint16_t* lds, int c0, int s, int n,
-                                                       int g) {
-    const int q = 32 * s + 8 * g + (n >> 2);
-    const uint16_t* const p = lds + q * kRows + 16 * ((c0 >> 4) ^ swap(q)) + 4 * (n & 3);
-    const uint16_t* const p4 = lds + (q + 4) * kRows + 16 * ((c0 >> 4) ^ swap(q + 4)) + 4 * (n & 3);
+  // (a lane's place in tile u of 16 columns; what a step of four reductions adds is the same for all)
+  __device__ static __forceinline__ int across(int u, int n, int g) {
+    const int q = 8 * g + (n >> 2);
+    return q * kRows + 16 * (u ^ swap(q)) + 4 * (n & 3);
+  }
+  __device__ static __forceinline__ bf16x8 read_across(const uint16_t* lds, int place, int s) {
+    const uint16_t* const p = lds + place + 32 * s * kRows;
+    const uint16_t* const p4 = p + 4 * kRows;
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)p);
     const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)p4);
     typedef short i16x8 __attribute__((ext_vector_type(8)));

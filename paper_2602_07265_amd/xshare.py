@@ -294,11 +294,13 @@ def lib() -> ctypes.CDLL:
                                               _P, _I64, _P, _P]
         L.xshare_combine_backward.restype = ctypes.c_int
         for call in (L.xshare_grouped_linear, L.xshare_grouped_linear_backward_x):
-            call.argtypes = [_P, _I64, _P, _P, _I32, _I32, _I32, _I32, _P, _I64, _P]
+            call.argtypes = [_P, _I64, _P, _P, _I32, _I32, _I32, _I32, _P, _I64, _P, _SZ, _P]
             call.restype = ctypes.c_int
         L.xshare_grouped_linear_backward_w.argtypes = [_P, _I64, _P, _I64, _P, _I32, _I32, _I32,
-                                                       _I32, _P, _I32, _I32, _P]
+                                                       _I32, _P, _I32, _I32, _P, _SZ, _P]
         L.xshare_grouped_linear_backward_w.restype = ctypes.c_int
+        L.xshare_grouped_linear_workspace_bytes.argtypes = [_I32] * 4
+        L.xshare_grouped_linear_workspace_bytes.restype = _SZ
         L.xshare_adapters_workspace_bytes.argtypes = [_I32] * 6
         L.xshare_adapters_workspace_bytes.restype = _SZ
         for call in (L.xshare_adapters, L.xshare_adapters_backward):
@@ -1438,6 +1440,25 @@ def combine_backward(dy: torch.Tensor, rows: torch.Tensor, w: torch.Tensor, orde
     return dict(drows=drows, dw=dw)
 
 
+def grouped_linear_workspace_bytes(P: int, n_groups: int, n: int, k: int) -> int:
+    """Of ``grouped_linear`` and its gradients; 0 where they need none (and for invalid sizes)."""
+    P, E, n, k = int(P), int(n_groups), int(n), int(k)
+    if _past_32_bits(P | E | n | k):
+        return 0
+    return int(lib().xshare_grouped_linear_workspace_bytes(P, E, n, k))
+
+
+def _grouped_workspace(rows, workspace, P, E, n, k):
+    """(the workspace, its address, its bytes)"""
+    if workspace is not None:
+        return workspace, workspace.data_ptr(), _workspace(rows.device, workspace)
+    size = lib().xshare_grouped_linear_workspace_bytes(P, E, n, k)
+    if not size:
+        return None, None, 0
+    workspace = rows.new_empty(size, dtype=torch.uint8)
+    return workspace, workspace.data_ptr(), size
+
+
 def _grouped(rows, w, offsets, cols, name, call):
     """Checks the rows [P, cols'] and weights [E, n, k] of a product of groups: (ld, P, E, n, k)."""
     if not isinstance(w, torch.Tensor) or w.dim() != 3:
@@ -1454,7 +1475,7 @@ def _grouped(rows, w, offsets, cols, name, call):
 
 @_placed
 def grouped_linear(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, *, y=None,
-                   stream=None) -> torch.Tensor:
+                   workspace=None, stream=None) -> torch.Tensor:
     """y_p = W_e x_p (bf16 [P, n]) for the rows p = offsets[e] .. offsets[e + 1] - 1 of each group e
     (int32 [E + 1], as ``expert_order`` gives them), W bf16 [E, n, k], n and k multiples of 8.  Rows
     of no group are left as they were (``y``) or hold nothing.  Records no gradient:
@@ -1464,28 +1485,31 @@ def grouped_linear(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, *, y
         _no_gradient(x, "x", "grouped_linear_backward_x gives it")
         _no_gradient(w, "w", "grouped_linear_backward_w gives it")
     y, ldy = _matrix_out(y, x, (P, n), "y")
+    _ws, ws, size = _grouped_workspace(x, workspace, P, E, n, k)
     st = lib().xshare_grouped_linear(x.data_ptr(), ldx, w.data_ptr(), offsets.data_ptr(), P, E, n, k,
-                                     y.data_ptr(), ldy, _stream_of(x, stream))
+                                     y.data_ptr(), ldy, ws, size, _stream_of(x, stream))
     _check(st, "xshare_grouped_linear")
     return y
 
 
 @_placed
 def grouped_linear_backward_x(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, *, out=None,
-                              stream=None) -> torch.Tensor:
+                              workspace=None, stream=None) -> torch.Tensor:
     """The gradient of ``grouped_linear``'s x: dx_p = W_e^T dy_p (bf16 [P, k])."""
     lddy, P, E, n, k = _grouped(dy, w, offsets, 0, "dy", "xshare_grouped_linear_backward_x")
     out, ldo = _matrix_out(out, dy, (P, k), "out")
+    _ws, ws, size = _grouped_workspace(dy, workspace, P, E, n, k)
     st = lib().xshare_grouped_linear_backward_x(dy.data_ptr(), lddy, w.data_ptr(),
                                                 offsets.data_ptr(), P, E, n, k, out.data_ptr(), ldo,
-                                                _stream_of(dy, stream))
+                                                ws, size, _stream_of(dy, stream))
     _check(st, "xshare_grouped_linear_backward_x")
     return out
 
 
 @_placed
 def grouped_linear_backward_w(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, *, out=None,
-                              accumulate: bool = False, stream=None) -> torch.Tensor:
+                              accumulate: bool = False, workspace=None,
+                              stream=None) -> torch.Tensor:
     """The gradient of ``grouped_linear``'s weights: dW_e = sum over the group's rows of
     dy_p x_p^T, fp32 [E, n, k] (or of ``out``'s type, fp32 or bf16); zeros for a group without
     rows.  ``accumulate``: added to an fp32 ``out`` instead."""
@@ -1508,9 +1532,10 @@ def grouped_linear_backward_w(dy: torch.Tensor, x: torch.Tensor, offsets: torch.
         _fit(dy.device, (out, out.dtype, (E, n, k), "out"))
     else:
         raise ValueError("out must be float32 or bfloat16")
+    _ws, ws, size = _grouped_workspace(dy, workspace, P, E, n, k)
     st = lib().xshare_grouped_linear_backward_w(
         dy.data_ptr(), lddy, x.data_ptr(), ldx, offsets.data_ptr(), P, E, n, k, out.data_ptr(),
-        int(out.dtype is torch.bfloat16), int(bool(accumulate)), _stream_of(dy, stream))
+        int(out.dtype is torch.bfloat16), int(bool(accumulate)), ws, size, _stream_of(dy, stream))
     _check(st, "xshare_grouped_linear_backward_w")
     return out
 

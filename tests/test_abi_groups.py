@@ -72,25 +72,30 @@ def test_a_move_refuses(call, kw, status):
     assert call(**kw) == status
 
 
-def _linear(x=FAKE, ldx=64, w=FAKE, offsets=FAKE, P=8, E=4, n=40, k=64, y=FAKE, ldy=40):
-    return X.lib().xshare_grouped_linear(x, ldx, w, offsets, P, E, n, k, y, ldy, None)
+def _linear(x=FAKE, ldx=64, w=FAKE, offsets=FAKE, P=8, E=4, n=40, k=64, y=FAKE, ldy=40, ws=FAKE,
+            ws_bytes=1 << 30):
+    return X.lib().xshare_grouped_linear(x, ldx, w, offsets, P, E, n, k, y, ldy, ws, ws_bytes, None)
 
 
-def _linear_x(x=FAKE, ldx=64, w=FAKE, offsets=FAKE, P=8, E=4, n=64, k=40, y=FAKE, ldy=40):
-    return X.lib().xshare_grouped_linear_backward_x(x, ldx, w, offsets, P, E, n, k, y, ldy, None)
+def _linear_x(x=FAKE, ldx=64, w=FAKE, offsets=FAKE, P=8, E=4, n=64, k=40, y=FAKE, ldy=40, ws=FAKE,
+              ws_bytes=1 << 30):
+    return X.lib().xshare_grouped_linear_backward_x(x, ldx, w, offsets, P, E, n, k, y, ldy, ws,
+                                                    ws_bytes, None)
 
 
 def _linear_w(dy=FAKE, lddy=40, x=FAKE, ldx=64, offsets=FAKE, P=8, E=4, n=40, k=64, dw=FAKE, dtype=0,
-              accumulate=0):
+              accumulate=0, ws=FAKE, ws_bytes=1 << 30):
     return X.lib().xshare_grouped_linear_backward_w(dy, lddy, x, ldx, offsets, P, E, n, k, dw, dtype,
-                                                    accumulate, None)
+                                                    accumulate, ws, ws_bytes, None)
 
 
 SIZES = [(dict(P=-1), X.EINVAL), (dict(E=0), X.EINVAL), (dict(n=0), X.EINVAL), (dict(k=0), X.EINVAL),
          (dict(n=36), X.EINVAL), (dict(k=60), X.EINVAL), (dict(P=BIG), X.EUNSUPPORTED),
          (dict(E=1025), X.EUNSUPPORTED), (dict(n=BIG), X.EUNSUPPORTED), (dict(k=BIG), X.EUNSUPPORTED),
          (dict(offsets=None), X.EINVAL), (dict(offsets=ODD), X.EINVAL), (dict(x=None), X.EINVAL),
-         (dict(x=OFF8), X.EINVAL), (dict(ldx=32), X.EINVAL), (dict(ldx=68), X.EINVAL)]
+         (dict(x=OFF8), X.EINVAL), (dict(ldx=32), X.EINVAL), (dict(ldx=68), X.EINVAL),
+         (dict(P=256, ws=None), X.EWORKSPACE), (dict(P=256, ws_bytes=1 << 20), X.EWORKSPACE),
+         (dict(P=256, ws=OFF8), X.EINVAL)]
 
 
 @pytest.mark.parametrize("call", [_linear, _linear_x, _linear_w])
@@ -102,12 +107,13 @@ def test_products_refuse(call, kw, status):
 @pytest.mark.parametrize("call,kw,status", [
     (_linear, dict(w=None), X.EINVAL), (_linear, dict(w=OFF8), X.EINVAL),
     (_linear, dict(y=OFF8), X.EINVAL), (_linear, dict(ldy=44), X.EINVAL),
-    (_linear, dict(ldx=(1 << 23) + 8), X.EUNSUPPORTED), (_linear, dict(P=0, x=None), X.OK),
+    (_linear, dict(ldx=(1 << 22) + 8), X.EUNSUPPORTED), (_linear, dict(P=0, x=None), X.OK),
     (_linear_x, dict(w=OFF8), X.EINVAL), (_linear_x, dict(y=None), X.EINVAL),
-    (_linear_x, dict(ldx=(1 << 23) + 8), X.EUNSUPPORTED), (_linear_x, dict(P=0, x=None), X.OK),
+    (_linear_x, dict(ldx=(1 << 22) + 8), X.EUNSUPPORTED), (_linear_x, dict(P=0, x=None), X.OK),
     (_linear_w, dict(dy=None), X.EINVAL), (_linear_w, dict(lddy=32), X.EINVAL),
     (_linear_w, dict(dw=None), X.EINVAL), (_linear_w, dict(dw=OFF8), X.EINVAL),
-    (_linear_w, dict(dtype=2), X.EINVAL), (_linear_w, dict(dtype=1, accumulate=1), X.EUNSUPPORTED)])
+    (_linear_w, dict(ldx=(1 << 22) + 8), X.EUNSUPPORTED),
+    (_linear_w, dict(lddy=(1 << 22) + 8), X.EUNSUPPORTED), (_linear_w, dict(dtype=2), X.EINVAL), (_linear_w, dict(dtype=1, accumulate=1), X.EUNSUPPORTED)])
 def test_a_product_refuses(call, kw, status):
     assert call(**kw) == status
 
@@ -146,6 +152,10 @@ def test_adapters_backward_refuses(kw):
 def test_workspaces_serve_smaller_batches():
     a = [X.adapters_workspace_bytes(T, 5, 24, 400, 4096, True) for T in range(0, 9000, 37)]
     o = [X.expert_order_workspace_bytes(T, 8, 300) for T in range(0, 9000, 37)]
+    p = [X.grouped_linear_workspace_bytes(P, 8, 40, 64) for P in range(0, 9000, 37)]
+    assert p == sorted(p) and p[0] == 0 and p[-1] == 64 << 20
+    assert X.grouped_linear_workspace_bytes(4096, 8, 40, 60) == 0
+    assert X.grouped_linear_workspace_bytes(PAST, 8, 40, 64) == 0
     for sizes in (a, o):
         assert all(s > 0 and s % 256 == 0 for s in sizes) and sizes == sorted(sizes)
     # h and dh: three bf16 parts of 16, 32, 64 or 128 ranks a token
