@@ -731,8 +731,8 @@ xshare_status xshare_block_experts(const xshare_block_experts_args* args);
  * (XSHARE_EUNSUPPORTED beyond).  Every call gives the same bits again.                       *
  * ---------------------------------------------------------------------------------------- */
 
-/* Workspace of xshare_expert_order (bytes, 256-aligned); 0 for invalid sizes.  That of T tokens
- * serves any smaller T too.                                                                */
+/* Workspace of xshare_expert_order (bytes, 256-aligned); 0 where it needs none (T * top_k up to
+ * 8192) and for invalid sizes.  That of T tokens serves any smaller T too.                  */
 size_t xshare_expert_order_workspace_bytes(int32_t T, int32_t top_k, int32_t n_experts);
 
 /*
@@ -744,7 +744,7 @@ size_t xshare_expert_order_workspace_bytes(int32_t T, int32_t top_k, int32_t n_e
  *   rows     out [T, top_k] int32: each pair's row, or -1.
  *   pairs    out [T * top_k] int32: the pair t * top_k + r of each row; -1 from
  *            offsets[n_experts] on.
- *   ws       of xshare_expert_order_workspace_bytes, 16-byte aligned.
+ *   ws       of xshare_expert_order_workspace_bytes, 16-byte aligned; may be NULL where that is 0.
  */
 xshare_status xshare_expert_order(const int32_t* ids, int32_t T, int32_t top_k, int32_t n_experts,
                                   int32_t* offsets, int32_t* rows, int32_t* pairs, void* ws,

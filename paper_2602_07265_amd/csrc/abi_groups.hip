@@ -170,9 +170,11 @@ xshare_status xshare_expert_order(const int32_t* ids, int32_t T, int32_t top_k, 
   if (T > 0 && (!ids || !rows || !pairs || !aligned(ids, 4) || !aligned(rows, 4) ||
                 !aligned(pairs, 4)))
     return XSHARE_EINVAL;
-  if (!ws || ws_bytes < xs::order_bytes(T * top_k, n_experts)) return XSHARE_EWORKSPACE;
-  if (!aligned(ws, 16)) return XSHARE_EINVAL;
-  const xs::OrderArgs a{ids, T * top_k, n_experts, offsets, rows, pairs, at<int32_t>(ws, 0)};
+  const size_t need = xs::order_bytes(T * top_k, n_experts);
+  if (need > 0 && (!ws || ws_bytes < need)) return XSHARE_EWORKSPACE;
+  if (need > 0 && !aligned(ws, 16)) return XSHARE_EINVAL;
+  const xs::OrderArgs a{ids, T * top_k, n_experts, offsets, rows, pairs,
+                        static_cast<int32_t*>(ws)};
   return status_of(xs::launch_order(a, stream));
 }
 

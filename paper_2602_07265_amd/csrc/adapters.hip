@@ -86,32 +86,86 @@ __global__ __launch_bounds__(256) void few_expand_kernel(AdaptersArgs a, const f
   a.out[(size_t)t * a.ld_out + c] = to_bf16(y);
 }
 
-// ---------------------------------------------------------------------------- many tokens
-
-// Tokens without an adapter: out = base, or zeros.
-__global__ __launch_bounds__(256) void rest_kernel(AdaptersArgs a, int columns) {
-  const int t = blockIdx.x;
-  if (a.rows[t] >= 0) return;
-  for (int c = 8 * threadIdx.x; c < columns; c += 8 * 256) {
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (a.base) v = *reinterpret_cast<const uint4*>(a.base + (size_t)t * a.ld_base + c);
-    *reinterpret_cast<uint4*>(a.out + (size_t)t * a.ld_out + c) = v;
+// Both in one launch, for factors that every workgroup may read: workgroup (1024 columns, t) makes
+// token t's h for itself, a wave a value at a time, while the first values of B_e are under way.
+__global__ __launch_bounds__(1024) void few_kernel(AdaptersArgs a) {
+  constexpr int kAhead = 4;                            // of eight values of a row of B_e
+  __shared__ float hs[kMaxRank];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int t = blockIdx.y, c = blockIdx.x * 1024 + threadIdx.x;
+  const int e = a.ids[t];
+  const bool live = (unsigned)e < (unsigned)a.L;       // (the same for the whole workgroup)
+  const uint16_t* const row = a.b + ((size_t)(live ? e : 0) * a.n + min(c, a.n - 1)) * a.r;
+  uint4 ahead[kAhead];
+  float base = 0.0f, scale = 1.0f;
+  if (a.base && c < a.n) base = value(a.base[(size_t)t * a.ld_base + c]);
+  if (live) {
+    if (a.scales) scale = a.scales[e];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      ahead[i] = *reinterpret_cast<const uint4*>(row + (8 * i < a.r ? 8 * i : 0));
+    const uint16_t* const x = a.x + (size_t)t * a.ldx;
+    for (int j = wave; j < a.r; j += 16) {
+      const uint16_t* const w = a.a + ((size_t)e * a.r + j) * a.d;
+      float sum = 0.0f;
+#pragma unroll 8
+      for (int k = 8 * lane; k < a.d; k += 512) {
+        float p[8], q[8];
+        values8(*reinterpret_cast<const uint4*>(x + k), p);
+        values8(*reinterpret_cast<const uint4*>(w + k), q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(p[i], q[i], sum);
+      }
+      sum = wave_sum(sum);
+      if (lane == 0) hs[j] = sum;
+    }
   }
+  __syncthreads();
+  if (c >= a.n) return;
+  float y = 0.0f;
+  if (live) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (8 * i >= a.r) break;
+      float q[8];
+      values8(ahead[i], q);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) y = __builtin_fmaf(q[u], hs[8 * i + u], y);
+    }
+    for (int j = 8 * kAhead; j < a.r; j += 8) {
+      float q[8];
+      values8(*reinterpret_cast<const uint4*>(row + j), q);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) y = __builtin_fmaf(q[u], hs[j + u], y);
+    }
+  }
+  a.out[(size_t)t * a.ld_out + c] = to_bf16(live ? __builtin_fmaf(scale, y, base) : base);
 }
 
-// [rows, cols] of each adapter with tokens -> [cols, rows]; a thread takes eight rows of a column.
-__global__ __launch_bounds__(256) void transpose_kernel(const uint16_t* in, uint16_t* out, int rows,
-                                                        int cols, const int32_t* offsets) {
+// ---------------------------------------------------------------------------- many tokens
+
+// A matrix [rows, cols] of each adapter with tokens -> [cols, rows].
+struct Transposed {
+  const uint16_t* in;
+  uint16_t* out;
+  int rows, cols;
+  int groups() const { return (int)(((size_t)rows / 8 * cols + 255) / 256); }
+};
+// Both factors; a thread takes eight rows of a column.
+__global__ __launch_bounds__(256) void transpose_kernel(Transposed a, Transposed b, int groups_a,
+                                                        const int32_t* offsets) {
   const int e = blockIdx.y;
   if (offsets[e] == offsets[e + 1]) return;
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const int c = (int)(i % cols), r = (int)(i / cols) * 8;
-  if (r >= rows) return;
-  const size_t at = (size_t)e * rows * cols;
+  const bool first = (int)blockIdx.x < groups_a;
+  const Transposed m = first ? a : b;
+  const size_t i = (size_t)(first ? blockIdx.x : blockIdx.x - groups_a) * 256 + threadIdx.x;
+  const int c = (int)(i % m.cols), r = (int)(i / m.cols) * 8;
+  if (r >= m.rows) return;
+  const size_t at = (size_t)e * m.rows * m.cols;
   uint32_t v[8];
 #pragma unroll
-  for (int q = 0; q < 8; ++q) v[q] = in[at + (size_t)(r + q) * cols + c];
-  *reinterpret_cast<uint4*>(out + at + (size_t)c * rows + r) =
+  for (int q = 0; q < 8; ++q) v[q] = m.in[at + (size_t)(r + q) * m.cols + c];
+  *reinterpret_cast<uint4*>(m.out + at + (size_t)c * m.rows + r) =
       make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
@@ -126,62 +180,70 @@ __device__ __forceinline__ void split3(float v, uint16_t (&p)[3]) {
 }
 
 struct Shrink {
-  const int32_t* offsets;
-  const int32_t* tokens;
-  int L, T, r, K;
   const uint16_t* x;           // [T, K]
   long ldx;
+  int K;
   const uint16_t* w;           // [L, r, K]
   const float* scales;         // [L], or null
   uint16_t* h;                 // [T, 3, 16 JT]
 };
+struct Tokens {                // in adapters' order
+  const int32_t* offsets;
+  const int32_t* tokens;
+  int L, T, r;
+};
 
-// h of 16 MT tokens of one adapter: the waves take blocks of 64 of the reduction in turn, operands
-// straight from memory, and their sums meet in LDS.
+// h of 16 MT tokens of one adapter: the waves take blocks of 64 of the reduction in turn, kAhead of
+// them at a time, operands straight from memory, and their sums meet in LDS.  The first `groups`
+// workgroups have one product's tiles, the others another's (x and A, dy and B transposed).
 template <int MT, int JT>
-__global__ __launch_bounds__(512) void shrink_kernel(Shrink a) {
-  constexpr int kWaves = 8;
+__global__ __launch_bounds__(512) void shrink_kernel(Tokens o, Shrink first_a, Shrink second,
+                                                     int groups) {
+  constexpr int kWaves = 8, kAhead = JT == 1 ? 4 : JT <= 4 ? 2 : 1;
   extern __shared__ floatx4 sums[];                    // [kWaves][MT JT][64]
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
+  const bool is_first = (int)blockIdx.x < groups;
+  const Shrink a = is_first ? first_a : second;
   Place p;
-  if (!find_place(a.offsets, a.L, a.T, 16 * MT, 1, p)) return;
+  if (!find_place(o.offsets, o.L, o.T, 16 * MT, 1, is_first ? blockIdx.x : blockIdx.x - groups, p))
+    return;
   const int e = p.e, first = p.first, live = p.live;
   const uint16_t* x[MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int token = a.tokens[first + min(16 * t + n, live - 1)];
-    x[t] = a.x + (size_t)token * a.ldx;
-  }
+  for (int t = 0; t < MT; ++t)
+    x[t] = a.x + (size_t)o.tokens[first + min(16 * t + n, live - 1)] * a.ldx;
   const uint16_t* w[JT];
 #pragma unroll
   for (int j = 0; j < JT; ++j)
-    w[j] = a.w + ((size_t)e * a.r + min(16 * j + n, a.r - 1)) * a.K;
+    w[j] = a.w + ((size_t)e * o.r + min(16 * j + n, o.r - 1)) * a.K;
   floatx4 acc[JT][MT];
 #pragma unroll
   for (int j = 0; j < JT; ++j)
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[j][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  for (int k0 = 64 * wave; k0 < a.K; k0 += 64 * kWaves) {
+  for (int k0 = 64 * kAhead * wave; k0 < a.K; k0 += 64 * kAhead * kWaves) {
+    uint4 fx[2 * kAhead][MT], fw[2 * kAhead][JT];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < 2 * kAhead; ++s) {
       const int k = k0 + 32 * s + 8 * g;
       const bool in = k < a.K;
-      uint4 fx[MT], fw[JT];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) fx[t] = in ? *reinterpret_cast<const uint4*>(x[t] + k) : zero;
+      for (int t = 0; t < MT; ++t) fx[s][t] = in ? *reinterpret_cast<const uint4*>(x[t] + k) : zero;
 #pragma unroll
-      for (int j = 0; j < JT; ++j) fw[j] = in ? *reinterpret_cast<const uint4*>(w[j] + k) : zero;
+      for (int j = 0; j < JT; ++j) fw[s][j] = in ? *reinterpret_cast<const uint4*>(w[j] + k) : zero;
+    }
+#pragma unroll
+    for (int s = 0; s < 2 * kAhead; ++s)
 #pragma unroll
       for (int j = 0; j < JT; ++j)
 #pragma unroll
         for (int t = 0; t < MT; ++t)
           acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              __builtin_bit_cast(bf16x8, fw[j]), __builtin_bit_cast(bf16x8, fx[t]), acc[j][t], 0, 0,
-              0);
-    }
+              __builtin_bit_cast(bf16x8, fw[s][j]), __builtin_bit_cast(bf16x8, fx[s][t]), acc[j][t],
+              0, 0, 0);
   }
 #pragma unroll
   for (int j = 0; j < JT; ++j)
@@ -198,7 +260,7 @@ __global__ __launch_bounds__(512) void shrink_kernel(Shrink a) {
     uint16_t parts[4][3];
 #pragma unroll
     for (int c = 0; c < 4; ++c)                        // (past the rank: zeros)
-      split3(16 * j + 4 * g + c < a.r ? v[c] * s : 0.0f, parts[c]);
+      split3(16 * j + 4 * g + c < o.r ? v[c] * s : 0.0f, parts[c]);
     uint16_t* const out = a.h + (size_t)(first + 16 * t + n) * (48 * JT) + 16 * j + 4 * g;
 #pragma unroll
     for (int q = 0; q < 3; ++q)
@@ -209,9 +271,8 @@ __global__ __launch_bounds__(512) void shrink_kernel(Shrink a) {
 }
 
 struct Expand {
-  const int32_t* offsets;
-  const int32_t* tokens;
-  int L, T, r, N;
+  const int32_t* rows;         // [T]
+  int N;
   const uint16_t* h;           // [T, 3, 16 JT]
   const uint16_t* w;           // [L, N, r]
   const float* scales;         // [L], or null
@@ -221,17 +282,37 @@ struct Expand {
   long ld_out;
 };
 constexpr int kExpandColumns = 512;    // of a workgroup
+constexpr int kRestTokens = 64;        // (lanes) of a workgroup that looks for tokens without an adapter
+
+// Tokens without an adapter, of kRestTokens from the first on: out = base, or zeros.
+__device__ __forceinline__ void copy_rest(const Expand& a, int T, int first) {
+  const int lane = threadIdx.x & 63;
+  const bool dead = first + lane < T && a.rows[min(first + lane, T - 1)] < 0;
+  for (uint64_t left = __ballot(dead); left; left &= left - 1) {   // (every wave sees the same)
+    const size_t t = first + __builtin_ctzll(left);
+    for (int c = 8 * threadIdx.x; c < a.N; c += 8 * 256) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (a.base) v = *reinterpret_cast<const uint4*>(a.base + t * a.ld_base + c);
+      *reinterpret_cast<uint4*>(a.out + t * a.ld_out + c) = v;
+    }
+  }
+}
 
 // out of 16 MT tokens of one adapter and kExpandColumns columns: each wave takes 32 of these at a
-// time, dealt so that a lane's eight results are neighbours.
+// time, dealt so that a lane's eight results are neighbours.  Workgroups from `groups` on look after the
+// tokens without an adapter.
 template <int MT, int JT>
-__global__ __launch_bounds__(256) void expand_kernel(Expand a) {
+__global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int groups) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
+  if ((int)blockIdx.x >= groups) {
+    copy_rest(a, o.T, (blockIdx.x - groups) * kRestTokens);
+    return;
+  }
   Place p;
   const int columns = (a.N + kExpandColumns - 1) / kExpandColumns;
-  if (!find_place(a.offsets, a.L, a.T, 16 * MT, columns, p)) return;
+  if (!find_place(o.offsets, o.L, o.T, 16 * MT, columns, blockIdx.x, p)) return;
   const int e = p.e, first = p.first, live = p.live;
   const int c0 = p.column * kExpandColumns;
   long token[MT];
@@ -239,13 +320,13 @@ __global__ __launch_bounds__(256) void expand_kernel(Expand a) {
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const int row = first + min(16 * t + n, live - 1);
-    token[t] = a.tokens[row];
+    token[t] = o.tokens[row];
 #pragma unroll
     for (int s = 0; s < JT; ++s)
       fh[t][s] = *reinterpret_cast<const bf16x8*>(a.h + (size_t)row * (48 * JT) + 32 * s + 8 * g);
   }
   const float scale = a.scales ? a.scales[e] : 1.0f;
-  const uint16_t* const w = a.w + (size_t)e * a.N * a.r;
+  const uint16_t* const w = a.w + (size_t)e * a.N * o.r;
   const int end = min(c0 + kExpandColumns, a.N);
   const uint4 zero = make_uint4(0, 0, 0, 0);
   for (int c = c0 + 32 * wave; c < end; c += 128) {
@@ -260,7 +341,7 @@ __global__ __launch_bounds__(256) void expand_kernel(Expand a) {
         // the first two parts of h lie one behind the other: W's row goes with both
         const int j = (32 * s + 8 * g) % (16 * JT);
         const uint4 v =
-            j < a.r ? *reinterpret_cast<const uint4*>(w + (size_t)col * a.r + j) : zero;
+            j < o.r ? *reinterpret_cast<const uint4*>(w + (size_t)col * o.r + j) : zero;
 #pragma unroll
         for (int t = 0; t < MT; ++t)
           acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v),
@@ -453,25 +534,27 @@ hipError_t allow_lds(K kernel, int bytes) {
                              hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
-hipError_t launch_shrink(const Shrink& s, hipStream_t stream) {
-  return by_rank(s.r, [&](auto j) {
+// One product, or two in one launch.
+hipError_t launch_shrink(const Tokens& o, const Shrink& a, const Shrink* b, hipStream_t stream) {
+  return by_rank(o.r, [&](auto j) {
     constexpr int JT = decltype(j)::value, MT = JT >= 4 ? 2 : 1;
     constexpr int kBytes = 8 * MT * JT * 64 * 16;
     const auto kernel = shrink_kernel<MT, JT>;
     const hipError_t e = allow_lds(kernel, kBytes);
     if (e != hipSuccess) return e;
-    kernel<<<(unsigned)most_tiles(s.T, s.L, 16 * MT, 1), 512, kBytes, stream>>>(s);
+    const int groups = (int)most_tiles(o.T, o.L, 16 * MT, 1);
+    kernel<<<b ? 2 * groups : groups, 512, kBytes, stream>>>(o, a, b ? *b : a, groups);
     return hipGetLastError();
   });
 }
 
-hipError_t launch_expand(const Expand& x, hipStream_t stream) {
-  return by_rank(x.r, [&](auto j) {
+hipError_t launch_expand(const Tokens& o, const Expand& x, hipStream_t stream) {
+  return by_rank(o.r, [&](auto j) {
     constexpr int JT = decltype(j)::value, MT = 2;
-    const long columns = (x.N + kExpandColumns - 1) / kExpandColumns;
-    const long grid = most_tiles(x.T, x.L, 16 * MT, columns);
-    if (grid * 256 > 0xFFFFFFFFl) return hipErrorInvalidConfiguration;
-    expand_kernel<MT, JT><<<(unsigned)grid, 256, 0, stream>>>(x);
+    const long groups = most_tiles(o.T, o.L, 16 * MT, (x.N + kExpandColumns - 1) / kExpandColumns);
+    const long rest = x.out == x.base ? 0 : (o.T + kRestTokens - 1) / kRestTokens;
+    if ((groups + rest) * 256 > 0xFFFFFFFFl) return hipErrorInvalidConfiguration;
+    expand_kernel<MT, JT><<<(unsigned)(groups + rest), 256, 0, stream>>>(o, x, (int)groups);
     return hipGetLastError();
   });
 }
@@ -500,6 +583,10 @@ hipError_t in_order(const AdaptersArgs& a, hipStream_t stream) {
 
 hipError_t launch_adapters(const AdaptersArgs& a, hipStream_t stream) {
   if (a.T <= kAdapterFew) {
+    if ((long)a.T * ((a.n + 1023) / 1024) * a.r * a.d <= kAdapterOne) {
+      few_kernel<<<dim3((a.n + 1023) / 1024, a.T), 1024, 0, stream>>>(a);
+      return hipGetLastError();
+    }
     float* const h = reinterpret_cast<float*>(a.h);    // (fp32 [T, r] in the place of three parts)
     few_shrink_kernel<<<dim3((a.r + 3) / 4, a.T), 256, 0, stream>>>(a, h);
     few_expand_kernel<<<dim3((a.n + 255) / 256, a.T), 256, 0, stream>>>(a, h);
@@ -507,30 +594,27 @@ hipError_t launch_adapters(const AdaptersArgs& a, hipStream_t stream) {
   }
   hipError_t e = in_order(a, stream);
   if (e != hipSuccess) return e;
-  const Shrink s{a.offsets, a.tokens, a.L, a.T, a.r, a.d, a.x, a.ldx, a.a, nullptr, a.h};
-  if ((e = launch_shrink(s, stream)) != hipSuccess) return e;
-  if (a.out != a.base) rest_kernel<<<a.T, 256, 0, stream>>>(a, a.n);
-  const Expand x{a.offsets, a.tokens, a.L, a.T, a.r, a.n, a.h, a.b, a.scales,
-                 a.base, a.ld_base, a.out, a.ld_out};
-  return launch_expand(x, stream);
+  const Tokens o{a.offsets, a.tokens, a.L, a.T, a.r};
+  if ((e = launch_shrink(o, {a.x, a.ldx, a.d, a.a, nullptr, a.h}, nullptr, stream)) != hipSuccess)
+    return e;
+  return launch_expand(
+      o, {a.rows, a.n, a.h, a.b, a.scales, a.base, a.ld_base, a.out, a.ld_out}, stream);
 }
 
 hipError_t launch_adapters_backward(const AdaptersArgs& a, hipStream_t stream) {
   hipError_t e = in_order(a, stream);
   if (e != hipSuccess) return e;
-  transpose_kernel<<<dim3((unsigned)(((size_t)a.r / 8 * a.d + 255) / 256), a.L), 256, 0, stream>>>(
-      a.a, a.at, a.r, a.d, a.offsets);
-  transpose_kernel<<<dim3((unsigned)(((size_t)a.n / 8 * a.r + 255) / 256), a.L), 256, 0, stream>>>(
-      a.b, a.bt, a.n, a.r, a.offsets);
   if (a.T > 0) {
-    const Shrink s{a.offsets, a.tokens, a.L, a.T, a.r, a.d, a.x, a.ldx, a.a, nullptr, a.h};
-    if ((e = launch_shrink(s, stream)) != hipSuccess) return e;
-    const Shrink g{a.offsets, a.tokens, a.L, a.T, a.r, a.n, a.dy, a.lddy, a.bt, a.scales, a.dh};
-    if ((e = launch_shrink(g, stream)) != hipSuccess) return e;
-    if (a.out != a.base) rest_kernel<<<a.T, 256, 0, stream>>>(a, a.d);
-    const Expand x{a.offsets, a.tokens, a.L, a.T, a.r, a.d, a.dh, a.at, nullptr,
-                   a.base, a.ld_base, a.out, a.ld_out};
-    if ((e = launch_expand(x, stream)) != hipSuccess) return e;
+    const Tokens o{a.offsets, a.tokens, a.L, a.T, a.r};
+    const Transposed ta{a.a, a.at, a.r, a.d}, tb{a.b, a.bt, a.n, a.r};
+    transpose_kernel<<<dim3(ta.groups() + tb.groups(), a.L), 256, 0, stream>>>(ta, tb, ta.groups(),
+                                                                              a.offsets);
+    const Shrink g{a.dy, a.lddy, a.n, a.bt, a.scales, a.dh};
+    if ((e = launch_shrink(o, {a.x, a.ldx, a.d, a.a, nullptr, a.h}, &g, stream)) != hipSuccess)
+      return e;
+    e = launch_expand(o, {a.rows, a.d, a.dh, a.at, nullptr, a.base, a.ld_base, a.out, a.ld_out},
+                      stream);
+    if (e != hipSuccess) return e;
   }
   const size_t na = (size_t)a.L * a.r * a.d, nb = (size_t)a.L * a.r * a.n;
   const bool parts = a.splits > 1;

@@ -77,7 +77,7 @@ __host__ __device__ inline Shares shares_of(long tiles, int reduction) {
 }
 template <Kind kKind>
 __device__ __forceinline__ int common_reduction(const Product& p) {
-  return kKind == kGradW ? p.P / p.E + 1 : p.reduction;
+  return kKind == kGradW ? p.P / p.E : p.reduction;
 }
 
 template <Kind kKind, int BA, int BB>
@@ -517,72 +517,70 @@ hipError_t launch_turns(Product a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// The forms of a product: its tile, and what 64 of the reduction cost in microseconds, `few` with
-// little else on the GPU, `full` for each tile that every compute unit has to work on.  Measured over
-// 1 to 64 groups of 1 to 4096 rows by four shapes of 512 to 4096; of 109 cases the choice came within
-// 10 % of the best form on 98 (forward) and 93 (dx), 3 and 4 % above it on average.
+// The forms of a product: its tile, and what it costs in microseconds: 64 of the reduction, `few` with
+// little else on the GPU, `full` for each tile that every compute unit has to work on, and `out`, a
+// tile's stores where the outputs are what is written most (fp32 dW).  Measured over 1 to 64 groups of
+// 1 to 4096 rows by four shapes of 512 to 4096; of 109 cases the choice came within 10 % of the best
+// form on 98 (forward) and 93 (dx), 3 and 4 % above it on average.
+enum Units { kShared, kAlone, kSplit };  // tiles of a unit: several, one, one and the last round split
 struct Form {
   int columns, rows;
-  float few, full;
+  float few, full, out;
+  Units units;
   hipError_t (*launch)(Product, hipStream_t);
-  bool turns;                  // turns_kernel, which splits what is left of a last round
 };
 const Form kForwardForms[] = {
-    {64, 32, 0.185f, 0.145f, launch_tile<kForward, 64, 32, 4, 1, 4>, false},
-    {64, 64, 0.23f, 0.205f, launch_tile<kForward, 64, 64, 2, 2, 3>, false},
-    {128, 64, 0.30f, 0.34f, launch_tile<kForward, 128, 64, 2, 2, 3>, false},
-    {256, 256, 1.07f, 1.5f, launch_turns<kForward>, true},
+    {64, 32, 0.185f, 0.145f, 0.0f, kShared, launch_tile<kForward, 64, 32, 4, 1, 4>},
+    {64, 64, 0.23f, 0.205f, 0.0f, kShared, launch_tile<kForward, 64, 64, 2, 2, 3>},
+    {128, 64, 0.30f, 0.34f, 0.0f, kShared, launch_tile<kForward, 128, 64, 2, 2, 3>},
+    {256, 256, 1.07f, 1.5f, 0.0f, kSplit, launch_turns<kForward>},
 };
 const Form kGradXForms[] = {
-    {64, 32, 0.225f, 0.145f, launch_tile<kGradX, 64, 32, 4, 1, 4>, false},
-    {64, 64, 0.25f, 0.205f, launch_tile<kGradX, 64, 64, 2, 2, 3>, false},
-    {128, 64, 0.38f, 0.33f, launch_tile<kGradX, 128, 64, 2, 2, 3>, false},
-    {128, 128, 0.52f, 0.68f, launch_tile<kGradX, 128, 128, 2, 2, 3>, false},
-    {256, 256, 1.35f, 1.7f, launch_turns<kGradX>, true},
+    {64, 32, 0.225f, 0.145f, 0.0f, kShared, launch_tile<kGradX, 64, 32, 4, 1, 4>},
+    {64, 64, 0.25f, 0.205f, 0.0f, kShared, launch_tile<kGradX, 64, 64, 2, 2, 3>},
+    {128, 64, 0.38f, 0.33f, 0.0f, kShared, launch_tile<kGradX, 128, 64, 2, 2, 3>},
+    {256, 256, 1.35f, 1.7f, 0.0f, kSplit, launch_turns<kGradX>},
 };
-// Outputs of many tiles are bound by writing them: with 96 rows a group or more on average in tiles of
-// 256 x 256 (128 groups' 256 rows by 1536 x 2048 in 544 us, 607 in tiles of 128 x 128), with fewer in
-// these (64 groups' 4 rows by 4096 x 4096 in 686 us, 789 in the others).
 const Form kGradWForms[] = {
-    {128, 64, 0.60f, 0.42f, launch_tile<kGradW, 128, 64, 2, 2, 3, 32>, false},
-    {128, 128, 0.82f, 0.64f, launch_tile<kGradW, 128, 128, 2, 2, 3, 32>, false},
-    {256, 256, 1.30f, 1.65f, launch_turns<kGradW>, true},
+    {128, 64, 0.60f, 0.42f, 1.4f, kShared, launch_tile<kGradW, 128, 64, 2, 2, 3, 32>},
+    {128, 128, 0.82f, 0.64f, 2.8f, kShared, launch_tile<kGradW, 128, 128, 2, 2, 3, 32>},
+    {256, 256, 1.30f, 1.5f, 12.5f, kAlone, launch_tile<kGradW, 256, 256, 2, 4, 4, 32>},
+    {256, 256, 1.30f, 1.65f, 12.5f, kSplit, launch_turns<kGradW>},
 };
-constexpr int kManyTiles = 1024;       // of 256 x 256
-constexpr int kWritten = 96;
 
 float form_cost(const Form& f, float tiles, int reduction) {
   const float blocks = (float)((reduction + kBlock - 1) / kBlock);
-  if (!f.turns) {
-    const float round = tiles / kUnits;
-    const float some = f.few + (f.full > f.few ? (f.full - f.few) * (round < 1 ? round : 1) : 0);
-    return blocks * (f.full * round > some ? f.full * round : some);
+  if (f.units == kShared) {
+    const float round = tiles / kUnits, full = blocks * f.full + f.out;
+    float some = blocks * f.few;
+    if (full > some) some += (full - some) * (round < 1 ? round : 1);
+    return full * round > some ? full * round : some;
   }
-  const Shares s = shares_of((long)(tiles + 0.999f), reduction);
+  Shares s{(long)(tiles + 0.999f), 0, 1};
+  if (f.units == kSplit) s = shares_of(s.whole, reduction);
   const long rounds = (s.whole + kUnits - 1) / kUnits;
-  float cost = rounds * f.full;
-  const int left = (int)(s.whole - (rounds - 1) * kUnits);
-  if (rounds > 0) cost -= (f.full - f.few) * (1.0f - (float)left / kUnits);
-  if (s.rest == 0) return blocks * cost;
+  const int left = (int)(s.whole - (rounds - 1) * kUnits);       // tiles of the last whole round
+  float cost = rounds * (blocks * f.full + f.out);
+  if (rounds > 0) cost -= (blocks * (f.full - f.few) + f.out) * (1.0f - (float)left / kUnits);
+  if (s.rest == 0) return cost;
   const int more = s.rest * s.parts;                   // parts, each written and read again
-  cost += (f.few + (f.full - f.few) * more / kUnits) / s.parts;
-  return blocks * cost + 4.0f + 0.1f * more;
+  return cost + blocks * (f.few + (f.full - f.few) * more / kUnits) / s.parts + 4.0f + 0.1f * more;
 }
 
 template <int N>
-const Form& form_for(const Form (&forms)[N], const Product& a, int groups, float mean,
-                     int reduction) {
+const Form& form_for(const Form (&forms)[N], const Product& a, int groups, int reduction) {
   int best = 0;
   float least = 0;
   for (int i = 0; i < N; ++i) {
     const Form& f = forms[i];
-    if (f.turns && a.P < kTurnsRows) continue;
+    if (f.units == kSplit && a.P < kTurnsRows) continue;
     const int columns = (a.columns + f.columns - 1) / f.columns;
-    // a group's last tile is half full on average (one group's size is known)
+    // the rows of dW, or of groups: their last tile is half full on average (one's size is known)
+    const float mean = (float)a.P / groups;
     const float rows = a.out_rows ? (float)((a.out_rows + f.rows - 1) / f.rows)
                        : groups == 1 ? (float)((a.P + f.rows - 1) / f.rows)
                        : mean > 1 ? mean / f.rows + 0.5f : 1.0f;
-    const float cost = form_cost(f, groups * columns * (rows > 1 ? rows : 1.0f), reduction);
+    const float cost = form_cost(f, (float)groups * columns * (rows > 1 ? rows : 1.0f), reduction);
     if (i == 0 || cost < least) {
       best = i;
       least = cost;
@@ -605,7 +603,7 @@ Product product_of(const GroupedArgs& g) {
 template <int N>
 hipError_t launch_rows(const Form (&forms)[N], const Product& a, hipStream_t stream) {
   const int groups = a.P < a.E ? a.P : a.E;
-  return form_for(forms, a, groups, (float)a.P / groups, a.reduction).launch(a, stream);
+  return form_for(forms, a, groups, a.reduction).launch(a, stream);
 }
 
 }  // namespace
@@ -641,12 +639,8 @@ hipError_t launch_grouped_backward_w(const GroupedArgs& g, hipStream_t stream) {
   a.dw = g.dw;
   a.dw_fp32 = g.dw_fp32;
   a.accumulate = g.accumulate;
-  const float mean = (float)a.P / a.E;
-  const long tiles = (long)a.E * ((a.columns + 255) / 256) * ((a.out_rows + 255) / 256);
-  if (tiles >= kManyTiles)
-    return mean >= kWritten ? launch_tile<kGradW, 256, 256, 2, 4, 4, 32>(a, stream)
-                            : launch_tile<kGradW, 128, 128, 2, 2, 3, 32>(a, stream);
-  return form_for(kGradWForms, a, a.E, mean, (int)mean + 1).launch(a, stream);
+  const int mean = a.P / a.E;
+  return form_for(kGradWForms, a, a.E, mean > 0 ? mean : 1).launch(a, stream);
 }
 
 }  // namespace xs

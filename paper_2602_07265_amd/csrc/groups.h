@@ -30,8 +30,7 @@ inline int order_parts(int pairs) {
   return pairs <= kOrderOne ? 0 : (pairs + kOrderPart - 1) / kOrderPart;
 }
 inline size_t order_bytes(int pairs, int E) {
-  const size_t b = align256(sizeof(int32_t) * size_t(order_parts(pairs)) * E);
-  return b > 0 ? b : 256;
+  return align256(sizeof(int32_t) * size_t(order_parts(pairs)) * E);
 }
 hipError_t launch_order(const OrderArgs& a, hipStream_t stream);
 
@@ -83,8 +82,11 @@ hipError_t launch_grouped_backward_w(const GroupedArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------------------- adapters
 
-// Tokens up to which an adapters call goes token by token in two launches, without an order.
+// Tokens up to which an adapters call goes token by token, without an order; in one launch where its
+// workgroups read no more values of A than this (each a whole A_e: one token of n = d = 4096, r = 16
+// in 4.9 us, 4.3 + 3.2 in two launches; 45 of n = 2048, d = 7168, r = 32 in 19.5, 5.8 + 3.2 in two).
 constexpr int kAdapterFew = 64;
+constexpr int kAdapterOne = 1 << 20;
 // Values of a row of h: the ranks of the kernels' instances, which have 1, 2, 4 or 8 tiles of 16.
 inline int padded_rank(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
 
@@ -93,7 +95,7 @@ constexpr int kGradColumns = 128;      // columns of x or dy of a workgroup
 inline int adapter_splits(int T, int L, int n, int d) {
   const long groups = long(L) * ((n + kGradColumns - 1) / kGradColumns +
                                  (d + kGradColumns - 1) / kGradColumns);
-  const long want = 768 / groups, most = (T + 255) / 256;
+  const long want = 511 / groups, most = (T + 255) / 256;
   const long n_parts = want < most ? want : most;
   return n_parts < 1 ? 1 : int(n_parts);
 }

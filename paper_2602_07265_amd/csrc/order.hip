@@ -20,6 +20,13 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 
+// What a lane wrote to the wave's part of LDS before this, its other lanes read after it (the wave's
+// LDS operations are done in order; the compiler keeps that order here).
+__device__ __forceinline__ void lanes_meet() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // The lanes whose key (of `bits` bits) is this lane's.
 __device__ __forceinline__ uint64_t same_key(int key, int bits) {
   uint64_t m = ~0ull;
@@ -36,32 +43,53 @@ __device__ __forceinline__ int lower_lanes(uint64_t m) {
                                    __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
 }
 
-// Pairs first .. first + len - 1 of the workgroup, dealt to its waves in runs: next[w][e] becomes
-// the row of the first pair of expert e in run w.  before: per expert, the pairs of earlier
-// workgroups (already added to the experts' first rows), or null.
-struct Runs {
-  int first, last, step;       // of this wave
-  __device__ __forceinline__ Runs(int begin, int end, int wave) {
-    step = ((end - begin + kWaves - 1) / kWaves + 63) / 64 * 64;
-    first = min(begin + wave * step, end);
-    last = min(first + step, end);
-  }
-};
-
 __device__ __forceinline__ int key_of(const OrderArgs& a, int i, int end) {
   const int id = i < end ? a.ids[i] : -1;
   return (unsigned)id < (unsigned)a.E ? id : a.E;      // E: no expert
 }
 
-// Per expert and wave the number of pairs in the wave's run.
-__device__ __forceinline__ void count_runs(const OrderArgs& a, const Runs& run, int* mine,
-                                           int lane) {
-  for (int e = lane; e < a.E; e += 64) mine[e] = 0;
-  for (int i = run.first; i < run.last; i += 64) {
-    const int key = key_of(a, i + lane, run.last);
-    if (key < a.E) atomicAdd(&mine[key], 1);           // (sums of ones: in any order)
+// The run of consecutive pairs of a wave among those that its workgroup sorts, and each pair's place
+// among its expert's in the run, of which it keeps the counts.
+struct Run {
+  static constexpr int kSteps = kOrderOne / kThreads;  // of 64 pairs, at most
+  int first, last;
+  int key[kSteps], rank[kSteps];
+
+  __device__ __forceinline__ Run(int begin, int end, int wave) {
+    const int step = ((end - begin + kWaves - 1) / kWaves + 63) / 64 * 64;
+    first = min(begin + wave * step, end);
+    last = min(first + step, end);
   }
-}
+  // counts [E]: the wave's own
+  __device__ __forceinline__ void count(const OrderArgs& a, int* counts, int bits, int lane) {
+    for (int e = lane; e < a.E; e += 64) counts[e] = 0;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) key[s] = key_of(a, first + 64 * s + lane, last);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      if (first + 64 * s >= last) break;
+      lanes_meet();                                    // a step reads what the last one wrote
+      const uint64_t same = same_key(key[s], bits);
+      const int lower = lower_lanes(same);
+      const bool live = key[s] < a.E;
+      const int before = live ? counts[key[s]] : 0;
+      rank[s] = before + lower;
+      lanes_meet();                                    // all lanes read before one writes
+      if (live && lower == 0) counts[key[s]] = before + __popcll(same);
+    }
+  }
+  // next [E]: the row of the run's first pair of each expert
+  __device__ __forceinline__ void place(const OrderArgs& a, const int* next, int lane) const {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int p = first + 64 * s + lane;
+      if (p >= last) break;
+      const int row = key[s] < a.E ? next[key[s]] + rank[s] : -1;
+      a.rows[p] = row;
+      if (row >= 0) a.pair_of[row] = p;
+    }
+  }
+};
 
 // Exclusive sum of v over the threads of the workgroup; `total` the sum of all.
 __device__ __forceinline__ int block_scan(int v, int* part, int& total) {
@@ -80,26 +108,6 @@ __device__ __forceinline__ int block_scan(int v, int* part, int& total) {
   return before + upto - v;
 }
 
-// Places the wave's run; next[e]: the row of its next pair of expert e.
-__device__ __forceinline__ void place_runs(const OrderArgs& a, const Runs& run, int* next, int bits,
-                                           int lane) {
-  for (int i = run.first; i < run.last; i += 64) {
-    const int p = i + lane;
-    const int key = key_of(a, p, run.last);
-    const uint64_t same = same_key(key, bits);
-    const int rank = lower_lanes(same);
-    const bool live = key < a.E;
-    const int row = live ? next[key] + rank : -1;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // all lanes read before one writes
-    __builtin_amdgcn_wave_barrier();
-    if (live && rank == 0) next[key] = row + __popcll(same);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if (p < run.last) a.rows[p] = row;
-    if (live) a.pair_of[row] = p;
-  }
-}
-
 // The whole sort (kParts false), or the second launch of two: part blockIdx.x of the pairs, whose
 // counts[part][e] the first launch wrote.
 template <bool kParts>
@@ -109,9 +117,9 @@ __global__ __launch_bounds__(kThreads) void order_kernel(OrderArgs a, int part_s
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int begin = kParts ? blockIdx.x * part_size : 0;
   const int end = kParts ? min(begin + part_size, a.pairs) : a.pairs;
-  const Runs run(begin, end, wave);
+  Run run(begin, end, wave);
   int* const mine = lds + wave * a.E;
-  count_runs(a, run, mine, lane);
+  run.count(a, mine, bits, lane);
   // thread e: expert e's pairs in all parts and in those before this one
   int all = 0, before = 0;
   if (kParts && tid < a.E) {
@@ -139,7 +147,7 @@ __global__ __launch_bounds__(kThreads) void order_kernel(OrderArgs a, int part_s
   }
   if (tid == 0 && (!kParts || blockIdx.x == 0)) a.offsets[a.E] = total;
   __syncthreads();
-  place_runs(a, run, mine, bits, lane);
+  run.place(a, mine, lane);
   // rows past the last expert's hold no pair
   for (int p = max(total, begin) + tid; p < end; p += kThreads) a.pair_of[p] = -1;
 }

@@ -110,12 +110,12 @@ __device__ __forceinline__ bool place_of(const int32_t* offsets, int E, int P, i
   }
   return false;
 }
-// The tile of this workgroup, of `columns` column tiles of every row tile of `tile` rows; false where
+// The tile of workgroup i, of `columns` column tiles of every row tile of `tile` rows; false where
 // there is none for it (the grid is an upper bound).
 __device__ __forceinline__ bool find_place(const int32_t* offsets, int E, int P, int tile, int columns,
-                                           Place& p) {
+                                           int i, Place& p) {
   const RowTiles c = count_row_tiles(offsets, E, P, tile);
-  const long at = piece_of(blockIdx.x, (long)c.total * columns);
+  const long at = piece_of(i, (long)c.total * columns);
   return at >= 0 && place_of(offsets, E, P, tile, columns, c, at, p);
 }
 

@@ -1342,14 +1342,16 @@ def expert_order(ids: torch.Tensor, n_experts: int, *, out=None, workspace=None,
             res[name] = ids.new_empty(shape)
         else:
             _fit(dev, (res[name], torch.int32, shape, name))
-    if workspace is None:
-        size = L.xshare_expert_order_workspace_bytes(T, k, N)
-        workspace = ids.new_empty(size, dtype=torch.uint8)
-    else:
+    if workspace is not None:
         size = _workspace(dev, workspace)
+    else:
+        size = L.xshare_expert_order_workspace_bytes(T, k, N)
+        if size:
+            workspace = ids.new_empty(size, dtype=torch.uint8)
     st = L.xshare_expert_order(ids.data_ptr(), T, k, N, res["offsets"].data_ptr(),
                                res["rows"].data_ptr(), res["pairs"].data_ptr(),
-                               workspace.data_ptr(), size, _stream_of(ids, stream))
+                               None if workspace is None else workspace.data_ptr(), size,
+                               _stream_of(ids, stream))
     _check(st, "xshare_expert_order")
     return res
 

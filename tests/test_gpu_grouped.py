@@ -40,10 +40,6 @@ CASES = [([1], 8, 8), ([1] * 8, 1536, 2048), ([0, 3, 0, 0, 1], 40, 72), ([24], 5
          ([40, 90, 0, 160], 384, 320)]
 
 
-def _counts(name):
-    return CASES[name]
-
-
 @pytest.mark.parametrize("case", range(len(CASES)))
 @pytest.mark.parametrize("lead,tail,pad", [(0, 0, 0), (3, 130, 8)])
 def test_products(case, lead, tail, pad):
@@ -71,6 +67,86 @@ def test_products(case, lead, tail, pad):
     within(dw, ref, mag, rel, "dw")
     within(dwb, ref, mag, rel, "dw bf16")
     within(more, ref + 1.0, mag, rel, "dw accumulated")
+
+
+# Every form of the three products (test_group_launches checks that these are what the cases get): its
+# tile, whether tiles are split, and groups that leave tiles nearly empty, nearly full and empty.
+SKEW = [3000, 0, 1, 700, 4491]
+FORMS = [("linear", "64x32", [700, 0, 300, 1], 520, 2312), ("linear", "64x64", [700, 0, 300, 1], 1032, 1096),
+         ("linear", "128x64", [700, 0, 300, 1], 2312, 520), ("linear", "turns", SKEW, 2312, 520),
+         ("linear", "turns", SKEW, 2048, 4104), ("linear", "turns", [8192], 4104, 264),
+         ("linear", "turns", [5000, 3191], 2304, 1000), ("linear", "turns", [4096], 4096, 1032),
+         ("x", "64x32", [700, 0, 300, 1], 2312, 520), ("x", "64x64", [700, 0, 300, 1], 1032, 1096),
+         ("x", "128x64", SKEW, 1032, 1096), ("x", "turns", SKEW, 520, 2312),
+         ("x", "turns", SKEW, 2056, 4104),
+         ("x", "turns", [5000, 3191], 264, 4104),
+         ("w", "128x64", [700, 0, 300, 1], 264, 520), ("w", "128x128", SKEW, 1032, 1096),
+         ("w", "256x256", [900, 0, 1, 33, 511, 512, 1531, 512], 2056, 2056), ("w", "turns", [8192], 1032, 1096),
+         ("w", "turns", [8191], 264, 520), ("w", "turns", [8191, 2], 2048, 4104)]
+
+
+@pytest.mark.parametrize("case", range(len(FORMS)))
+def test_forms(case):
+    """In buffers between guards, the workspace too."""
+    from paper_2602_07265_amd import xshare as X
+    what, form, counts, n, k = FORMS[case]
+    say(f"products form {form} of {what}: {counts} n={n} k={k}")
+    P, edge, offsets, x, dy, w = _case(counts, n, k, case)
+    need = X.grouped_linear_workspace_bytes(P, len(counts), n, k)
+    ws = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    if what == "w":
+        buf = torch.full((len(counts) + 2, n, k), 5.0, device=DEV)
+        X.grouped_linear_backward_w(dy, x, offsets, out=buf[1:-1], workspace=ws[:need])
+        ref, mag = OG.grouped_linear_backward_w(dy, x, edge)
+        # a split reduction is up to 256 sums' sum
+        rel = chain(max(counts)) + 256 * 2.0 ** -24
+    else:
+        cols, red = (n, k) if what == "linear" else (k, n)
+        buf = torch.full((P + 2, cols), 5.0, dtype=torch.bfloat16, device=DEV)
+        call, ref = (X.grouped_linear, OG.grouped_linear) if what == "linear" else \
+            (X.grouped_linear_backward_x, OG.grouped_linear_backward_x)
+        out = dict(y=buf[1:-1]) if what == "linear" else dict(out=buf[1:-1])
+        call(x if what == "linear" else dy, w, offsets, workspace=ws[:need], **out)
+        ref, mag = ref(x if what == "linear" else dy, w, edge,
+                       torch.zeros((P, cols), dtype=torch.float64, device=DEV))
+        rel = chain(red) + 256 * 2.0 ** -24
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0xA5).all() and (buf[0] == 5.0).all() and (buf[-1] == 5.0).all()
+    within(buf[1:-1], ref, mag, rel, form)
+
+
+@pytest.mark.parametrize("what,counts,n,k", [("linear", SKEW, 2048, 4104), ("x", SKEW, 520, 2312),
+                                             ("w", [8191, 2], 2048, 4104)])
+def test_split_forms_again_and_with_infinities(what, counts, n, k):
+    """The same bits again, and a row's infinity stays in its row (or group) where tiles are split."""
+    from paper_2602_07265_amd import xshare as X
+    P, edge, offsets, x, dy, w = _case(counts, n, k, 7)
+    call = {"linear": lambda: X.grouped_linear(x, w, offsets),
+            "x": lambda: X.grouped_linear_backward_x(dy, w, offsets),
+            "w": lambda: X.grouped_linear_backward_w(dy, x, offsets)}[what]
+    first = call()
+    assert torch.equal(first, call()) and torch.equal(first, call())
+    x[edge[1]], dy[edge[1]] = float("inf"), float("inf")
+    got = call()
+    torch.cuda.synchronize()
+    if what == "w":
+        assert torch.equal(got[0], first[0]) and not got[1].isfinite().any()
+    else:
+        at = edge[1]                                   # the second group has rows, or the next ones do
+        keep = torch.arange(P, device=DEV) != at
+        assert torch.equal(got[keep], first[keep]) and not got[at].isfinite().any()
+
+
+def test_split_gradient_accumulates():
+    from paper_2602_07265_amd import xshare as X
+    counts, n, k = [8191], 264, 520
+    P, edge, offsets, x, dy, w = _case(counts, n, k, 8)
+    one = X.grouped_linear_backward_w(dy, x, offsets)
+    two = X.grouped_linear_backward_w(dy, x, offsets, out=one.clone(), accumulate=True)
+    half = X.grouped_linear_backward_w(dy, x, offsets,
+                                       out=torch.empty_like(one, dtype=torch.bfloat16))
+    torch.cuda.synchronize()
+    assert torch.equal(two, one + one) and torch.equal(half, one.to(torch.bfloat16))
 
 
 @pytest.mark.parametrize("E,P,n,k", [(1024, 700, 72, 136), (100, 5000, 264, 200), (65, 65, 128, 512)])
