@@ -193,6 +193,26 @@ struct Tokens {                // in adapters' order
   int L, T, r;
 };
 
+// Four values of h of one token, ranks `rank` on, as its three parts; past the rank zeros.
+template <int JT>
+__device__ __forceinline__ void store_h(uint16_t* row, int rank, int r, const floatx4& v, float s) {
+  uint16_t parts[4][3];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) split3(rank + c < r ? v[c] * s : 0.0f, parts[c]);
+#pragma unroll
+  for (int q = 0; q < 3; ++q)
+    *reinterpret_cast<uint2*>(row + q * 16 * JT + rank) =
+        make_uint2(parts[0][q] | (uint32_t)parts[1][q] << 16,
+                   parts[2][q] | (uint32_t)parts[3][q] << 16);
+}
+
+constexpr int kShrinkTokens = 32;      // of a workgroup of shrink_tile_kernel
+template <int JT>
+struct ShrinkLds {
+  static constexpr int kStages = JT == 4 ? 4 : 3;
+  static constexpr int kStage = (16 * JT + kShrinkTokens) * kBlock;   // elements
+};
+
 // h of 16 MT tokens of one adapter: the waves take blocks of 64 of the reduction in turn, kAhead of
 // them at a time, operands straight from memory, and their sums meet in LDS.  The first `groups`
 // workgroups have one product's tiles, the others another's (x and A, dy and B transposed).
@@ -257,16 +277,78 @@ __global__ __launch_bounds__(512) void shrink_kernel(Tokens o, Shrink first_a, S
 #pragma unroll
     for (int q = 1; q < kWaves; ++q) v += sums[(q * MT * JT + i) * 64 + lane];
     if (16 * t + n >= live) continue;
-    uint16_t parts[4][3];
+    store_h<JT>(a.h + (size_t)(first + 16 * t + n) * (48 * JT), 16 * j + 4 * g, o.r, v, s);
+  }
+}
+
+// The same for ranks past 32, where the factor is what is read most: 32 tokens, both operands through
+// LDS, the waves dealing the ranks among them.
+template <int JT>
+__global__ __launch_bounds__(256) void shrink_tile_kernel(Tokens o, Shrink first_a, Shrink second,
+                                                          int groups) {
+  constexpr int kThreads = 256, BA = 16 * JT, BB = kShrinkTokens, MA = JT / 4, MB = BB / 16;
+  constexpr int kStages = ShrinkLds<JT>::kStages, kStage = ShrinkLds<JT>::kStage;
+  using OpA = Operand<false, false, BA, kThreads>;
+  using OpB = Operand<false, false, BB, kThreads>;
+  static_assert(OpB::kLoads == 1, "a piece of a row each");
+  extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  const bool is_first = (int)blockIdx.x < groups;
+  const Shrink a = is_first ? first_a : second;
+  Place p;
+  if (!find_place(o.offsets, o.L, o.T, BB, 1, is_first ? blockIdx.x : blockIdx.x - groups, p)) return;
+  OpA oa;
+  oa.init(a.w + (size_t)p.e * o.r * a.K, a.K, o.r, a.K, tid);
+  const int at = 8 * (tid % 8 ^ OpB::swap(tid / 8));   // the piece of a block that the lane brings
+  const uint16_t* const x =
+      a.x + (size_t)o.tokens[p.first + min(tid / 8, p.live - 1)] * a.ldx + at;
+  const int blocks = (a.K + kBlock - 1) / kBlock;
+  auto load = [&](int b, uint16_t* stage) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c)                        // (past the rank: zeros)
-      split3(16 * j + 4 * g + c < o.r ? v[c] * s : 0.0f, parts[c]);
-    uint16_t* const out = a.h + (size_t)(first + 16 * t + n) * (48 * JT) + 16 * j + 4 * g;
+    for (int j = 0; j < OpA::kLoads; ++j) oa.load(b, stage, j, wave);
+    to_lds(b * kBlock + at < a.K ? x + b * kBlock : reinterpret_cast<const uint16_t*>(kZeros),
+           stage + BA * kBlock + wave * 512);
+  };
+  floatx4 acc[MA][MB];
 #pragma unroll
-    for (int q = 0; q < 3; ++q)
-      *reinterpret_cast<uint2*>(out + q * 16 * JT) =
-          make_uint2(parts[0][q] | (uint32_t)parts[1][q] << 16,
-                     parts[2][q] | (uint32_t)parts[3][q] << 16);
+  for (int m = 0; m < MA; ++m)
+#pragma unroll
+    for (int t = 0; t < MB; ++t) acc[m][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  auto step = [&](int b, const uint16_t* __restrict__ stage, uint16_t* __restrict__ next) {
+    load(b + kStages - 1, next);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      bf16x8 fa[MA], fb[MB];
+#pragma unroll
+      for (int m = 0; m < MA; ++m) fa[m] = OpA::read_along(stage, (wave * MA + m) * 16 + n, s, g);
+#pragma unroll
+      for (int t = 0; t < MB; ++t) fb[t] = OpB::read_along(stage + BA * kBlock, 16 * t + n, s, g);
+#pragma unroll
+      for (int m = 0; m < MA; ++m)
+#pragma unroll
+        for (int t = 0; t < MB; ++t)
+          acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[m], fb[t], acc[m][t], 0, 0, 0);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) load(s, lds + s * kStage);
+  int cur = 0;                                         // the buffer of block b
+  for (int b = 0; b < blocks; ++b) {
+    wait_loads<(OpA::kLoads + 1) * (kStages - 2)>();
+    step(b, lds + cur * kStage, lds + (cur == 0 ? kStages - 1 : cur - 1) * kStage);
+    cur = cur + 1 == kStages ? 0 : cur + 1;
+  }
+  wait_loads<0>();
+  const float scale = a.scales ? a.scales[p.e] : 1.0f;
+#pragma unroll
+  for (int t = 0; t < MB; ++t) {
+    if (16 * t + n >= p.live) continue;
+    uint16_t* const row = a.h + (size_t)(p.first + 16 * t + n) * (48 * JT);
+#pragma unroll
+    for (int m = 0; m < MA; ++m)
+      store_h<JT>(row, (wave * MA + m) * 16 + 4 * g, o.r, acc[m][t], scale);
   }
 }
 
@@ -280,8 +362,8 @@ struct Expand {
   long ld_base;
   uint16_t* out;
   long ld_out;
+  int columns;                 // of a workgroup, a multiple of 128 (set by the launch)
 };
-constexpr int kExpandColumns = 512;    // of a workgroup
 constexpr int kRestTokens = 64;        // (lanes) of a workgroup that looks for tokens without an adapter
 
 // Tokens without an adapter, of kRestTokens from the first on: out = base, or zeros.
@@ -298,8 +380,8 @@ __device__ __forceinline__ void copy_rest(const Expand& a, int T, int first) {
   }
 }
 
-// out of 16 MT tokens of one adapter and kExpandColumns columns: each wave takes 32 of these at a
-// time, dealt so that a lane's eight results are neighbours.  Workgroups from `groups` on look after the
+// out of 16 MT tokens of one adapter and a.columns columns: each wave takes 32 of these at a time,
+// dealt so that a lane's eight results are neighbours.  Workgroups from `groups` on look after the
 // tokens without an adapter.
 template <int MT, int JT>
 __global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int groups) {
@@ -311,10 +393,10 @@ __global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int gro
     return;
   }
   Place p;
-  const int columns = (a.N + kExpandColumns - 1) / kExpandColumns;
+  const int columns = (a.N + a.columns - 1) / a.columns;
   if (!find_place(o.offsets, o.L, o.T, 16 * MT, columns, blockIdx.x, p)) return;
   const int e = p.e, first = p.first, live = p.live;
-  const int c0 = p.column * kExpandColumns;
+  const int c0 = p.column * a.columns;
   long token[MT];
   bf16x8 fh[MT][JT];
 #pragma unroll
@@ -327,34 +409,55 @@ __global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int gro
   }
   const float scale = a.scales ? a.scales[e] : 1.0f;
   const uint16_t* const w = a.w + (size_t)e * a.N * o.r;
-  const int end = min(c0 + kExpandColumns, a.N);
+  const int end = min(c0 + a.columns, a.N);
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  for (int c = c0 + 32 * wave; c < end; c += 128) {
-    floatx4 acc[2][MT];
+  // W's rows go with both parts of h: with 16 ranks the parts lie in one operand, else in two
+  constexpr int kSteps = JT == 1 ? 1 : JT / 2;
+  uint4 fw[2][kSteps], base[MT];
+  auto fetch = [&](int c) {                            // under way while the columns before are stored
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      base[t] = zero;
+      if (a.base && 16 * t + n < live && c + 8 * g < a.N)
+        base[t] = *reinterpret_cast<const uint4*>(a.base + token[t] * a.ld_base + c + 8 * g);
+    }
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const int col = min(c + 8 * (n >> 2) + 4 * m + (n & 3), a.N - 1);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) acc[m][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int s = 0; s < JT; ++s) {
-        // the first two parts of h lie one behind the other: W's row goes with both
+      for (int s = 0; s < kSteps; ++s) {
         const int j = (32 * s + 8 * g) % (16 * JT);
-        const uint4 v =
-            j < o.r ? *reinterpret_cast<const uint4*>(w + (size_t)col * o.r + j) : zero;
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-          acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v),
-                                                              fh[t][s], acc[m][t], 0, 0, 0);
+        fw[m][s] = j < o.r ? *reinterpret_cast<const uint4*>(w + (size_t)col * o.r + j) : zero;
       }
     }
+  };
+  if (c0 + 32 * wave < end) fetch(c0 + 32 * wave);
+  for (int c = c0 + 32 * wave; c < end; c += 128) {
     const int to = c + 8 * g;
+    uint4 here[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) here[t] = base[t];
+    floatx4 acc[2][MT];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        acc[m][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const bf16x8 v = __builtin_bit_cast(bf16x8, fw[m][s]);
+          acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, fh[t][s], acc[m][t], 0, 0, 0);
+          if constexpr (JT > 1)
+            acc[m][t] =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, fh[t][kSteps + s], acc[m][t], 0, 0, 0);
+        }
+      }
+    if (c + 128 < end) fetch(c + 128);
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       if (16 * t + n >= live || to >= a.N) continue;
-      float v[8] = {};
-      if (a.base)
-        values8(*reinterpret_cast<const uint4*>(a.base + token[t] * a.ld_base + to), v);
+      float v[8];
+      values8(here[t], v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(scale, acc[i / 4][t][i % 4], v[i]);
       *reinterpret_cast<uint4*>(a.out + token[t] * a.ld_out + to) = to_bf16x8(v);
@@ -373,16 +476,28 @@ struct Factors {
   float *da, *db;              // [L, r, d] and [L, n, r]; where splits > 1 a part's of the workspace
 };
 
+// LDS of factors_kernel: blocks of kB tokens, so many that loads are long under way.
+template <int JT>
+struct FactorsLds {
+  static constexpr int kB = JT <= 2 ? 64 : 32;
+  static constexpr int kStages = JT == 1 || JT == 4 ? 3 : JT == 2 ? 2 : 4;
+  static constexpr int kStage = kB * (kGradColumns + 48 * JT);        // elements
+  static constexpr int kBytes = kStages * kStage * 2;
+};
+
 // The gradients of kGradColumns columns of a factor's long side: dA from x and dh, dB from dy and
-// h, both operands across the reduction, which runs over the adapter's tokens in blocks of 64.
+// h, both operands across the reduction, which runs over the adapter's tokens in blocks of kB.
 // Workgroup (column tile: dA's, then dB's; part of the tokens; adapter).
 template <int JT>
 __global__ __launch_bounds__(256) void factors_kernel(Factors a) {
-  constexpr int kThreads = 256, kRank = 16 * JT;
-  using Wide = Operand<true, false, kGradColumns, kThreads>;
-  constexpr int kHPieces = 3 * kRank / 8;              // 16-byte pieces of a row of h
-  constexpr int kHLoads = (kBlock * kHPieces + kThreads - 1) / kThreads;
-  constexpr int kStage = kBlock * (kGradColumns + 3 * kRank);
+  using Lds = FactorsLds<JT>;
+  constexpr int kThreads = 256, kRank = 16 * JT, kB = Lds::kB, kStages = Lds::kStages;
+  using Wide = Operand<true, false, kGradColumns, kThreads, kB>;
+  using Rank = Operand<true, false, kRank, kB * kRank / 8, kB>;        // each part of h
+  constexpr int kPartPieces = kB * kRank / 8, kPieces = 3 * kPartPieces;   // 16 bytes each
+  constexpr int kHLoads = (kPieces + kThreads - 1) / kThreads;
+  constexpr int kLoads = Wide::kLoads + kPieces / kThreads;    // of a wave and block, at least
+  static_assert(kPieces % 64 == 0, "whole waves");
   extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -395,9 +510,9 @@ __global__ __launch_bounds__(256) void factors_kernel(Factors a) {
   int lo, hi;
   group_rows(a.offsets, e, a.T, lo, hi);
   {  // this part of the adapter's tokens, in whole blocks
-    const int blocks = (hi - lo + kBlock - 1) / kBlock;
-    const int from = (int)((long)blocks * blockIdx.y / a.splits) * kBlock;
-    const int upto = (int)((long)blocks * (blockIdx.y + 1) / a.splits) * kBlock;
+    const int blocks = (hi - lo + kB - 1) / kB;
+    const int from = (int)((long)blocks * blockIdx.y / a.splits) * kB;
+    const int upto = (int)((long)blocks * (blockIdx.y + 1) / a.splits) * kB;
     hi = min(hi, lo + upto);
     lo += from;
   }
@@ -408,34 +523,43 @@ __global__ __launch_bounds__(256) void factors_kernel(Factors a) {
   const uint16_t* const skinny = is_a ? a.dh : a.h;
   const uint16_t* const zeros = reinterpret_cast<const uint16_t*>(kZeros);
 
-  // lane's piece of load j of the wide rows: row j * kStep + tid / kPieces, `column` on
-  int token[Wide::kLoads];
-  static_assert(Wide::kStep % 16 == 0, "one column for every load");
+  // Load j of the wide rows brings a wave four of them, sixteen lanes `column` on of each.  Their
+  // tokens come by scalar loads: vector ones would be done in order with the blocks' loads, so that
+  // to wait for them would be to wait for those.
+  constexpr int kWaveRows = 4;
+  static_assert(Wide::kStep == kWaveRows * 4 && Wide::kPieces == 16, "four waves, sixteen lanes a row");
+  using Scalar = const __attribute__((address_space(4))) int32_t*;
+  const Scalar tokens = (Scalar)(uintptr_t)(a.tokens + lo);
+  int token[Wide::kLoads][kWaveRows];
   const int column = min(Wide::column(tid, 0), width - c0 - 8);
   auto fetch = [&](int b) {
 #pragma unroll
-    for (int j = 0; j < Wide::kLoads; ++j) {
-      const int q = b * kBlock + j * Wide::kStep + tid / Wide::kPieces;
-      token[j] = q < rows ? a.tokens[lo + q] : -1;
-    }
+    for (int j = 0; j < Wide::kLoads; ++j)
+#pragma unroll
+      for (int i = 0; i < kWaveRows; ++i) {
+        const int q = b * kB + j * Wide::kStep + wave * kWaveRows + i;
+        token[j][i] = tokens[max(min(q, rows - 1), 0)];
+      }
   };
-  // h's rows: LDS [3][64][kRank], each part an operand of its own
-  using Rank = Operand<true, false, kRank, kBlock * kRank / 8>;
+  // the wide rows of the tokens that were fetched; LDS [3][kB][kRank] of h's
   auto load = [&](int b, uint16_t* stage) {
 #pragma unroll
-    for (int j = 0; j < Wide::kLoads; ++j)
-      to_lds(token[j] >= 0 ? wide + c0 + (size_t)token[j] * ld + column : zeros,
+    for (int j = 0; j < Wide::kLoads; ++j) {
+      const int lo2 = g & 1 ? token[j][1] : token[j][0], hi2 = g & 1 ? token[j][3] : token[j][2];
+      const int t = g & 2 ? hi2 : lo2;
+      const bool in = b * kB + j * Wide::kStep + wave * kWaveRows + g < rows;
+      to_lds(in ? wide + c0 + (size_t)t * ld + column : zeros,
              stage + j * kThreads * 8 + wave * 512);
-    uint16_t* const hl = stage + kBlock * kGradColumns;
+    }
+    uint16_t* const hl = stage + kB * kGradColumns;
 #pragma unroll
     for (int j = 0; j < kHLoads; ++j) {
-      const int i = j * kThreads + tid;                // piece of the stage's [3][64][kRank / 8]
-      if (kBlock * kHPieces % kThreads != 0 && j * kThreads + wave * 64 >= kBlock * kHPieces)
-        break;                                         // (whole waves)
-      const int part = i / (kBlock * kRank / 8), in = i % (kBlock * kRank / 8);
+      if (kPieces % kThreads != 0 && j * kThreads + wave * 64 >= kPieces) break;   // (whole waves)
+      const int i = j * kThreads + tid;
+      const int part = i / kPartPieces, in = i % kPartPieces;
       const int q = in / (kRank / 8), slot = in % (kRank / 8);
       const int c = 8 * (slot ^ Rank::swap(q) << 1);
-      const int row = b * kBlock + q;
+      const int row = b * kB + q;
       to_lds(row < rows ? skinny + (size_t)(lo + row) * (3 * kRank) + part * kRank + c : zeros,
              hl + (j * kThreads + wave * 64) * 8);
     }
@@ -446,41 +570,50 @@ __global__ __launch_bounds__(256) void factors_kernel(Factors a) {
   for (int m = 0; m < kTiles; ++m)
 #pragma unroll
     for (int j = 0; j < JT; ++j) acc[m][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  auto step = [&](const uint16_t* __restrict__ stage) {
+  auto step = [&](auto of_a, int b, const uint16_t* __restrict__ stage, uint16_t* __restrict__ next) {
+    load(b + kStages - 1, next);
+    fetch(b + kStages);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < kB / 32; ++s) {
       bf16x8 fw[kTiles];
 #pragma unroll
       for (int m = 0; m < kTiles; ++m)
         fw[m] = Wide::read_across(stage, Wide::across(wave * kTiles + m, n, g), s);
 #pragma unroll
       for (int part = 0; part < 3; ++part) {
-        const uint16_t* const hl = stage + kBlock * kGradColumns + part * kBlock * kRank;
+        const uint16_t* const hl = stage + kB * kGradColumns + part * kB * kRank;
 #pragma unroll
         for (int j = 0; j < JT; ++j) {
           const bf16x8 fh = Rank::read_across(hl, Rank::across(j, n, g), s);
 #pragma unroll
           for (int m = 0; m < kTiles; ++m)
-            acc[m][j] = is_a ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[m], fh, acc[m][j], 0, 0, 0)
-                             : __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, fw[m], acc[m][j], 0, 0, 0);
+            acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                of_a ? fw[m] : fh, of_a ? fh : fw[m], acc[m][j], 0, 0, 0);
         }
       }
     }
   };
-  const int blocks = (rows + kBlock - 1) / kBlock;
-  if (blocks > 0) {
+  const int blocks = (rows + kB - 1) / kB;
+  auto run = [&](auto of_a) {
     fetch(0);
-    load(0, lds);
-    if (blocks > 1) fetch(1);
-    for (int b = 0; b < blocks; ++b) {
-      uint16_t* const here = lds + (b & 1) * kStage;
-      wait_loads<0>();
-      if (b + 1 < blocks) {
-        load(b + 1, lds + (~b & 1) * kStage);
-        if (b + 2 < blocks) fetch(b + 2);
-      }
-      step(here);
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) {
+      load(s, lds + s * Lds::kStage);
+      fetch(s + 1);
     }
+    int cur = 0;                                       // the buffer of block b
+    for (int b = 0; b < blocks; ++b) {
+      wait_loads<kLoads*(kStages - 2)>();
+      step(of_a, b, lds + cur * Lds::kStage, lds + (cur == 0 ? kStages - 1 : cur - 1) * Lds::kStage);
+      cur = cur + 1 == kStages ? 0 : cur + 1;
+    }
+    wait_loads<0>();
+  };
+  if (blocks > 0) {                                    // (one question, not one for each product)
+    if (is_a)
+      run(std::true_type());
+    else
+      run(std::false_type());
   }
   const size_t plane = (size_t)blockIdx.y * a.L * a.r * ((size_t)a.n + a.d);
   const float scale = is_a || !a.scales ? 1.0f : a.scales[e];   // (dh has its own in it)
@@ -537,22 +670,37 @@ hipError_t allow_lds(K kernel, int bytes) {
 // One product, or two in one launch.
 hipError_t launch_shrink(const Tokens& o, const Shrink& a, const Shrink* b, hipStream_t stream) {
   return by_rank(o.r, [&](auto j) {
-    constexpr int JT = decltype(j)::value, MT = JT >= 4 ? 2 : 1;
-    constexpr int kBytes = 8 * MT * JT * 64 * 16;
-    const auto kernel = shrink_kernel<MT, JT>;
-    const hipError_t e = allow_lds(kernel, kBytes);
-    if (e != hipSuccess) return e;
-    const int groups = (int)most_tiles(o.T, o.L, 16 * MT, 1);
-    kernel<<<b ? 2 * groups : groups, 512, kBytes, stream>>>(o, a, b ? *b : a, groups);
+    constexpr int JT = decltype(j)::value;
+    const Shrink& second = b ? *b : a;
+    if constexpr (JT >= 4) {
+      constexpr int kBytes = ShrinkLds<JT>::kStages * ShrinkLds<JT>::kStage * 2;
+      static_assert(kBytes <= 64 * 1024, "LDS that needs no permission");
+      const int groups = (int)most_tiles(o.T, o.L, kShrinkTokens, 1);
+      shrink_tile_kernel<JT>
+          <<<b ? 2 * groups : groups, 256, kBytes, stream>>>(o, a, second, groups);
+    } else {
+      constexpr int kBytes = 8 * JT * 64 * 16;
+      const int groups = (int)most_tiles(o.T, o.L, 16, 1);
+      shrink_kernel<1, JT><<<b ? 2 * groups : groups, 512, kBytes, stream>>>(o, a, second, groups);
+    }
     return hipGetLastError();
   });
 }
 
-hipError_t launch_expand(const Tokens& o, const Expand& x, hipStream_t stream) {
+// Workgroups of expand_kernel: enough for every compute unit, each with columns enough to make up for
+// its start (finding its tokens and reading their h).
+constexpr int kExpandGroups = 1024, kExpandMost = 2048;
+
+hipError_t launch_expand(const Tokens& o, const Expand& args, hipStream_t stream) {
   return by_rank(o.r, [&](auto j) {
     constexpr int JT = decltype(j)::value, MT = 2;
-    const long groups = most_tiles(o.T, o.L, 16 * MT, (x.N + kExpandColumns - 1) / kExpandColumns);
-    const long rest = x.out == x.base ? 0 : (o.T + kRestTokens - 1) / kRestTokens;
+    // as many columns a workgroup as leave about kExpandGroups of them
+    Expand x = args;
+    const long tiles = most_tiles(o.T, o.L, 16 * MT, 1);
+    const long columns = tiles * x.N / kExpandGroups / 128 * 128;
+    x.columns = (int)(columns < 128 ? 128 : columns < kExpandMost ? columns : kExpandMost);
+    const long groups = most_tiles(o.T, o.L, 16 * MT, (x.N + x.columns - 1) / x.columns);
+    const long rest = args.out == args.base ? 0 : (o.T + kRestTokens - 1) / kRestTokens;
     if ((groups + rest) * 256 > 0xFFFFFFFFl) return hipErrorInvalidConfiguration;
     expand_kernel<MT, JT><<<(unsigned)(groups + rest), 256, 0, stream>>>(o, x, (int)groups);
     return hipGetLastError();
@@ -562,7 +710,7 @@ hipError_t launch_expand(const Tokens& o, const Expand& x, hipStream_t stream) {
 hipError_t launch_factors(const Factors& f, hipStream_t stream) {
   return by_rank(f.r, [&](auto j) {
     constexpr int JT = decltype(j)::value;
-    constexpr int kBytes = 2 * kBlock * (kGradColumns + 48 * JT) * 2;
+    constexpr int kBytes = FactorsLds<JT>::kBytes;
     static_assert(kBytes <= 160 * 1024, "LDS of a compute unit");
     const auto kernel = factors_kernel<JT>;
     const hipError_t e = allow_lds(kernel, kBytes);
@@ -598,7 +746,7 @@ hipError_t launch_adapters(const AdaptersArgs& a, hipStream_t stream) {
   if ((e = launch_shrink(o, {a.x, a.ldx, a.d, a.a, nullptr, a.h}, nullptr, stream)) != hipSuccess)
     return e;
   return launch_expand(
-      o, {a.rows, a.n, a.h, a.b, a.scales, a.base, a.ld_base, a.out, a.ld_out}, stream);
+      o, {a.rows, a.n, a.h, a.b, a.scales, a.base, a.ld_base, a.out, a.ld_out, 0}, stream);
 }
 
 hipError_t launch_adapters_backward(const AdaptersArgs& a, hipStream_t stream) {
@@ -612,7 +760,7 @@ hipError_t launch_adapters_backward(const AdaptersArgs& a, hipStream_t stream) {
     const Shrink g{a.dy, a.lddy, a.n, a.bt, a.scales, a.dh};
     if ((e = launch_shrink(o, {a.x, a.ldx, a.d, a.a, nullptr, a.h}, &g, stream)) != hipSuccess)
       return e;
-    e = launch_expand(o, {a.rows, a.d, a.dh, a.at, nullptr, a.base, a.ld_base, a.out, a.ld_out},
+    e = launch_expand(o, {a.rows, a.d, a.dh, a.at, nullptr, a.base, a.ld_base, a.out, a.ld_out, 0},
                       stream);
     if (e != hipSuccess) return e;
   }

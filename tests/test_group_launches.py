@@ -47,7 +47,8 @@ def test_adapter_forms():
     # few tokens: in one launch and in two; many: every width of the rank's tiles
     for want in ("few_kernel", "few_shrink_kernel", "few_expand_kernel", "transpose_kernel",
                  "sum_parts_kernel", *(f"factors_kernel<{j}>" for j in (1, 2, 4, 8)),
-                 *(f"shrink_kernel<{1 if j < 4 else 2}, {j}>" for j in (1, 2, 4, 8)),
+                 "shrink_kernel<1, 1>", "shrink_kernel<1, 2>", "shrink_tile_kernel<4>",
+                 "shrink_tile_kernel<8>",
                  *(f"expand_kernel<2, {j}>" for j in (1, 2, 4, 8))):
         assert want in kernels, want
     for (what, T, *_), names in zip(cases, got):
