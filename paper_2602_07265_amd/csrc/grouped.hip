@@ -114,6 +114,16 @@ __device__ __forceinline__ bool tile_at(const Product& p, const RowTiles& c, lon
   t.part = -1;
   return true;
 }
+// Part `part` of `parts` of a tile's reduction, in whole blocks of kB.
+template <Kind kKind, int kB>
+__device__ __forceinline__ void take_part(Tile& t, int part, int parts) {
+  const int blocks = (t.reduction + kB - 1) / kB;
+  const int from = (int)((long)blocks * part / parts) * kB;
+  const int upto = (int)((long)blocks * (part + 1) / parts) * kB;
+  t.reduction = min(upto, t.reduction) - from;
+  t.a += kKind == kForward ? from : from * t.lda;
+  t.b += kKind == kGradW ? from * t.ldb : from;
+}
 template <Kind kKind, int BB>
 __device__ __forceinline__ long count_tiles(const Product& p, RowTiles& c) {
   if constexpr (kKind == kGradW) return (long)p.E * p.column_tiles * p.row_tiles;
@@ -134,13 +144,8 @@ __device__ __forceinline__ bool find_tile(const Product& p, Tile& t) {
   }
   const long at = piece_of(i - (int)whole, (long)s.rest * s.parts);
   if (at < 0 || !tile_at<kKind, BA, BB>(p, c, s.whole + at / s.parts, t)) return false;
-  const int blocks = (t.reduction + kBlock - 1) / kBlock, part = (int)(at % s.parts);
-  const int from = (int)((long)blocks * part / s.parts) * kBlock;
-  const int upto = (int)((long)blocks * (part + 1) / s.parts) * kBlock;
+  take_part<kKind, kBlock>(t, (int)(at % s.parts), s.parts);
   t.part = (int)at;
-  t.reduction = min(upto, t.reduction) - from;
-  t.a += kKind == kForward ? from : from * t.lda;
-  t.b += kKind == kGradW ? from * t.ldb : from;
   return true;
 }
 
@@ -188,8 +193,10 @@ __device__ __forceinline__ void store(const Product& a, const Tile& t, int r, in
   }
 }
 
-template <Kind kKind, int BA, int BB, int WA, int WB, int kStages, int kB>
-__global__ __launch_bounds__(64 * WA * WB) void tile_kernel(Product a) {
+// BA columns by BB rows; WA waves along the columns by WB along the rows; kGroups such groups of waves,
+// each with a part of the reduction and buffers of its own, whose sums meet in LDS.
+template <Kind kKind, int BA, int BB, int WA, int WB, int kStages, int kB, int kGroups>
+__global__ __launch_bounds__(64 * WA * WB * kGroups) void tile_kernel(Product a) {
   constexpr bool kAcrossA = kKind != kForward, kAcrossB = kKind == kGradW;
   constexpr int kThreads = 64 * WA * WB;
   constexpr int MA = BA / WA / 16, MB = BB / WB / 16;
@@ -200,20 +207,24 @@ __global__ __launch_bounds__(64 * WA * WB) void tile_kernel(Product a) {
   using OpB = Operand<kAcrossB, false, BB, kThreads, kB>;
   constexpr int kLoads = OpA::kLoads + OpB::kLoads;
   constexpr int kStage = (BA + BB) * kB;
-  extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
-  const int tid = threadIdx.x, lane = tid & 63;
+  extern __shared__ __attribute__((aligned(16))) uint16_t lds_of_all[];
+  const int tid = threadIdx.x % kThreads, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  uint16_t* const lds = lds_of_all + group * kStages * kStage;
   const int wa = wave % WA, wb = wave / WA;
   const int n = lane & 15, g = lane >> 4;
 
   Tile tile;
   if (!find_tile<kKind, BA, BB>(a, tile)) return;     // (its parts are turns_kernel's alone)
+  // (every group takes as many steps, for they meet at the barriers)
+  const int blocks = ((tile.reduction + kB - 1) / kB + kGroups - 1) / kGroups;
+  if constexpr (kGroups > 1) take_part<kKind, kB>(tile, group, kGroups);
   const int reduction = tile.reduction;
   OpA oa;
   OpB ob;
   oa.init(tile.a, tile.lda, a.columns - tile.c0, reduction, tid);
   ob.init(tile.b, tile.ldb, tile.rows_left, reduction, tid);
-  const int blocks = (reduction + kB - 1) / kB;
 
   floatx4 acc[MA][MB];
 #pragma unroll
@@ -273,6 +284,19 @@ __global__ __launch_bounds__(64 * WA * WB) void tile_kernel(Product a) {
     wait_loads<0>();
   }
 
+  if constexpr (kGroups > 1) {
+    floatx4* const sums = reinterpret_cast<floatx4*>(lds_of_all) + tid;
+    if (group > 0)
+#pragma unroll
+      for (int i = 0; i < MA * MB; ++i)
+        sums[((group - 1) * MA * MB + i) * kThreads] = acc[i / MB][i % MB];
+    __syncthreads();
+    if (group > 0) return;
+    for (int q = 0; q < kGroups - 1; ++q)
+#pragma unroll
+      for (int i = 0; i < MA * MB; ++i)
+        acc[i / MB][i % MB] += sums[(q * MA * MB + i) * kThreads];
+  }
 #pragma unroll
   for (int t = 0; t < MB; ++t) {
     floatx4 v[MA];
@@ -495,13 +519,15 @@ hipError_t launch(const Product& a, F kernel, long grid, int threads, int bytes,
   return hipGetLastError();
 }
 
-template <Kind kKind, int BA, int BB, int WA, int WB, int kStages, int kB = kBlock>
+template <Kind kKind, int BA, int BB, int WA, int WB, int kStages, int kB = kBlock, int kGroups = 1>
 hipError_t launch_tile(Product a, hipStream_t stream) {
-  constexpr int kBytes = kStages * (BA + BB) * kB * 2;
+  constexpr int kBytes = kGroups * kStages * (BA + BB) * kB * 2;
+  static_assert((kGroups - 1) * BA * BB * 4 <= kBytes, "the groups' sums");
   static_assert(kBytes <= 160 * 1024, "LDS of a compute unit");
   a.sums = nullptr;
   const long tiles = most_tiles<kKind, BA, BB>(a);
-  return launch(a, tile_kernel<kKind, BA, BB, WA, WB, kStages, kB>, tiles, 64 * WA * WB, kBytes, stream);
+  return launch(a, tile_kernel<kKind, BA, BB, WA, WB, kStages, kB, kGroups>, tiles,
+                64 * WA * WB * kGroups, kBytes, stream);
 }
 
 template <Kind kKind>
@@ -518,10 +544,14 @@ hipError_t launch_turns(Product a, hipStream_t stream) {
 }
 
 // The forms of a product: its tile, and what it costs in microseconds: 64 of the reduction, `few` with
-// little else on the GPU, `full` for each tile that every compute unit has to work on, and `out`, a
-// tile's stores where the outputs are what is written most (fp32 dW).  Measured over 1 to 64 groups of
-// 1 to 4096 rows by four shapes of 512 to 4096; of 109 cases the choice came within 10 % of the best
-// form on 98 (forward) and 93 (dx), 3 and 4 % above it on average.
+// little else on the GPU, `full` for each tile that every compute unit has to work on, and `out`, what a
+// tile takes besides (finding its rows, the first loads, the stores).  Measured over 1 to 64 groups of
+// 1 to 4096 rows by ten shapes of 72 to 10304; there the rule's choice took 3.5 % (forward) and 4.7 %
+// (dx) longer than the fastest form on average, and within 10 % of it in 160 of 184 and 147 of 178.
+// Both sides, in the forms' order without the first: 64 rows of one group by (4096, 4096) 15.7, 18.5,
+// 23.7 and 70 us (29.7 split); 1024 rows 73, 53, 43 and 76 (53); 4096 rows 285, 195, 154 and 97 (99);
+// 512 rows in each of 8 groups 349, 268, 220 and 172 (149).  The first against the second: one row by
+// (256, 10304) 22.7 and 32 us.
 enum Units { kShared, kAlone, kSplit };  // tiles of a unit: several, one, one and the last round split
 struct Form {
   int columns, rows;
@@ -530,16 +560,18 @@ struct Form {
   hipError_t (*launch)(Product, hipStream_t);
 };
 const Form kForwardForms[] = {
-    {64, 32, 0.185f, 0.145f, 0.0f, kShared, launch_tile<kForward, 64, 32, 4, 1, 4>},
-    {64, 64, 0.23f, 0.205f, 0.0f, kShared, launch_tile<kForward, 64, 64, 2, 2, 3>},
-    {128, 64, 0.30f, 0.34f, 0.0f, kShared, launch_tile<kForward, 128, 64, 2, 2, 3>},
-    {256, 256, 1.07f, 1.5f, 0.0f, kSplit, launch_turns<kForward>},
+    {64, 32, 0.122f, 0.145f, 1.2f, kShared, launch_tile<kForward, 64, 32, 4, 1, 3, 64, 2>},
+    {64, 32, 0.185f, 0.13f, 0.6f, kShared, launch_tile<kForward, 64, 32, 4, 1, 4>},
+    {64, 64, 0.23f, 0.19f, 0.65f, kShared, launch_tile<kForward, 64, 64, 2, 2, 3>},
+    {128, 64, 0.30f, 0.32f, 1.4f, kShared, launch_tile<kForward, 128, 64, 2, 2, 3>},
+    {256, 256, 1.07f, 1.4f, 9.0f, kSplit, launch_turns<kForward>},
 };
 const Form kGradXForms[] = {
-    {64, 32, 0.225f, 0.145f, 0.0f, kShared, launch_tile<kGradX, 64, 32, 4, 1, 4>},
-    {64, 64, 0.25f, 0.205f, 0.0f, kShared, launch_tile<kGradX, 64, 64, 2, 2, 3>},
-    {128, 64, 0.38f, 0.33f, 0.0f, kShared, launch_tile<kGradX, 128, 64, 2, 2, 3>},
-    {256, 256, 1.35f, 1.7f, 0.0f, kSplit, launch_turns<kGradX>},
+    {64, 32, 0.155f, 0.15f, 1.2f, kShared, launch_tile<kGradX, 64, 32, 4, 1, 3, 64, 2>},
+    {64, 32, 0.225f, 0.13f, 0.6f, kShared, launch_tile<kGradX, 64, 32, 4, 1, 4>},
+    {64, 64, 0.25f, 0.19f, 0.7f, kShared, launch_tile<kGradX, 64, 64, 2, 2, 3>},
+    {128, 64, 0.38f, 0.31f, 1.4f, kShared, launch_tile<kGradX, 128, 64, 2, 2, 3>},
+    {256, 256, 1.30f, 1.55f, 12.0f, kSplit, launch_turns<kGradX>},
 };
 const Form kGradWForms[] = {
     {128, 64, 0.60f, 0.42f, 1.4f, kShared, launch_tile<kGradW, 128, 64, 2, 2, 3, 32>},

@@ -4,14 +4,16 @@ import test_gpu_adapters
 import test_gpu_grouped
 from group_launches import group_launches
 
-LINEAR = {"64x32": "tile_kernel<0, 64, 32, 4, 1, 4, 64>", "64x64": "tile_kernel<0, 64, 64, 2, 2, 3, 64>",
-          "128x64": "tile_kernel<0, 128, 64, 2, 2, 3, 64>", "turns": "turns_kernel<0>"}
-GRAD_X = {"64x32": "tile_kernel<1, 64, 32, 4, 1, 4, 64>", "64x64": "tile_kernel<1, 64, 64, 2, 2, 3, 64>",
-          "128x64": "tile_kernel<1, 128, 64, 2, 2, 3, 64>",
+LINEAR = {"64x32 x 2": "tile_kernel<0, 64, 32, 4, 1, 3, 64, 2>",
+          "64x32": "tile_kernel<0, 64, 32, 4, 1, 4, 64, 1>", "64x64": "tile_kernel<0, 64, 64, 2, 2, 3, 64, 1>",
+          "128x64": "tile_kernel<0, 128, 64, 2, 2, 3, 64, 1>", "turns": "turns_kernel<0>"}
+GRAD_X = {"64x32 x 2": "tile_kernel<1, 64, 32, 4, 1, 3, 64, 2>",
+          "64x32": "tile_kernel<1, 64, 32, 4, 1, 4, 64, 1>", "64x64": "tile_kernel<1, 64, 64, 2, 2, 3, 64, 1>",
+          "128x64": "tile_kernel<1, 128, 64, 2, 2, 3, 64, 1>",
           "turns": "turns_kernel<1>"}
-GRAD_W = {"128x64": "tile_kernel<2, 128, 64, 2, 2, 3, 32>",
-          "128x128": "tile_kernel<2, 128, 128, 2, 2, 3, 32>",
-          "256x256": "tile_kernel<2, 256, 256, 2, 4, 4, 32>", "turns": "turns_kernel<2>"}
+GRAD_W = {"128x64": "tile_kernel<2, 128, 64, 2, 2, 3, 32, 1>",
+          "128x128": "tile_kernel<2, 128, 128, 2, 2, 3, 32, 1>",
+          "256x256": "tile_kernel<2, 256, 256, 2, 4, 4, 32, 1>", "turns": "turns_kernel<2>"}
 OF = {"linear": LINEAR, "x": GRAD_X, "w": GRAD_W}
 
 
