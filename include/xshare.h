@@ -728,7 +728,9 @@ xshare_status xshare_block_experts(const xshare_block_experts_args* args);
  * set selection) -> xshare_expert_order -> xshare_dispatch -> xshare_grouped_linear ... ->    *
  * xshare_combine, and back.  Adapters stand beside a shared projection (xshare_block_linear).*
  * Limits: T * k and every other size at most 2^20, at most 1024 experts or adapters, k <= 32 *
- * (XSHARE_EUNSUPPORTED beyond).  Every call gives the same bits again.                       *
+ * (XSHARE_EUNSUPPORTED beyond).  Every call gives the same bits again.  What a call writes     *
+ * must not overlap what it reads but where it says so; matrices of rows that do are refused   *
+ * (XSHARE_EINVAL).                                                                            *
  * ---------------------------------------------------------------------------------------- */
 
 /* Workspace of xshare_expert_order (bytes, 256-aligned); 0 where it needs none (T * top_k up to
@@ -754,7 +756,7 @@ xshare_status xshare_expert_order(const int32_t* ids, int32_t T, int32_t top_k, 
  * xshare_dispatch -- each token to its pairs' rows: out[rows[t, r]] = x[t].
  *
  *   x, out   [T, d] and [T * top_k, d] of `dtype` (XSHARE_BF16, XSHARE_F32), rows ldx and ld_out
- *            elements apart (at least d), any alignment of their elements; they do not overlap.
+ *            elements apart (at least d), any alignment of their elements.
  *   rows     as xshare_expert_order writes it: distinct; an entry outside [0, T * top_k) is no row.
  *
  * Rows that no pair has are left as they were.  The gradient of x is xshare_combine of out's
@@ -841,8 +843,8 @@ xshare_status xshare_grouped_linear_backward_w(const uint16_t* dy, int64_t lddy,
  *   a, b        [n_adapters, rank, d] and [n_adapters, n, rank] bf16, 16-byte aligned.
  *   ids         [T] int32: each token's adapter; outside [0, n_adapters): none.
  *   scales      [n_adapters] fp32, or NULL: 1.
- *   base, out   xshare_adapters: [T, n]; _backward: [T, d] bf16; base NULL: zeros.  out may be base;
- *               otherwise they do not overlap.
+ *   base, out   xshare_adapters: [T, n]; _backward: [T, d] bf16; base NULL: zeros.  out may be base
+ *               (but not x or dy, whatever base is).
  *   dy          _backward only: [T, n] bf16, the gradient of xshare_adapters' out.
  *   da, db      _backward only, out: [n_adapters, rank, d] and [n_adapters, n, rank] fp32, 16-byte
  *               aligned; zeros for an adapter without tokens.
@@ -879,7 +881,8 @@ size_t xshare_adapters_workspace_bytes(int32_t T, int32_t n_adapters, int32_t ra
  * xshare_adapters -- low-rank adapters of many requests beside a shared projection:
  * out_t = base_t + scales[e] B_e A_e x_t, e = ids[t]; out_t = base_t for a token without one (it
  * has no part in anything else).  A_e x_t is held in fp32 (to 16 bits or more where it meets
- * B_e), sums are fp32, and out is rounded once.
+ * B_e), sums are fp32, and out is rounded once.  Infinities in a token's x or in its adapter's
+ * factors may give that token NaN in place of infinities.
  */
 xshare_status xshare_adapters(const xshare_adapters_args* args);
 

@@ -52,6 +52,29 @@ bool valid_matrix(const void* p, int64_t ld, int32_t cols) {
   return p && aligned(p, 16) && ld >= cols && ld % 8 == 0;
 }
 
+// A matrix of rows, as a call is given it.
+struct Rows {
+  const void* p;
+  int64_t ld;
+  int64_t rows;
+  int32_t cols;
+};
+// Whether two matrices of elements of `size` bytes share memory.  Columns of one buffer that lie side
+// by side do not.
+bool overlap(const Rows& a, const Rows& b, uint64_t size) {
+  if (!a.p || !b.p || a.rows == 0 || b.rows == 0) return false;
+  const uint64_t p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
+  const uint64_t bytes_p = (uint64_t(a.rows - 1) * uint64_t(a.ld) + a.cols) * size;
+  const uint64_t bytes_q = (uint64_t(b.rows - 1) * uint64_t(b.ld) + b.cols) * size;
+  if (p + bytes_p <= q || q + bytes_q <= p) return false;
+  if (a.ld != b.ld) return true;
+  const uint64_t row = uint64_t(a.ld) * size;          // b's first column from a's on, within a row
+  const uint64_t apart = p <= q ? (q - p) % row : (row - (p - q) % row) % row;
+  return apart < a.cols * size || apart + b.cols * size > row;
+}
+bool same(const Rows& a, const Rows& b) { return a.p == b.p && a.ld == b.ld; }
+uint64_t bytes_of(int32_t dtype) { return dtype == XSHARE_F32 ? 4 : 2; }
+
 xs::MoveArgs move_args(int32_t dtype, int32_t T, int32_t k, int32_t d, const int32_t* rows) {
   xs::MoveArgs a{};
   a.fp32 = dtype == XSHARE_F32;
@@ -109,7 +132,6 @@ xshare_status run_adapters(const xshare_adapters_args* p, bool backward) {
         !valid_matrix(p->out, p->ld_out, cols))
       return XSHARE_EINVAL;
     if (p->base && !valid_matrix(p->base, p->ld_base, cols)) return XSHARE_EINVAL;
-    if (p->base == p->out && p->ld_base != p->ld_out) return XSHARE_EINVAL;
     if (backward && !valid_matrix(p->dy, p->lddy, p->n)) return XSHARE_EINVAL;
   }
   if (backward && (!p->da || !p->db || !aligned(p->da, 16) || !aligned(p->db, 16)))
@@ -118,6 +140,11 @@ xshare_status run_adapters(const xshare_adapters_args* p, bool backward) {
       xs::adapters_layout(p->T, p->n_adapters, p->rank, p->n, p->d, backward);
   if (!p->ws || p->ws_bytes < A.total) return XSHARE_EWORKSPACE;
   if (!aligned(p->ws, 16)) return XSHARE_EINVAL;
+  // (some workgroups write out while others read x; the factors' gradients read x and dy after it)
+  const Rows out{p->out, p->ld_out, p->T, cols}, base{p->base, p->ld_base, p->T, cols};
+  if (overlap(out, {p->x, p->ldx, p->T, p->d}, 2) || (!same(out, base) && overlap(out, base, 2)) ||
+      (backward && overlap(out, {p->dy, p->lddy, p->T, p->n}, 2)))
+    return XSHARE_EINVAL;
   xs::AdaptersArgs a{};
   a.T = p->T;
   a.L = p->n_adapters;
@@ -186,6 +213,8 @@ xshare_status xshare_dispatch(const void* x, int64_t ldx, int32_t dtype, int32_t
   if (!valid_rows(x, dtype, ldx, d) || !valid_rows(out, dtype, ld_out, d) || !rows ||
       !aligned(rows, 4))
     return XSHARE_EINVAL;
+  if (overlap({x, ldx, T, d}, {out, ld_out, int64_t(T) * top_k, d}, bytes_of(dtype)))
+    return XSHARE_EINVAL;
   xs::MoveArgs a = move_args(dtype, T, top_k, d, rows);
   a.token = x;
   a.ld_token = ldx;
@@ -201,6 +230,8 @@ xshare_status xshare_combine(const void* src, int64_t ld_src, int32_t dtype, int
   if (st != XSHARE_OK || T == 0) return st;
   if (!valid_rows(src, dtype, ld_src, d) || !valid_rows(y, dtype, ldy, d) || !rows ||
       !aligned(rows, 4) || !aligned(w, 4))
+    return XSHARE_EINVAL;
+  if (overlap({src, ld_src, int64_t(T) * top_k, d}, {y, ldy, T, d}, bytes_of(dtype)))
     return XSHARE_EINVAL;
   xs::MoveArgs a = move_args(dtype, T, top_k, d, rows);
   a.row = src;
@@ -220,6 +251,10 @@ xshare_status xshare_combine_backward(const void* dy, int64_t lddy, const void* 
   if (!valid_rows(dy, dtype, lddy, d) || !valid_rows(src, dtype, ld_src, d) ||
       !valid_rows(dsrc, dtype, ld_dsrc, d) || !rows || !aligned(rows, 4) || !w || !aligned(w, 4) ||
       !dw || !aligned(dw, 4))
+    return XSHARE_EINVAL;
+  const Rows out{dsrc, ld_dsrc, int64_t(T) * top_k, d}, from{src, ld_src, out.rows, d};
+  if (overlap({dy, lddy, T, d}, out, bytes_of(dtype)) ||
+      (!same(from, out) && overlap(from, out, bytes_of(dtype))))
     return XSHARE_EINVAL;
   xs::MoveArgs a = move_args(dtype, T, top_k, d, rows);
   a.token = dy;
@@ -244,6 +279,7 @@ xshare_status xshare_grouped_linear(const uint16_t* x, int64_t ldx, const uint16
     return XSHARE_EINVAL;
   if (ldx > kMaxRowStride) return XSHARE_EUNSUPPORTED;
   if (const xshare_status bad = check_sums(P, ws, ws_bytes)) return bad;
+  if (overlap({x, ldx, P, k}, {y, ldy, P, n}, 2)) return XSHARE_EINVAL;
   xs::GroupedArgs a = grouped_args(P, n_groups, n, k, offsets, ws);
   a.x = x;
   a.ldx = ldx;
@@ -264,6 +300,7 @@ xshare_status xshare_grouped_linear_backward_x(const uint16_t* dy, int64_t lddy,
     return XSHARE_EINVAL;
   if (lddy > kMaxRowStride) return XSHARE_EUNSUPPORTED;
   if (const xshare_status bad = check_sums(P, ws, ws_bytes)) return bad;
+  if (overlap({dy, lddy, P, n}, {dx, lddx, P, k}, 2)) return XSHARE_EINVAL;
   xs::GroupedArgs a = grouped_args(P, n_groups, n, k, offsets, ws);
   a.dy = dy;
   a.lddy = lddy;

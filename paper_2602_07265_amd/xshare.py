@@ -1290,14 +1290,24 @@ def _order_rows(order, device):
     if rows.dim() != 2:
         raise ValueError("an order's rows are [T, k]")
     T, k = rows.shape
-    _fit(device, (rows, torch.int32, (T, k), "order's rows"))
+    if rows.dtype is not torch.int32 or rows.device != device or not rows.is_contiguous():
+        _fit(device, (rows, torch.int32, (T, k), "order's rows"))
     return rows, T, k
+
+
+def _is_whole(t, like, shape):
+    """Whether t is a matrix of shape without gaps, of like's type and device: the usual case, in few
+    lookups."""
+    return isinstance(t, torch.Tensor) and t.dtype is like.dtype and t.shape == shape \
+        and t.device == like.device and t.is_contiguous()
 
 
 def _matrix_out(t, like, shape, name):
     """A given output or a new one of shape, of like's type and device; and its row stride."""
     if t is None:
         return like.new_empty(shape), shape[1]
+    if _is_whole(t, like, shape):
+        return t, shape[1]
     ld = _rows(t, like.dtype, name, shape[1])
     _on(like.device, t, name)
     if t.shape[0] != shape[0]:
@@ -1307,6 +1317,8 @@ def _matrix_out(t, like, shape, name):
 
 def _matrix_in(t, like, shape, name):
     """The row stride of an input of shape, of like's type and device."""
+    if _is_whole(t, like, shape):
+        return shape[1]
     ld = _rows(t, like.dtype, name, shape[1])
     _on(like.device, t, name)
     if t.shape[0] != shape[0]:

@@ -12,8 +12,8 @@ from block_launches import RECORDER
 
 
 def group_launches(cases):
-    """For each case, ("linear" | "x" | "w", P, E, n, k), ("adapters" | "backward", T, L, r, n, d) or
-    ("order", T, k, E), the names of the kernels of one call, for instance
+    """For each case, ("linear" | "x" | "w", P, E, n, k), ("adapters" | "backward", T, L, r, n, d),
+    ("order", T, k, E) or ("beside", P, n, k, ld, apart), the names of the kernels of one call, for instance
     tile_kernel<0, 64, 32, 4, 1, 4, 64>."""
     with tempfile.TemporaryDirectory() as tmp:
         so = os.path.join(tmp, "recorder.so")
@@ -38,29 +38,34 @@ def _child():
     sys.path.insert(0, os.path.join(L.ROOT, "paper_2602_07265_amd"))
     import xshare as X
     X.LIB_PATH = request["lib"]
-    lib, fake, big = X.lib(), ctypes.c_void_p(1 << 20), 1 << 44
+    lib, fake, far, big = X.lib(), ctypes.c_void_p(1 << 20), ctypes.c_void_p(1 << 50), 1 << 44
     out = []
     for what, *c in request["cases"]:
         rec.recorder_clear()
         if what == "order":
             T, k, E = c
             status = lib.xshare_expert_order(fake, T, k, E, fake, fake, fake, fake, big, None)
+        elif what == "beside":
+            P, n, k, ld, apart = c                     # y lies `apart` elements from x, in rows of ld
+            status = lib.xshare_grouped_linear(fake, ld, fake, fake, P, 2, n, k,
+                                               ctypes.c_void_p(fake.value + 2 * apart), ld, fake, big,
+                                               None)
         elif what in ("adapters", "backward"):
             T, N, r, n, d = c
             cols = n if what == "adapters" else d
             a = X.AdaptersArgs(struct_size=ctypes.sizeof(X.AdaptersArgs), T=T, n_adapters=N, rank=r,
                                n=n, d=d, ldx=d, ld_out=cols, lddy=n, ws_bytes=big)
             for name in ("x", "a", "b", "ids", "out", "dy", "da", "db", "ws"):
-                setattr(a, name, fake)
+                setattr(a, name, far if name == "out" else fake)
             call = lib.xshare_adapters if what == "adapters" else lib.xshare_adapters_backward
             status = call(ctypes.byref(a))
         else:
             P, E, n, k = c
             if what == "linear":
-                status = lib.xshare_grouped_linear(fake, k, fake, fake, P, E, n, k, fake, n, fake,
+                status = lib.xshare_grouped_linear(fake, k, fake, fake, P, E, n, k, far, n, fake,
                                                    big, None)
             elif what == "x":
-                status = lib.xshare_grouped_linear_backward_x(fake, n, fake, fake, P, E, n, k, fake,
+                status = lib.xshare_grouped_linear_backward_x(fake, n, fake, fake, P, E, n, k, far,
                                                               k, fake, big, None)
             else:
                 status = lib.xshare_grouped_linear_backward_w(fake, n, fake, k, fake, P, E, n, k,

@@ -11,6 +11,7 @@ from test_block_sizes import BIG as PAST
 from test_block_sizes import OnGpu
 
 FAKE = ctypes.c_void_p(1 << 20)
+FAR = ctypes.c_void_p(1 << 30)
 ODD = ctypes.c_void_p((1 << 20) + 1)
 OFF8 = ctypes.c_void_p((1 << 20) + 8)
 BIG = (1 << 20) + 8
@@ -33,16 +34,16 @@ def test_order_refuses(kw, status):
     assert _order(**kw) == status
 
 
-def _dispatch(x=FAKE, ldx=40, dtype=0, T=8, k=2, d=40, rows=FAKE, out=FAKE, ld_out=40):
+def _dispatch(x=FAKE, ldx=40, dtype=0, T=8, k=2, d=40, rows=FAKE, out=FAR, ld_out=40):
     return X.lib().xshare_dispatch(x, ldx, dtype, T, k, d, rows, out, ld_out, None)
 
 
-def _combine(src=FAKE, ld=40, dtype=0, T=8, k=2, d=40, rows=FAKE, w=FAKE, y=FAKE, ldy=40):
+def _combine(src=FAKE, ld=40, dtype=0, T=8, k=2, d=40, rows=FAKE, w=FAKE, y=FAR, ldy=40):
     return X.lib().xshare_combine(src, ld, dtype, T, k, d, rows, w, y, ldy, None)
 
 
 def _backward(dy=FAKE, lddy=40, src=FAKE, ld=40, dtype=0, T=8, k=2, d=40, rows=FAKE, w=FAKE,
-              dsrc=FAKE, ldd=40, dw=FAKE):
+              dsrc=FAR, ldd=40, dw=FAKE):
     return X.lib().xshare_combine_backward(dy, lddy, src, ld, dtype, T, k, d, rows, w, dsrc, ldd, dw,
                                            None)
 
@@ -73,12 +74,12 @@ def test_a_move_refuses(call, kw, status):
     assert call(**kw) == status
 
 
-def _linear(x=FAKE, ldx=64, w=FAKE, offsets=FAKE, P=8, E=4, n=40, k=64, y=FAKE, ldy=40, ws=FAKE,
+def _linear(x=FAKE, ldx=64, w=FAKE, offsets=FAKE, P=8, E=4, n=40, k=64, y=FAR, ldy=40, ws=FAKE,
             ws_bytes=1 << 30):
     return X.lib().xshare_grouped_linear(x, ldx, w, offsets, P, E, n, k, y, ldy, ws, ws_bytes, None)
 
 
-def _linear_x(x=FAKE, ldx=64, w=FAKE, offsets=FAKE, P=8, E=4, n=64, k=40, y=FAKE, ldy=40, ws=FAKE,
+def _linear_x(x=FAKE, ldx=64, w=FAKE, offsets=FAKE, P=8, E=4, n=64, k=40, y=FAR, ldy=40, ws=FAKE,
               ws_bytes=1 << 30):
     return X.lib().xshare_grouped_linear_backward_x(x, ldx, w, offsets, P, E, n, k, y, ldy, ws,
                                                     ws_bytes, None)
@@ -124,6 +125,7 @@ def _adapters(call, **kw):
              ldx=40, ld_base=40, ld_out=40, lddy=40, ws_bytes=1 << 30)
     for name in ("x", "a", "b", "ids", "scales", "base", "out", "dy", "da", "db", "ws"):
         f[name] = FAKE
+    f["out"] = FAR
     f.update(kw)
     return getattr(X.lib(), call)(ctypes.byref(X.AdaptersArgs(**f)))
 
@@ -137,7 +139,7 @@ def _adapters(call, **kw):
     (dict(d=BIG), X.EUNSUPPORTED), (dict(x=None), X.EINVAL), (dict(x=OFF8), X.EINVAL),
     (dict(ldx=32), X.EINVAL), (dict(ldx=44), X.EINVAL), (dict(a=None), X.EINVAL),
     (dict(b=OFF8), X.EINVAL), (dict(ids=None), X.EINVAL), (dict(scales=ODD), X.EINVAL),
-    (dict(base=OFF8), X.EINVAL), (dict(ld_base=32), X.EINVAL), (dict(ld_base=48), X.EINVAL),
+    (dict(base=OFF8), X.EINVAL), (dict(ld_base=32), X.EINVAL), (dict(base=FAR, ld_base=48), X.EINVAL),
     (dict(out=None), X.EINVAL), (dict(ld_out=32), X.EINVAL), (dict(ws=None), X.EWORKSPACE),
     (dict(ws_bytes=512), X.EWORKSPACE), (dict(ws=OFF8), X.EINVAL)])
 def test_adapters_refuse(call, kw, status):
@@ -148,6 +150,31 @@ def test_adapters_refuse(call, kw, status):
 @pytest.mark.parametrize("kw", [dict(dy=None), dict(lddy=32), dict(da=None), dict(db=OFF8)])
 def test_adapters_backward_refuses(kw):
     assert _adapters("xshare_adapters_backward", **kw) == X.EINVAL
+
+
+def _past(elements, at=FAKE, size=2):
+    return ctypes.c_void_p(at.value + elements * size)
+
+
+@pytest.mark.parametrize("call", [
+    lambda: _dispatch(out=FAKE, dtype=1), lambda: _dispatch(out=_past(8 * 40 - 1), dtype=1),
+    lambda: _dispatch(x=_past(16 * 40 - 1, FAR, 4)), lambda: _combine(y=FAKE, k=1, dtype=1),
+    lambda: _combine(src=_past(8 * 40 - 1, FAR, 4)), lambda: _backward(dy=FAR, dtype=1),
+    lambda: _backward(dsrc=FAKE, src=FAR, dy=_past(16 * 40 - 1, FAKE, 4)),
+    lambda: _backward(dsrc=FAKE, src=_past(40, FAKE, 4), dy=FAR),
+    lambda: _backward(dsrc=FAKE, ldd=48, dy=FAR), lambda: _linear(y=FAKE, ldy=64),
+    lambda: _linear(y=_past(7 * 64 + 56)), lambda: _linear(x=_past(32), ldx=104, y=FAKE, ldy=104),
+    lambda: _linear(x=FAKE, ldx=104, y=_past(3 * 104 + 56), ldy=104),
+    lambda: _linear_x(y=FAKE, ldy=64),
+    lambda: _linear_x(y=_past(7 * 64 + 56)), lambda: _adapters("xshare_adapters", out=FAKE),
+    lambda: _adapters("xshare_adapters", out=FAKE, base=FAR, x=_past(7 * 40 + 32)),
+    lambda: _adapters("xshare_adapters", out=FAKE, base=_past(40), x=FAR),
+    lambda: _adapters("xshare_adapters", out=FAKE, ld_base=48, x=FAR),
+    lambda: _adapters("xshare_adapters_backward", x=FAR, dy=FAR, out=FAKE, base=_past(8)),
+    lambda: _adapters("xshare_adapters_backward", x=FAR, base=None, out=FAKE),
+    lambda: _adapters("xshare_adapters_backward", dy=FAR, base=None, out=FAKE)])
+def test_outputs_over_inputs(call):
+    assert call() == X.EINVAL
 
 
 def test_workspaces_serve_smaller_batches():

@@ -247,3 +247,32 @@ def test_calls_on_a_stream_that_is_not_current():
         torch.cuda.synchronize()
         for v in got:
             assert torch.equal(v, ref[name]), name
+
+
+def test_rows_side_by_side_in_one_buffer():
+    """Inputs and outputs that are columns of one buffer, their rows as far apart."""
+    from paper_2602_07265_amd import xshare as X
+    v = _inputs(3)
+    w13, _ = _weights()
+    o = X.expert_order(X.gate(v["logits"], K)["ids"], E)
+    want = X.grouped_linear(X.dispatch(v["x"], o), w13, o["offsets"])
+    buf = torch.zeros(T * K, D + 2 * F, device=DEV, dtype=torch.bfloat16)
+    X.dispatch(v["x"], o, out=buf[:, :D])
+    y = X.grouped_linear(buf[:, :D], w13, o["offsets"], y=buf[:, D:])
+    assert torch.equal(y, want) and torch.equal(buf[:, D:], want)
+
+
+def test_a_residual_as_base_is_not_the_output():
+    from paper_2602_07265_amd import xshare as X
+    x = _inputs(4)["x"]
+    g = torch.Generator(device=DEV).manual_seed(5)
+    a = torch.randn(4, 16, D, generator=g, device=DEV).to(torch.bfloat16)
+    b = torch.randn(4, D, 16, generator=g, device=DEV).to(torch.bfloat16)
+    ids = torch.randint(-1, 4, (T,), generator=g, device=DEV, dtype=torch.int32)
+    want = X.adapters(x, a, b, ids, base=x.clone())
+    assert torch.equal(X.adapters(x, a, b, ids, base=x), want)
+    for n in (T, 5):
+        with pytest.raises(X.XShareError):
+            X.adapters(x[:n], a, b, ids[:n], base=x[:n], out=x[:n])
+        with pytest.raises(X.XShareError):
+            X.adapters_backward(x[:n], want[:n], a, b, ids[:n], base=x[:n], out=dict(dx=x[:n]))

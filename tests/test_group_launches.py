@@ -59,3 +59,11 @@ def test_adapter_forms():
             assert names in (["few_kernel"], ["few_shrink_kernel", "few_expand_kernel"])
         elif what == "adapters":
             assert names[-3 if T <= 8192 else -4].startswith("order_") and len(names) in (3, 4)
+
+
+def test_columns_of_one_buffer_do_not_overlap():
+    cases = [("beside", 8, 40, 64, 104, 64), ("beside", 8, 40, 64, 104, -40),
+             ("beside", 8, 40, 64, 128, 88), ("beside", 8, 40, 64, 104, 4 * 104 + 64),
+             ("beside", 8, 40, 64, 104, 7 * 104 + 64), ("beside", 8, 40, 64, 64, 8 * 64),
+             ("beside", 8, 64, 64, 64, -8 * 64)]
+    assert all(len(names) == 1 for names in group_launches(cases))
