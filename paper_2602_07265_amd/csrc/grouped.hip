@@ -406,6 +406,7 @@ __global__ __launch_bounds__(512, 2) void turns_kernel(Product a) {
     __builtin_amdgcn_sched_barrier(0);
   };
   std::integral_constant<int, -1> reads;
+  std::integral_constant<int, 6> six;
   std::integral_constant<int, 8> eight;
   std::integral_constant<int, 12> twelve;
   // One block, a quarter of its products a turn: what a turn reads was loaded two blocks ago, and what
@@ -433,7 +434,40 @@ __global__ __launch_bounds__(512, 2) void turns_kernel(Product a) {
     meet(eight);                                       // and the rest of it
     multiply(1, 0);
   };
-  if (blocks > 0) {
+  // The same without the second half of B, which holds no rows: two turns (the three products
+  // of 554 rows of 12 groups by (2104, 9304) take 196 us, without it 257).
+  auto half_block = [&](int b, uint16_t* __restrict__ here, uint16_t* __restrict__ other) {
+    read_b(0, here + 2 * kHalf);
+    read_a(0, 0, here);
+    read_a(0, 1, here);
+    __builtin_amdgcn_sched_barrier(0);
+    load_a(b + 1, 1, other + kHalf);
+    meet(six);                                         // this block's second half of A is there
+    multiply(0, 0);
+    read_a(1, 0, here + kHalf);
+    read_a(1, 1, here + kHalf);
+    __builtin_amdgcn_sched_barrier(0);
+    load_a(b + 2, 0, here);
+    load_b(b + 2, 0, here + 2 * kHalf);
+    meet(six);                                         // and the next one's other halves
+    multiply(1, 0);
+  };
+  if (blocks > 0 && tile.live <= 128) {
+    load_a(0, 0, lds);
+    load_b(0, 0, lds + 2 * kHalf);
+    load_a(0, 1, lds + kHalf);
+    load_a(1, 0, lds + kStage);
+    load_b(1, 0, lds + kStage + 2 * kHalf);
+    meet(six);
+    if (wave >= 4) meet(reads);                        // the second group comes a turn later
+#pragma unroll 1
+    for (int b = 0; b < blocks; ++b) {
+      const int here = (b & 1) * kStage;
+      half_block(b, lds + here, lds + (kStage - here));
+    }
+    if (wave < 4) meet(reads);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load outlives the workgroup's LDS
+  } else if (blocks > 0) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       load_a(b, 0, lds + b * kStage);
@@ -607,11 +641,12 @@ const Form& form_for(const Form (&forms)[N], const Product& a, int groups, int r
     const Form& f = forms[i];
     if (f.units == kSplit && a.P < kTurnsRows) continue;
     const int columns = (a.columns + f.columns - 1) / f.columns;
-    // the rows of dW, or of groups: their last tile is half full on average (one's size is known)
-    const float mean = (float)a.P / groups;
+    // the rows of dW, or of groups: their last tile is half full on average (one's size is known);
+    // turns_kernel works on that in halves
+    const float mean = (float)a.P / groups, last = f.units == kSplit ? 0.25f : 0.5f;
     const float rows = a.out_rows ? (float)((a.out_rows + f.rows - 1) / f.rows)
                        : groups == 1 ? (float)((a.P + f.rows - 1) / f.rows)
-                       : mean > 1 ? mean / f.rows + 0.5f : 1.0f;
+                       : mean > 1 ? mean / f.rows + last : 1.0f;
     const float cost = form_cost(f, (float)groups * columns * (rows > 1 ? rows : 1.0f), reduction);
     if (i == 0 || cost < least) {
       best = i;

@@ -72,11 +72,14 @@ def test_products(case, lead, tail, pad):
 # Every form of the three products (test_group_launches checks that these are what the cases get): its
 # tile, whether tiles are split, and groups that leave tiles nearly empty, nearly full and empty.
 SKEW = [3000, 0, 1, 700, 4491]
+HALVES = [2176, 127, 2177, 3712]    # of 256 rows' tiles, the last ones: 128, 127, 129 and 128
 FORMS = [("linear", "64x32 x 2", [40, 0, 19, 1], 520, 2312), ("linear", "64x32 x 2", [1], 72, 10248),
          ("linear", "64x32", [700, 0, 300, 1], 520, 2312), ("linear", "64x64", [700, 0, 300, 1], 1032, 1096),
          ("linear", "128x64", [700, 0, 300, 1], 2312, 520), ("linear", "turns", SKEW, 2312, 520),
          ("linear", "turns", SKEW, 2048, 4104), ("linear", "turns", [8192], 4104, 264),
-         ("linear", "turns", [5000, 3191], 2304, 1000), ("linear", "turns", [4096], 4096, 1032),
+         ("linear", "turns", [5000, 3191], 2304, 1000),
+         ("linear", "turns", HALVES, 2312, 520), ("linear", "turns", HALVES, 2048, 4104),
+         ("x", "turns", HALVES, 2056, 4104), ("linear", "turns", [4096], 4096, 1032),
          ("x", "64x32 x 2", [700, 0, 300, 1], 2312, 520), ("x", "64x32 x 2", [0, 33], 10248, 72),
          ("x", "64x32", [700, 0, 300, 1], 520, 520), ("x", "64x64", [700, 0, 300, 1], 1032, 1096),
          ("x", "128x64", SKEW, 1032, 1096), ("x", "128x64", SKEW, 520, 2312),
