@@ -6,7 +6,7 @@
 // One kernel computes a tile [BB output rows, BA output columns] from two operands in LDS, blocks
 // of 64 of the reduction at a time.  The output's columns are the matrix instruction's rows (A),
 // the output's rows its columns (B), so a lane's four results are neighbours in a row of the
-// output.  An operand lies either along the reduction (rows of x, dy, and of W going forward) or
+// output (dW's the other way round, see store).  An operand lies either along the reduction (rows of x, dy, and of W going forward) or
 // across it (W in dx, both operands of dW); what lies across is read from LDS by transposing
 // loads, four reductions of one column in each.  Loads go straight to LDS, 16 bytes a lane; 16-byte
 // pieces are swapped within a row so that the reads of the instruction's operands hit
@@ -149,28 +149,60 @@ __device__ __forceinline__ bool find_tile(const Product& p, Tile& t) {
   return true;
 }
 
-// The results of 16 output rows (`r` this lane's, of the tile) and MA column tiles from column c on:
-// lane (n, g) holds columns 4 g .. 4 g + 3 of each tile in row n; kSpread: of the pairs that
-// tile_kernel deals.
+// One product of operands; dW's the other way round, so that a lane's results are a column's.
+template <Kind kKind>
+__device__ __forceinline__ floatx4 multiply_add(const bf16x8& a, const bf16x8& b, const floatx4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(kKind == kGradW ? b : a, kKind == kGradW ? a : b, c, 0,
+                                                 0, 0);
+}
+
+// The results of 16 output rows from r0 on and MA column tiles from column c on.  Lane (n, g) holds
+// columns 4 g .. 4 g + 3 of each tile in row n; kSpread: of the pairs that tile_kernel deals; kGradW:
+// rows 4 g .. 4 g + 3 of column n, so that 16 lanes store 64 neighbouring bytes and not 16 of each of 16
+// rows (dW of 128 groups of 256 rows by (1536, 2048): 502 us, 558 the other way; 64 of 64 rows by
+// (2048, 1536): 185 us, 224).
 template <Kind kKind, bool kSpread, int MA>
-__device__ __forceinline__ void store(const Product& a, const Tile& t, int r, int c, int g,
+__device__ __forceinline__ void store(const Product& a, const Tile& t, int r0, int c, int n, int g,
                                       const floatx4 (&v)[MA]) {
-  if (r >= t.live) return;
   if constexpr (kKind == kGradW) {
-    const size_t row = ((size_t)t.e * a.out_rows + t.first + r) * a.columns;
+    const size_t first = ((size_t)t.e * a.out_rows + t.first + r0 + 4 * g) * a.columns;
+    const int live = t.live - r0 - 4 * g;
+    if (a.dw_fp32) {
+      auto rows = [&](auto accumulate) {               // (one question, not one for each value)
 #pragma unroll
-    for (int m = 0; m < MA; ++m) {
-      const int at = c + 16 * m + 4 * g;
-      if (at >= a.columns) continue;                   // (columns come in eights)
-      if (a.dw_fp32) {
-        floatx4* const out = reinterpret_cast<floatx4*>(static_cast<float*>(a.dw) + row + at);
-        *out = a.accumulate ? *out + v[m] : v[m];
-      } else {
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dw) + row + at) =
-            make_uint2(to_bf16x2(v[m][0], v[m][1]), to_bf16x2(v[m][2], v[m][3]));
+        for (int j = 0; j < 4; ++j) {
+          float* const out = static_cast<float*>(a.dw) + first + (size_t)j * a.columns;
+#pragma unroll
+          for (int m = 0; m < MA; ++m) {
+            const int at = c + 16 * m + n;
+            if (j < live && at < a.columns) out[at] = accumulate ? out[at] + v[m][j] : v[m][j];
+          }
+        }
+      };
+      if (a.accumulate)
+        rows(std::true_type());
+      else
+        rows(std::false_type());
+    } else {
+      const bool odd = n & 1;                          // two columns of rows j (even lanes), j + 1 (odd)
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        const int row = j + odd;
+        uint16_t* const out = static_cast<uint16_t*>(a.dw) + first + (size_t)row * a.columns;
+#pragma unroll
+        for (int m = 0; m < MA; ++m) {
+          const int at = c + 16 * m + (n & ~1);
+          const float mine = odd ? v[m][j + 1] : v[m][j], other = odd ? v[m][j] : v[m][j + 1];
+          const float next = __int_as_float(
+              __builtin_amdgcn_mov_dpp(__float_as_int(other), 0xB1, 0xF, 0xF, true));  // lane n ^ 1's
+          if (row < live && at < a.columns)
+            *reinterpret_cast<uint32_t*>(out + at) = to_bf16x2(odd ? next : mine, odd ? mine : next);
+        }
       }
     }
   } else {
+    const int r = r0 + n;
+    if (r >= t.live) return;
     uint16_t* const out = a.out + (size_t)(t.first + r) * a.ldo;
     if constexpr (kSpread) {
 #pragma unroll
@@ -267,7 +299,7 @@ __global__ __launch_bounds__(64 * WA * WB * kGroups) void tile_kernel(Product a)
       for (int t = 0; t < MB; ++t)
 #pragma unroll
         for (int m = 0; m < MA; ++m)
-          acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[m], fb[t], acc[m][t], 0, 0, 0);
+          acc[m][t] = multiply_add<kKind>(fa[m], fb[t], acc[m][t]);
     }
   };
   if (blocks > 0) {
@@ -302,7 +334,7 @@ __global__ __launch_bounds__(64 * WA * WB * kGroups) void tile_kernel(Product a)
     floatx4 v[MA];
 #pragma unroll
     for (int m = 0; m < MA; ++m) v[m] = acc[m][t];
-    store<kKind, kSpread>(a, tile, wb * MB * 16 + 16 * t + n, tile.c0 + wa * MA * 16, g, v);
+    store<kKind, kSpread>(a, tile, wb * MB * 16 + 16 * t, tile.c0 + wa * MA * 16, n, g, v);
   }
 }
 
@@ -397,8 +429,8 @@ __global__ __launch_bounds__(512, 2) void turns_kernel(Product a) {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int m = 0; m < 4; ++m)
-          acc[ha][hb][t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[ha][s][m], fb[hb][s][t],
-                                                                      acc[ha][hb][t][m], 0, 0, 0);
+          acc[ha][hb][t][m] =
+              multiply_add<kKind>(fa[ha][s][m], fb[hb][s][t], acc[ha][hb][t][m]);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
@@ -498,8 +530,8 @@ __global__ __launch_bounds__(512, 2) void turns_kernel(Product a) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int ha = 0; ha < 2; ++ha)
-        store<kKind, kSpread>(a, tile, hb * 128 + wb * 32 + 16 * t + n, tile.c0 + ha * 128 + wa * 64,
-                              g, acc[ha][hb][t]);
+        store<kKind, kSpread>(a, tile, hb * 128 + wb * 32 + 16 * t, tile.c0 + ha * 128 + wa * 64, n, g,
+                              acc[ha][hb][t]);
 }
 
 // The parts of the tiles that turns_kernel splits, summed in order and stored: workgroup (quarter,
@@ -524,8 +556,8 @@ __global__ __launch_bounds__(512) void join_kernel(Product a) {
 #pragma unroll
       for (int m = 0; m < 4; ++m)
         v[m] += from[(size_t)p * kTileQuads + (16 * ha + 8 * hb + 4 * t + m) * 512];
-    store<kKind, kSpread>(a, tile, hb * 128 + wb * 32 + 16 * t + (lane & 15),
-                          tile.c0 + ha * 128 + wa * 64, lane >> 4, v);
+    store<kKind, kSpread>(a, tile, hb * 128 + wb * 32 + 16 * t, tile.c0 + ha * 128 + wa * 64, lane & 15,
+                          lane >> 4, v);
   }
 }
 
