@@ -159,8 +159,8 @@ __device__ __forceinline__ floatx4 multiply_add(const bf16x8& a, const bf16x8& b
 // The results of 16 output rows from r0 on and MA column tiles from column c on.  Lane (n, g) holds
 // columns 4 g .. 4 g + 3 of each tile in row n; kSpread: of the pairs that tile_kernel deals; kGradW:
 // rows 4 g .. 4 g + 3 of column n, so that 16 lanes store 64 neighbouring bytes and not 16 of each of 16
-// rows (dW of 128 groups of 256 rows by (1536, 2048): 502 us, 558 the other way; 64 of 64 rows by
-// (2048, 1536): 185 us, 224).
+// rows (dW of 128 groups of 256 rows by (1536, 2048): 471 us, 558 the other way, of which 273 are the
+// stores alone; 64 of 64 rows by (2048, 1536): 158 us, 191.  y and dx took no less time so).
 template <Kind kKind, bool kSpread, int MA>
 __device__ __forceinline__ void store(const Product& a, const Tile& t, int r0, int c, int n, int g,
                                       const floatx4 (&v)[MA]) {
@@ -611,13 +611,15 @@ hipError_t launch_turns(Product a, hipStream_t stream) {
 
 // The forms of a product: its tile, and what it costs in microseconds: 64 of the reduction, `few` with
 // little else on the GPU, `full` for each tile that every compute unit has to work on, and `out`, what a
-// tile takes besides (finding its rows, the first loads, the stores).  Measured over 1 to 64 groups of
-// 1 to 4096 rows by ten shapes of 72 to 10304; there the rule's choice took 3.5 % (forward) and 4.7 %
-// (dx) longer than the fastest form on average, and within 10 % of it in 160 of 184 and 147 of 178.
+// tile takes besides (finding its rows, the first loads, the stores).  Measured over 1 to 256 groups of
+// 1 to 16384 rows by ten shapes of 72 to 10304; there the rule's choice took 3.5 % (forward), 4.7 % (dx)
+// and 2.1 % (dW) longer than the fastest form on average, and within 10 % of it in 160 of 184, 147 of
+// 178 and 299 of 325.
 // Both sides, in the forms' order without the first: 64 rows of one group by (4096, 4096) 15.7, 18.5,
 // 23.7 and 70 us (29.7 split); 1024 rows 73, 53, 43 and 76 (53); 4096 rows 285, 195, 154 and 97 (99);
 // 512 rows in each of 8 groups 349, 268, 220 and 172 (149).  The first against the second: one row by
-// (256, 10304) 22.7 and 32 us.
+// (256, 10304) 22.7 and 32 us.  dW of 256 rows in each of 64 groups by (7592, 344) 425, 353, 280 and
+// 293 us; of 4096 rows in each of 4 by (512, 4096) 90, 86, 158 and 109.
 enum Units { kShared, kAlone, kSplit };  // tiles of a unit: several, one, one and the last round split
 struct Form {
   int columns, rows;
@@ -640,16 +642,16 @@ const Form kGradXForms[] = {
     {256, 256, 1.30f, 1.55f, 12.0f, kSplit, launch_turns<kGradX>},
 };
 const Form kGradWForms[] = {
-    {128, 64, 0.60f, 0.42f, 1.4f, kShared, launch_tile<kGradW, 128, 64, 2, 2, 3, 32>},
-    {128, 128, 0.82f, 0.64f, 2.8f, kShared, launch_tile<kGradW, 128, 128, 2, 2, 3, 32>},
-    {256, 256, 1.30f, 1.5f, 12.5f, kAlone, launch_tile<kGradW, 256, 256, 2, 4, 4, 32>},
-    {256, 256, 1.30f, 1.65f, 12.5f, kSplit, launch_turns<kGradW>},
+    {128, 64, 0.46f, 0.41f, 1.4f, kShared, launch_tile<kGradW, 128, 64, 2, 2, 3, 32>},
+    {128, 128, 0.92f, 0.51f, 3.1f, kShared, launch_tile<kGradW, 128, 128, 2, 2, 3, 32>},
+    {256, 256, 2.53f, 1.48f, 12.5f, kAlone, launch_tile<kGradW, 256, 256, 2, 4, 4, 32>},
+    {256, 256, 0.77f, 1.33f, 20.4f, kSplit, launch_turns<kGradW>},
 };
 
-float form_cost(const Form& f, float tiles, int reduction) {
+float form_cost(const Form& f, float out, float tiles, int reduction) {
   const float blocks = (float)((reduction + kBlock - 1) / kBlock);
   if (f.units == kShared) {
-    const float round = tiles / kUnits, full = blocks * f.full + f.out;
+    const float round = tiles / kUnits, full = blocks * f.full + out;
     float some = blocks * f.few;
     if (full > some) some += (full - some) * (round < 1 ? round : 1);
     return full * round > some ? full * round : some;
@@ -658,8 +660,8 @@ float form_cost(const Form& f, float tiles, int reduction) {
   if (f.units == kSplit) s = shares_of(s.whole, reduction);
   const long rounds = (s.whole + kUnits - 1) / kUnits;
   const int left = (int)(s.whole - (rounds - 1) * kUnits);       // tiles of the last whole round
-  float cost = rounds * (blocks * f.full + f.out);
-  if (rounds > 0) cost -= (blocks * (f.full - f.few) + f.out) * (1.0f - (float)left / kUnits);
+  float cost = rounds * (blocks * f.full + out);
+  if (rounds > 0) cost -= (blocks * (f.full - f.few) + out) * (1.0f - (float)left / kUnits);
   if (s.rest == 0) return cost;
   const int more = s.rest * s.parts;                   // parts, each written and read again
   return cost + blocks * (f.few + (f.full - f.few) * more / kUnits) / s.parts + 4.0f + 0.1f * more;
@@ -679,7 +681,11 @@ const Form& form_for(const Form (&forms)[N], const Product& a, int groups, int r
     const float rows = a.out_rows ? (float)((a.out_rows + f.rows - 1) / f.rows)
                        : groups == 1 ? (float)((a.P + f.rows - 1) / f.rows)
                        : mean > 1 ? mean / f.rows + last : 1.0f;
-    const float cost = form_cost(f, (float)groups * columns * (rows > 1 ? rows : 1.0f), reduction);
+    // of dW's tiles, much of which is their stores, the part that is there
+    const float cover =
+        a.out_rows ? (float)a.columns * a.out_rows / ((float)columns * f.columns * rows * f.rows) : 1.0f;
+    const float cost =
+        form_cost(f, f.out * cover, (float)groups * columns * (rows > 1 ? rows : 1.0f), reduction);
     if (i == 0 || cost < least) {
       best = i;
       least = cost;

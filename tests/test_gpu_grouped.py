@@ -86,7 +86,8 @@ FORMS = [("linear", "64x32 x 2", [40, 0, 19, 1], 520, 2312), ("linear", "64x32 x
          ("x", "turns", SKEW, 2056, 4104),
          ("x", "turns", [5000, 3191], 264, 4104),
          ("w", "128x64", [700, 0, 300, 1], 264, 520), ("w", "128x128", SKEW, 1032, 1096),
-         ("w", "256x256", [900, 0, 1, 33, 511, 512, 1531, 512], 2056, 2056), ("w", "turns", [8192], 1032, 1096),
+         ("w", "256x256", [900, 0, 1, 33, 511, 512, 1531, 512], 1016, 2040),
+         ("w", "256x256", [900, 0, 1, 33, 511, 512, 1531, 512], 2048, 4104), ("w", "turns", [8192], 1032, 1096),
          ("w", "turns", [8191], 264, 520), ("w", "turns", [8191, 2], 2048, 4104)]
 
 
