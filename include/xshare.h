@@ -734,7 +734,7 @@ xshare_status xshare_block_experts(const xshare_block_experts_args* args);
  * ---------------------------------------------------------------------------------------- */
 
 /* Workspace of xshare_expert_order (bytes, 256-aligned); 0 where it needs none (T * top_k up to
- * 8192) and for invalid sizes.  That of T tokens serves any smaller T too.                  */
+ * 4096) and for invalid sizes.  That of T tokens serves any smaller T too.                  */
 size_t xshare_expert_order_workspace_bytes(int32_t T, int32_t top_k, int32_t n_experts);
 
 /*

@@ -24,13 +24,22 @@ struct OrderArgs {
   int32_t* pair_of;            // [pairs]
   int32_t* counts;             // [order_parts(pairs), E], unused by one workgroup
 };
-constexpr int kOrderOne = 8192;     // pairs that one workgroup sorts by itself
-constexpr int kOrderPart = 4096;    // pairs of a workgroup where there are several
-inline int order_parts(int pairs) {
-  return pairs <= kOrderOne ? 0 : (pairs + kOrderPart - 1) / kOrderPart;
+constexpr int kOrderOne = 4096;     // pairs that one workgroup sorts by itself
+constexpr int kOrderMost = 8192;    // and can
+constexpr int kOrderParts = 64;     // workgroups where there are several, as far as that goes
+inline int order_part(int pairs) {
+  int part = 1024;                  // pairs of a workgroup
+  while (part < kOrderMost && pairs > kOrderParts * part) part *= 2;
+  return part;
 }
+inline int order_parts(int pairs) {
+  return pairs <= kOrderOne ? 0 : (pairs + order_part(pairs) - 1) / order_part(pairs);
+}
+// (the counts of as many parts as fewer pairs may have)
 inline size_t order_bytes(int pairs, int E) {
-  return align256(sizeof(int32_t) * size_t(order_parts(pairs)) * E);
+  if (pairs <= kOrderOne) return 0;
+  const int parts = order_parts(pairs);
+  return align256(sizeof(int32_t) * size_t(parts > kOrderParts ? parts : kOrderParts) * E);
 }
 hipError_t launch_order(const OrderArgs& a, hipStream_t stream);
 

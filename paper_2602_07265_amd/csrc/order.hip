@@ -5,10 +5,13 @@
 // lanes that hold the same expert find each other by one ballot for each bit of the id, so that
 // a lane's place among them is a count of lower lanes and nothing depends on the order of
 // atomics.  One workgroup sorts up to kOrderOne pairs in one launch; more go in two: the counts
-// of each workgroup's part, then every workgroup sums the parts before its own.
+// of each workgroup's part, then every workgroup sums the parts before its own.  Both sides at 4096
+// pairs of 128 experts: 6.9 and 6.6 us (which need a workspace); at 8192 of 256: 12.0 and 6.4.
 //
 // A call reads and writes 12 bytes a pair, 1.6 MB at 131072 pairs: the launches and the waves'
-// chains over their runs bound it.
+// chains over their runs bound it.  32768 pairs of 256 experts take 7.5 us, 131072 10.0 and 2^20 22
+// (0.6 TB/s).  In parts of 4096 pairs, of which a wave has four steps: 10.1, 10.8 and 23; of 2048
+// pairs 2^20 take 32, for each workgroup sums the counts of all 512.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -50,8 +53,8 @@ __device__ __forceinline__ int key_of(const OrderArgs& a, int i, int end) {
 
 // The run of consecutive pairs of a wave among those that its workgroup sorts, and each pair's place
 // among its expert's in the run, of which it keeps the counts.
+template <int kSteps>                                  // of 64 pairs, at most
 struct Run {
-  static constexpr int kSteps = kOrderOne / kThreads;  // of 64 pairs, at most
   int first, last;
   int key[kSteps], rank[kSteps];
 
@@ -117,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void order_kernel(OrderArgs a, int part_s
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int begin = kParts ? blockIdx.x * part_size : 0;
   const int end = kParts ? min(begin + part_size, a.pairs) : a.pairs;
-  Run run(begin, end, wave);
+  Run<(kParts ? kOrderMost : kOrderOne) / kThreads> run(begin, end, wave);
   int* const mine = lds + wave * a.E;
   run.count(a, mine, bits, lane);
   // thread e: expert e's pairs in all parts and in those before this one
@@ -172,7 +175,7 @@ hipError_t launch_order(const OrderArgs& a, hipStream_t stream) {
   int bits = 1;
   while ((1 << bits) <= a.E) ++bits;                   // keys 0 .. E
   const size_t lds = sizeof(int) * (size_t(kWaves) * a.E + kWaves);
-  const int parts = order_parts(a.pairs);
+  const int parts = order_parts(a.pairs), part = order_part(a.pairs);
   const auto kernel = parts ? order_kernel<true> : order_kernel<false>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
@@ -180,8 +183,8 @@ hipError_t launch_order(const OrderArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   if (parts)
-    order_count_kernel<<<parts, kThreads, sizeof(int) * a.E, stream>>>(a, kOrderPart);
-  kernel<<<parts ? parts : 1, kThreads, lds, stream>>>(a, kOrderPart, bits);
+    order_count_kernel<<<parts, kThreads, sizeof(int) * a.E, stream>>>(a, part);
+  kernel<<<parts ? parts : 1, kThreads, lds, stream>>>(a, part, bits);
   return hipGetLastError();
 }
 

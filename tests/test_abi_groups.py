@@ -178,6 +178,9 @@ def test_outputs_over_inputs(call):
 
 
 def test_workspaces_serve_smaller_batches():
+    assert X.expert_order_workspace_bytes(512, 8, 300) == 0
+    edges = [X.expert_order_workspace_bytes(T, 1, 300) for T in (4097, 65536, 65537, 524288, 1 << 20)]
+    assert edges == sorted(edges) and edges[0] > 0
     a = [X.adapters_workspace_bytes(T, 5, 24, 400, 4096, True) for T in range(0, 9000, 37)]
     o = [X.expert_order_workspace_bytes(T, 8, 300) for T in range(0, 9000, 37)]
     p = [X.grouped_linear_workspace_bytes(P, 8, 40, 64) for P in range(0, 9000, 37)]

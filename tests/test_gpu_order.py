@@ -48,7 +48,8 @@ def _ids(T, k, n, kind, seed=0):
 # one workgroup and its last size, several and their parts' edges
 @pytest.mark.parametrize("T,k,n", [(1, 1, 1), (1, 8, 256), (1, 32, 1024), (33, 2, 7), (129, 8, 1),
                                    (1024, 8, 256), (8192, 1, 1024), (8193, 1, 63), (2731, 3, 64),
-                                   (4096, 5, 65), (16384, 8, 128)])
+                                   (4096, 5, 65), (16384, 8, 128), (512, 8, 1024), (4097, 1, 63),
+                                   (8192, 8, 300), (65537, 1, 1024), (32768, 16, 9), (524289, 1, 33)])
 @pytest.mark.parametrize("kind", ["random", "dropped", "none", "one", "wild", "sorted"])
 def test_order(T, k, n, kind):
     say(f"order case T={T} k={k} n={n} {kind}")

@@ -36,7 +36,7 @@ def test_many_tiles_are_not_split():
 
 
 def test_order_in_one_launch_or_two():
-    got = group_launches([("order", 1, 1, 1), ("order", 1024, 8, 256), ("order", 8193, 1, 63)])
+    got = group_launches([("order", 1, 1, 1), ("order", 512, 8, 256), ("order", 4097, 1, 63)])
     assert got == [["order_kernel<false>"], ["order_kernel<false>"],
                    ["order_count_kernel", "order_kernel<true>"]]
 
@@ -58,7 +58,7 @@ def test_adapter_forms():
         if what == "adapters" and T <= 64:
             assert names in (["few_kernel"], ["few_shrink_kernel", "few_expand_kernel"])
         elif what == "adapters":
-            assert names[-3 if T <= 8192 else -4].startswith("order_") and len(names) in (3, 4)
+            assert names[-3 if T <= 4096 else -4].startswith("order_") and len(names) in (3, 4)
 
 
 def test_columns_of_one_buffer_do_not_overlap():
