@@ -10,6 +10,10 @@
 // that the products with them are as exact as those of fp32 values; y and dx, which are rounded
 // to bf16, take two of the three.  Going backward the factors are transposed first, which are
 // small beside the rows, and dh and dx are the two forward products on them.
+//
+// 4000 tokens of 5 adapters of rank 16, n = d = 4096: h 12.6 us (33 MB, 2.6 TB/s: 251 workgroups, each a
+// chain of loads), y 13.8 (66 MB, 4.8 TB/s), h and dh in one launch 19.9 (3.3 TB/s), the factors'
+// gradients 16.5 (4.0 TB/s), the order 4.9 and the transposed factors 3.0.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

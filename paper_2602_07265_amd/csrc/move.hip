@@ -3,7 +3,9 @@
 // rows[t, r] is the row of pair (t, r), or no row at all.  Dispatch reads a token once and writes its
 // rows; combine reads a token's rows, sums them in rank order in fp32, weighted, and rounds once
 // (the gradient of dispatch is the same without weights); combine's gradient takes a wave for each
-// pair: dR = w dy and dw = <dy, R> in one pass over both.  All are bound by memory.
+// pair: dR = w dy and dw = <dy, R> in one pass over both.  All are bound by memory: 4099 tokens of 2048
+// bf16 values, 4 of 8 pairs of each with a row, take 18 us each way (84 MB, 4.7 TB/s) and 26 back
+// through combine (151 MB, 5.8 TB/s).
 //
 // Rows of any length and alignment are moved 16 bytes at a time: the GPU's vector loads and stores
 // need no more than the element's alignment (AnyVec says so to the compiler).
