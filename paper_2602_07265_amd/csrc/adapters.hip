@@ -173,14 +173,25 @@ __global__ __launch_bounds__(256) void transpose_kernel(Transposed a, Transposed
       make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
-// v as three bf16 values that sum up to it (to 24 bits); infinities and NaN as one.
-__device__ __forceinline__ void split3(float v, uint16_t (&p)[3]) {
-  p[0] = to_bf16(v);
-  const float hi = value(p[0]);
-  const bool finite = fabsf(hi) < __builtin_inff();
-  const float rest = finite ? v - hi : 0.0f;
-  p[1] = to_bf16(rest);
-  p[2] = to_bf16(rest - value(p[1]));
+// Eight elements of a row from k on, or zeros in their place (the load of the row's first goes on).
+__device__ __forceinline__ uint4 load8(const uint16_t* row, int k, bool in) {
+  const uint4 v = *reinterpret_cast<const uint4*>(row + (in ? k : 0));
+  return make_uint4(in ? v.x : 0, in ? v.y : 0, in ? v.z : 0, in ? v.w : 0);
+}
+
+// Two values, each as three bf16 values that sum up to it (to 24 bits); infinities and NaN as one.
+struct Split {
+  uint32_t p0, p1, p2;
+};
+__device__ __forceinline__ Split split3(float lo, float hi) {
+  Split s;
+  s.p0 = to_bf16x2(lo, hi);
+  const float lo0 = __uint_as_float(s.p0 << 16), hi0 = __uint_as_float(s.p0 & 0xFFFF0000u);
+  lo = fabsf(lo0) < __builtin_inff() ? lo - lo0 : 0.0f;
+  hi = fabsf(hi0) < __builtin_inff() ? hi - hi0 : 0.0f;
+  s.p1 = to_bf16x2(lo, hi);
+  s.p2 = to_bf16x2(lo - __uint_as_float(s.p1 << 16), hi - __uint_as_float(s.p1 & 0xFFFF0000u));
+  return s;
 }
 
 struct Shrink {
@@ -200,14 +211,11 @@ struct Tokens {                // in adapters' order
 // Four values of h of one token, ranks `rank` on, as its three parts; past the rank zeros.
 template <int JT>
 __device__ __forceinline__ void store_h(uint16_t* row, int rank, int r, const floatx4& v, float s) {
-  uint16_t parts[4][3];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) split3(rank + c < r ? v[c] * s : 0.0f, parts[c]);
-#pragma unroll
-  for (int q = 0; q < 3; ++q)
-    *reinterpret_cast<uint2*>(row + q * 16 * JT + rank) =
-        make_uint2(parts[0][q] | (uint32_t)parts[1][q] << 16,
-                   parts[2][q] | (uint32_t)parts[3][q] << 16);
+  const Split a = split3(rank < r ? v[0] * s : 0.0f, rank + 1 < r ? v[1] * s : 0.0f);
+  const Split b = split3(rank + 2 < r ? v[2] * s : 0.0f, rank + 3 < r ? v[3] * s : 0.0f);
+  *reinterpret_cast<uint2*>(row + rank) = make_uint2(a.p0, b.p0);
+  *reinterpret_cast<uint2*>(row + 16 * JT + rank) = make_uint2(a.p1, b.p1);
+  *reinterpret_cast<uint2*>(row + 32 * JT + rank) = make_uint2(a.p2, b.p2);
 }
 
 template <int JT, int BB>
@@ -246,7 +254,6 @@ __global__ __launch_bounds__(512) void shrink_kernel(Tokens o, Shrink first_a, S
   for (int j = 0; j < JT; ++j)
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[j][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  const uint4 zero = make_uint4(0, 0, 0, 0);
   for (int k0 = 64 * kAhead * wave; k0 < a.K; k0 += 64 * kAhead * kWaves) {
     uint4 fx[2 * kAhead][MT], fw[2 * kAhead][JT];
 #pragma unroll
@@ -254,9 +261,9 @@ __global__ __launch_bounds__(512) void shrink_kernel(Tokens o, Shrink first_a, S
       const int k = k0 + 32 * s + 8 * g;
       const bool in = k < a.K;
 #pragma unroll
-      for (int t = 0; t < MT; ++t) fx[s][t] = in ? *reinterpret_cast<const uint4*>(x[t] + k) : zero;
+      for (int t = 0; t < MT; ++t) fx[s][t] = load8(x[t], k, in);
 #pragma unroll
-      for (int j = 0; j < JT; ++j) fw[s][j] = in ? *reinterpret_cast<const uint4*>(w[j] + k) : zero;
+      for (int j = 0; j < JT; ++j) fw[s][j] = load8(w[j], k, in);
     }
 #pragma unroll
     for (int s = 0; s < 2 * kAhead; ++s)
@@ -420,14 +427,13 @@ __global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int gro
   const float scale = a.scales ? a.scales[e] : 1.0f;
   const uint16_t* const w = a.w + (size_t)e * a.N * o.r;
   const int end = min(c0 + a.columns, a.N);
-  const uint4 zero = make_uint4(0, 0, 0, 0);
   // W's rows go with both parts of h: with 16 ranks the parts lie in one operand, else in two
   constexpr int kSteps = JT == 1 ? 1 : JT / 2;
   uint4 fw[2][kSteps], base[MT];
   auto fetch = [&](int c) {                            // under way while the columns before are stored
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      base[t] = zero;
+      base[t] = make_uint4(0, 0, 0, 0);
       if (a.base && 16 * t + n < live && c + 8 * g < a.N)
         base[t] = *reinterpret_cast<const uint4*>(a.base + token[t] * a.ld_base + c + 8 * g);
     }
@@ -437,7 +443,7 @@ __global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int gro
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         const int j = (32 * s + 8 * g) % (16 * JT);
-        fw[m][s] = j < o.r ? *reinterpret_cast<const uint4*>(w + (size_t)col * o.r + j) : zero;
+        fw[m][s] = load8(w + (size_t)col * o.r, j, j < o.r);
       }
     }
   };
