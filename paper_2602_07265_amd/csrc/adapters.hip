@@ -8,12 +8,12 @@
 // lane for each of y.  More are put in adapters' order first, and tiles of tokens of one adapter
 // go through the matrix instructions.  h and dh are held as sums of three bf16 values (24 bits), so
 // that the products with them are as exact as those of fp32 values; y and dx, which are rounded
-// to bf16, take two of the three.  Going backward the factors are transposed first, which are
-// small beside the rows, and dh and dx are the two forward products on them.
+// to bf16, take two of the three.  Going backward the factors are transposed first (order.hip), which
+// are small beside the rows, and dh and dx are the two forward products on them.
 //
 // 4000 tokens of 5 adapters of rank 16, n = d = 4096: h 12.6 us (33 MB, 2.6 TB/s: 251 workgroups, each a
 // chain of loads), y 13.8 (66 MB, 4.8 TB/s), h and dh in one launch 19.9 (3.3 TB/s), the factors'
-// gradients 16.5 (4.0 TB/s), the order 4.9 and the transposed factors 3.0.
+// gradients 16.5 (4.0 TB/s), the order, with the transposed factors beside it or without, 5.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -147,31 +147,6 @@ __global__ __launch_bounds__(1024) void few_kernel(AdaptersArgs a) {
 }
 
 // ---------------------------------------------------------------------------- many tokens
-
-// A matrix [rows, cols] of each adapter with tokens -> [cols, rows].
-struct Transposed {
-  const uint16_t* in;
-  uint16_t* out;
-  int rows, cols;
-  int groups() const { return (int)(((size_t)rows / 8 * cols + 255) / 256); }
-};
-// Both factors; a thread takes eight rows of a column.
-__global__ __launch_bounds__(256) void transpose_kernel(Transposed a, Transposed b, int groups_a,
-                                                        const int32_t* offsets) {
-  const int e = blockIdx.y;
-  if (offsets[e] == offsets[e + 1]) return;
-  const bool first = (int)blockIdx.x < groups_a;
-  const Transposed m = first ? a : b;
-  const size_t i = (size_t)(first ? blockIdx.x : blockIdx.x - groups_a) * 256 + threadIdx.x;
-  const int c = (int)(i % m.cols), r = (int)(i / m.cols) * 8;
-  if (r >= m.rows) return;
-  const size_t at = (size_t)e * m.rows * m.cols;
-  uint32_t v[8];
-#pragma unroll
-  for (int q = 0; q < 8; ++q) v[q] = m.in[at + (size_t)(r + q) * m.cols + c];
-  *reinterpret_cast<uint4*>(m.out + at + (size_t)c * m.rows + r) =
-      make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
-}
 
 // Eight elements of a row from k on, or zeros in their place (the load of the row's first goes on).
 __device__ __forceinline__ uint4 load8(const uint16_t* row, int k, bool in) {
@@ -845,9 +820,8 @@ hipError_t launch_factors(const Factors& f, hipStream_t stream) {
   });
 }
 
-hipError_t in_order(const AdaptersArgs& a, hipStream_t stream) {
-  OrderArgs o{a.ids, a.T, a.L, a.offsets, a.rows, a.tokens, a.counts};
-  return launch_order(o, stream);
+OrderArgs order_of(const AdaptersArgs& a) {
+  return {a.ids, a.T, a.L, a.offsets, a.rows, a.tokens, a.counts};
 }
 
 }  // namespace
@@ -863,7 +837,7 @@ hipError_t launch_adapters(const AdaptersArgs& a, hipStream_t stream) {
     few_expand_kernel<<<dim3((a.n + 255) / 256, a.T), 256, 0, stream>>>(a, h);
     return hipGetLastError();
   }
-  hipError_t e = in_order(a, stream);
+  hipError_t e = launch_order(order_of(a), stream);
   if (e != hipSuccess) return e;
   const Tokens o{a.offsets, a.tokens, a.L, a.T, a.r};
   if ((e = launch_shrink(o, {a.x, a.ldx, a.d, a.a, nullptr, a.h}, nullptr, stream)) != hipSuccess)
@@ -873,13 +847,11 @@ hipError_t launch_adapters(const AdaptersArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_adapters_backward(const AdaptersArgs& a, hipStream_t stream) {
-  hipError_t e = in_order(a, stream);
+  hipError_t e = launch_order_and_transpose(order_of(a), {a.a, a.at, a.r, a.d}, {a.b, a.bt, a.n, a.r},
+                                            stream);
   if (e != hipSuccess) return e;
   if (a.T > 0) {
     const Tokens o{a.offsets, a.tokens, a.L, a.T, a.r};
-    const Transposed ta{a.a, a.at, a.r, a.d}, tb{a.b, a.bt, a.n, a.r};
-    transpose_kernel<<<dim3(ta.groups() + tb.groups(), a.L), 256, 0, stream>>>(ta, tb, ta.groups(),
-                                                                              a.offsets);
     const Shrink g{a.dy, a.lddy, a.n, a.bt, a.scales, a.dh};
     if ((e = launch_shrink(o, {a.x, a.ldx, a.d, a.a, nullptr, a.h}, &g, stream)) != hipSuccess)
       return e;

@@ -41,7 +41,16 @@ inline size_t order_bytes(int pairs, int E) {
   const int parts = order_parts(pairs);
   return align256(sizeof(int32_t) * size_t(parts > kOrderParts ? parts : kOrderParts) * E);
 }
+// A matrix [rows, cols] of each expert with pairs -> [cols, rows].
+struct Transposed {
+  const uint16_t* in;
+  uint16_t* out;
+  int rows, cols;
+};
 hipError_t launch_order(const OrderArgs& a, hipStream_t stream);
+// The order and, beside it where it is one launch, both transposed.
+hipError_t launch_order_and_transpose(const OrderArgs& a, const Transposed& first,
+                                      const Transposed& second, hipStream_t stream);
 
 // ---------------------------------------------------------------------------- moves
 

@@ -111,11 +111,45 @@ __device__ __forceinline__ int block_scan(int v, int* part, int& total) {
   return before + upto - v;
 }
 
+// Both matrices of expert e, kThreads threads a workgroup; a thread takes eight rows of a column.
+struct Transposes {
+  Transposed first, second;
+  int groups, groups_first;    // workgroups of an expert, those of its first matrix
+};
+int transpose_groups(const Transposed& m) {
+  return (int)(((size_t)m.rows / 8 * m.cols + kThreads - 1) / kThreads);
+}
+__device__ __forceinline__ void transpose(const Transposes& t, int e, int group) {
+  const bool first = group < t.groups_first;
+  const Transposed m = first ? t.first : t.second;
+  const size_t i = (size_t)(first ? group : group - t.groups_first) * kThreads + threadIdx.x;
+  const int c = (int)(i % m.cols), r = (int)(i / m.cols) * 8;
+  if (r >= m.rows) return;
+  const size_t at = (size_t)e * m.rows * m.cols;
+  uint32_t v[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = m.in[at + (size_t)(r + q) * m.cols + c];
+  *reinterpret_cast<uint4*>(m.out + at + (size_t)c * m.rows + r) =
+      make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+__global__ __launch_bounds__(kThreads) void transpose_kernel(Transposes t, const int32_t* offsets) {
+  const int e = blockIdx.y;
+  if (offsets[e] < offsets[e + 1]) transpose(t, e, blockIdx.x);
+}
+
 // The whole sort (kParts false), or the second launch of two: part blockIdx.x of the pairs, whose
 // counts[part][e] the first launch wrote.
 template <bool kParts>
-__global__ __launch_bounds__(kThreads) void order_kernel(OrderArgs a, int part_size, int bits) {
+__global__ __launch_bounds__(kThreads) void order_kernel(OrderArgs a, int part_size, int bits,
+                                                         Transposes beside) {
   extern __shared__ int lds[];                         // [kWaves][E] and [kWaves]
+  if (!kParts && blockIdx.x > 0) {                     // (an expert's pairs are not known yet)
+    const int e = (blockIdx.x - 1) / beside.groups;
+    int has = 0;
+    for (int i = threadIdx.x; i < a.pairs; i += kThreads) has |= a.ids[i] == e;
+    if (__syncthreads_or(has)) transpose(beside, e, (blockIdx.x - 1) % beside.groups);
+    return;
+  }
   int* const part = lds + kWaves * a.E;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int begin = kParts ? blockIdx.x * part_size : 0;
@@ -169,9 +203,7 @@ __global__ __launch_bounds__(kThreads) void order_count_kernel(OrderArgs a, int 
     a.counts[(size_t)blockIdx.x * a.E + e] = lds[e];
 }
 
-}  // namespace
-
-hipError_t launch_order(const OrderArgs& a, hipStream_t stream) {
+hipError_t run(const OrderArgs& a, const Transposes& beside, hipStream_t stream) {
   int bits = 1;
   while ((1 << bits) <= a.E) ++bits;                   // keys 0 .. E
   const size_t lds = sizeof(int) * (size_t(kWaves) * a.E + kWaves);
@@ -184,7 +216,31 @@ hipError_t launch_order(const OrderArgs& a, hipStream_t stream) {
   }
   if (parts)
     order_count_kernel<<<parts, kThreads, sizeof(int) * a.E, stream>>>(a, part);
-  kernel<<<parts ? parts : 1, kThreads, lds, stream>>>(a, part, bits);
+  const unsigned grid = parts ? parts : 1 + a.E * beside.groups;
+  kernel<<<grid, kThreads, lds, stream>>>(a, part, bits, beside);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_order(const OrderArgs& a, hipStream_t stream) {
+  return run(a, Transposes{}, stream);
+}
+
+// Every workgroup beside the sort looks through the ids for its expert, up to kOrderOne of them: a launch
+// less, as long as the workgroups are so few that they take no longer than the sort (adapters' gradients
+// of 4000 tokens, 5 of rank 16, n = d = 4096: 55.7 us, 58.0 in two launches; of 13 tokens 35 and 41 with
+// the forward call).
+constexpr int kMostBeside = 1024;
+hipError_t launch_order_and_transpose(const OrderArgs& a, const Transposed& first,
+                                      const Transposed& second, hipStream_t stream) {
+  Transposes t{first, second, 0, transpose_groups(first)};
+  const int groups = t.groups_first + transpose_groups(second);
+  const bool beside = a.pairs > 0 && order_parts(a.pairs) == 0 && (long)a.E * groups <= kMostBeside;
+  if (beside) t.groups = groups;
+  const hipError_t e = run(a, t, stream);
+  if (e != hipSuccess || beside || a.pairs == 0) return e;
+  transpose_kernel<<<dim3(groups, a.E), kThreads, 0, stream>>>(t, a.offsets);
   return hipGetLastError();
 }
 
