@@ -108,12 +108,15 @@ constexpr int kAdapterOne = 1 << 20;
 // Values of a row of h: the ranks of the kernels' instances, which have 1, 2, 4 or 8 tiles of 16.
 inline int padded_rank(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
 
-// Parts that the rows of an adapter are summed in for its factors' gradients.
+// Parts that the rows of an adapter are summed in for its factors' gradients: as many as make two
+// workgroups for every compute unit, of 256 rows or more on average, for their sums take a launch
+// (2094 tokens of 26 adapters of rank 120, n = 192, d = 376: 36.8 us in 2 parts, 32.4 in one; 5482 of 2,
+// rank 72, n = 2704, d = 4584: 132 in 4, 153 in 2).
 constexpr int kGradColumns = 128;      // columns of x or dy of a workgroup
 inline int adapter_splits(int T, int L, int n, int d) {
   const long groups = long(L) * ((n + kGradColumns - 1) / kGradColumns +
                                  (d + kGradColumns - 1) / kGradColumns);
-  const long want = 511 / groups, most = (T + 255) / 256;
+  const long want = 511 / groups, most = T / (256l * L);
   const long n_parts = want < most ? want : most;
   return n_parts < 1 ? 1 : int(n_parts);
 }
