@@ -4,7 +4,7 @@
 //   dA_e = sum over its tokens of dh_t x_t^T,  dB_e = s_e sum of dy_t h_t^T,  h_t = A_e x_t
 //
 // Every product has one short side, r, so all are bound by reading and writing rows of d and n
-// values.  Up to kAdapterFew tokens are worked on one by one: a wave for each value of h, then a
+// values.  Few tokens (few_tokens) are worked on one by one: a wave for each value of h, then a
 // lane for each of y.  More are put in adapters' order first, and tiles of tokens of one adapter
 // go through the matrix instructions.  h and dh are held as sums of three bf16 values (24 bits), so
 // that the products with them are as exact as those of fp32 values; y and dx, which are rounded
@@ -827,7 +827,7 @@ OrderArgs order_of(const AdaptersArgs& a) {
 }  // namespace
 
 hipError_t launch_adapters(const AdaptersArgs& a, hipStream_t stream) {
-  if (a.T <= kAdapterFew) {
+  if (few_tokens(a.T, a.r, a.n, a.d)) {
     if ((long)a.T * ((a.n + 1023) / 1024) * a.r * a.d <= kAdapterOne) {
       few_kernel<<<dim3((a.n + 1023) / 1024, a.T), 1024, 0, stream>>>(a);
       return hipGetLastError();

@@ -100,10 +100,20 @@ hipError_t launch_grouped_backward_w(const GroupedArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------------------- adapters
 
-// Tokens up to which an adapters call goes token by token, without an order; in one launch where its
-// workgroups read no more values of A than this (each a whole A_e: one token of n = d = 4096, r = 16
-// in 4.9 us, 4.3 + 3.2 in two launches; 45 of n = 2048, d = 7168, r = 32 in 19.5, 5.8 + 3.2 in two).
-constexpr int kAdapterFew = 64;
+// Whether an adapters call goes token by token, without an order: by what both ways take in microseconds,
+// each token's factors at 9 TB/s from the caches against an order and, for each tile, chains over d.
+// Measured with 8 adapters at 48 to 256 tokens.  n = d = 4096: rank 16 8.4 us of 128 tokens, 16.6 in
+// order; rank 64 13.5 of 96, 24.8, and 29.4 of 256, 25.5; rank 128 12.9 of 48. n = 8192, d = 512, rank 64:
+// 16.9 of 96, 14.0.
+constexpr int kAdapterFew = 256;
+inline bool few_tokens(int T, int r, int n, int d) {
+  const float one_by_one = 4.0f + float(T) * r * (float(n) + d) / 4.4e6f;
+  const float in_order = 9.0f + d * (1.4f + r / 40.0f) * 1e-3f + float(r) * n / 2.5e6f;
+  return T <= kAdapterFew && one_by_one <= in_order;
+}
+// In one launch where its workgroups read no more values of A than this (each a whole A_e: one token of
+// n = d = 4096, r = 16 in 4.9 us, 4.3 + 3.2 in two launches; 45 of n = 2048, d = 7168, r = 32 in 19.5,
+// 5.8 + 3.2 in two).
 constexpr int kAdapterOne = 1 << 20;
 // Values of a row of h: the ranks of the kernels' instances, which have 1, 2, 4 or 8 tiles of 16.
 inline int padded_rank(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }

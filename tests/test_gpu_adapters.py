@@ -33,7 +33,8 @@ def _case(T, L, r, n, d, seed, none=0.25, pad=0, runs=False):
 SHAPES = [(1, 3, 8, 8, 8), (1, 4, 16, 4096, 4096), (2, 5, 24, 264, 520), (17, 3, 128, 136, 1000),
           (64, 20, 32, 2048, 712), (65, 20, 32, 520, 712), (65, 1, 16, 64, 72), (200, 7, 64, 328, 456),
           (300, 2, 40, 1032, 72), (333, 64, 8, 136, 264), (700, 1, 128, 264, 136),
-          (1500, 3, 16, 200, 1160), (513, 5, 104, 72, 520), (8300, 2, 72, 136, 328), (8200, 70, 48, 72, 200)]
+          (1500, 3, 16, 200, 1160), (513, 5, 104, 72, 520), (8300, 2, 72, 136, 328), (8200, 70, 48, 72, 200),
+          (256, 8, 24, 264, 520), (257, 8, 24, 264, 520), (200, 3, 128, 1032, 72)]
 
 
 @pytest.mark.parametrize("T,L,r,n,d", SHAPES)

@@ -54,11 +54,15 @@ def test_adapter_forms():
                  "expand_kernel<2, 1>", "expand_kernel<2, 2>", "expand_tile_kernel<4>",
                  "expand_tile_kernel<8>"):
         assert want in kernels, want
-    for (what, T, *_), names in zip(cases, got):
-        if what == "adapters" and T <= 64:
-            assert names in (["few_kernel"], ["few_shrink_kernel", "few_expand_kernel"])
+    few = []
+    for (what, T, *rest), names in zip(cases, got):
+        if what == "adapters" and names[0].startswith("few_"):
+            assert names in (["few_kernel"], ["few_shrink_kernel", "few_expand_kernel"]) and T <= 256
+            few.append((T, *rest))
         elif what == "adapters":
             assert names[-3 if T <= 4096 else -4].startswith("order_") and len(names) in (3, 4)
+    assert (1, 3, 8, 8, 8) in few and (256, 8, 24, 264, 520) in few
+    assert (257, 8, 24, 264, 520) not in few and (200, 3, 128, 1032, 72) not in few
 
 
 def test_columns_of_one_buffer_do_not_overlap():
