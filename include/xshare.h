@@ -730,7 +730,8 @@ xshare_status xshare_block_experts(const xshare_block_experts_args* args);
  * Limits: T * k and every other size at most 2^20, at most 1024 experts or adapters, k <= 32 *
  * (XSHARE_EUNSUPPORTED beyond).  Every call gives the same bits again.  What a call writes     *
  * must not overlap what it reads but where it says so; matrices of rows that do are refused   *
- * (XSHARE_EINVAL).                                                                            *
+ * (XSHARE_EINVAL).  Columns of one buffer side by side do not overlap; of matrices whose rows  *
+ * lie differently far apart, any in the same range of memory do, but for those of a single row. *
  * ---------------------------------------------------------------------------------------- */
 
 /* Workspace of xshare_expert_order (bytes, 256-aligned); 0 where it needs none (T * top_k up to

@@ -60,19 +60,22 @@ struct Rows {
   int32_t cols;
 };
 // Whether two matrices of elements of `size` bytes share memory.  Columns of one buffer that lie side
-// by side do not.
+// by side do not.  (Rows that lie differently far apart are taken to meet where the matrices' memory
+// does; a single row has no distance of its own.)
 bool overlap(const Rows& a, const Rows& b, uint64_t size) {
   if (!a.p || !b.p || a.rows == 0 || b.rows == 0) return false;
   const uint64_t p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
   const uint64_t bytes_p = (uint64_t(a.rows - 1) * uint64_t(a.ld) + a.cols) * size;
   const uint64_t bytes_q = (uint64_t(b.rows - 1) * uint64_t(b.ld) + b.cols) * size;
   if (p + bytes_p <= q || q + bytes_q <= p) return false;
-  if (a.ld != b.ld) return true;
-  const uint64_t row = uint64_t(a.ld) * size;          // b's first column from a's on, within a row
+  if (a.rows == 1 && b.rows == 1) return true;
+  if (a.rows > 1 && b.rows > 1 && a.ld != b.ld) return true;
+  const uint64_t row = uint64_t(a.rows > 1 ? a.ld : b.ld) * size;
+  // b's first column from a's on, within a row
   const uint64_t apart = p <= q ? (q - p) % row : (row - (p - q) % row) % row;
   return apart < a.cols * size || apart + b.cols * size > row;
 }
-bool same(const Rows& a, const Rows& b) { return a.p == b.p && a.ld == b.ld; }
+bool same(const Rows& a, const Rows& b) { return a.p == b.p && (a.ld == b.ld || a.rows == 1); }
 uint64_t bytes_of(int32_t dtype) { return dtype == XSHARE_F32 ? 4 : 2; }
 
 xs::MoveArgs move_args(int32_t dtype, int32_t T, int32_t k, int32_t d, const int32_t* rows) {
