@@ -1054,6 +1054,12 @@ def _no_gradient(t, name, instead):
                          f"call under torch.no_grad(); {instead}")
 
 
+def _no_second_gradient(t, name):
+    """The same for the incoming gradient of a backward call, which requires one where a gradient is
+    itself to be differentiated.  (The call's other operands may be parameters, which always do.)"""
+    _no_gradient(t, name, "there is no call for the gradient of a gradient")
+
+
 def _stream_of(x, stream):
     """The handle of x's device's current stream, without a Stream object where torch gives it
     (3 us less a call, of about 10 that the shortest of these calls take)."""
@@ -1118,13 +1124,16 @@ def gate_backward(logits: torch.Tensor, ids: torch.Tensor, dw: torch.Tensor, *, 
                   renormalize: bool = True, scale: float = 1.0, out=None,
                   stream=None) -> torch.Tensor:
     """The gradient of the logits (fp32 [T, N]) from dw, the gradient of ``gate``'s weights, for
-    its choice ids; score, renormalize and scale as given to ``gate``."""
+    its choice ids; score, renormalize and scale as given to ``gate``.  Records no gradient itself,
+    as the other backward calls, and refuses an incoming one that requires a gradient."""
     dtype, ld = _logits(logits)
     T, N = logits.shape
     k = ids.shape[1] if ids.dim() == 2 else -1
     if (T | N | k) >> 31:
         _sizes(T | N | k, "xshare_gate_backward")
     _fit(logits.device, (ids, torch.int32, (T, k), "ids"), (dw, torch.float32, (T, k), "dw"))
+    if dw.requires_grad:
+        _no_second_gradient(dw, "dw")
     if out is None:
         out = logits.new_empty((T, N), dtype=torch.float32)
     else:
@@ -1411,6 +1420,8 @@ def _combine(src, w, order, out, stream, name):
 def dispatch_backward(drows: torch.Tensor, order: dict, *, out=None, stream=None) -> torch.Tensor:
     """The gradient of ``dispatch``'s x [T, d] from that of its rows [T k, d]: each token's rows,
     summed in fp32 and rounded once."""
+    if isinstance(drows, torch.Tensor) and drows.requires_grad:
+        _no_second_gradient(drows, "drows")
     return _combine(drows, None, order, out, stream, "drows")
 
 
@@ -1433,6 +1444,8 @@ def combine_backward(dy: torch.Tensor, rows: torch.Tensor, w: torch.Tensor, orde
     """The gradients of ``combine`` from dy [T, d]: dict(drows [T k, d], dw fp32 [T, k]).  drows
     outside the order's rows is left as it was (``out``) or holds nothing; dw is 0 there."""
     dtype, lddy = _movable(dy, "dy")
+    if dy.requires_grad:
+        _no_second_gradient(dy, "dy")
     at, T, k = _order_rows(order, dy.device)
     d = dy.shape[1]
     if (T | k | d) >> 31:
@@ -1511,6 +1524,8 @@ def grouped_linear_backward_x(dy: torch.Tensor, w: torch.Tensor, offsets: torch.
                               workspace=None, stream=None) -> torch.Tensor:
     """The gradient of ``grouped_linear``'s x: dx_p = W_e^T dy_p (bf16 [P, k])."""
     lddy, P, E, n, k = _grouped(dy, w, offsets, 0, "dy", "xshare_grouped_linear_backward_x")
+    if dy.requires_grad:
+        _no_second_gradient(dy, "dy")
     out, ldo = _matrix_out(out, dy, (P, k), "out")
     _ws, ws, size = _grouped_workspace(dy, workspace, P, E, n, k)
     st = lib().xshare_grouped_linear_backward_x(dy.data_ptr(), lddy, w.data_ptr(),
@@ -1528,6 +1543,8 @@ def grouped_linear_backward_w(dy: torch.Tensor, x: torch.Tensor, offsets: torch.
     dy_p x_p^T, fp32 [E, n, k] (or of ``out``'s type, fp32 or bf16); zeros for a group without
     rows.  ``accumulate``: added to an fp32 ``out`` instead."""
     lddy = _rows(dy, torch.bfloat16, "dy")
+    if dy.requires_grad:
+        _no_second_gradient(dy, "dy")
     ldx = _rows(x, torch.bfloat16, "x")
     P, n = dy.shape
     k = x.shape[1]
@@ -1621,6 +1638,8 @@ def adapters_backward(dy: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: tor
     """The gradients of ``adapters`` from dy [T, n]: dict(dx bf16 [T, d], da fp32 [adapters, rank, d],
     db fp32 [adapters, n, rank]).  ``base`` [T, d]: what dx is added to (the shared projection's
     part; ``out["dx"]`` may be it); zeros in da and db for adapters without tokens."""
+    if isinstance(dy, torch.Tensor) and dy.requires_grad:
+        _no_second_gradient(dy, "dy")
     dx, da, db = (None, None, None) if out is None else (out.get("dx"), out.get("da"),
                                                          out.get("db"))
     p, dx, _ws = _adapters_args(x, a, b, ids, scales, base, dx, workspace, stream, True)
