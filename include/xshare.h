@@ -892,6 +892,12 @@ xshare_status xshare_adapters(const xshare_adapters_args* args);
  * out_t = base_t + A_e^T dh_t (base: the part of x's gradient that the shared projection gives),
  * da_e = sum over its tokens of dh_t x_t^T, db_e = scales[e] times the sum of dy_t h_t^T (base
  * itself passes dy on).  The last two in fp32 throughout (h and dh to 24 bits).
+ *
+ * An infinity in a token's x makes that column of its adapter's da, and through h all of its db,
+ * infinities or NaN (NaN also where a product in fp32 would give an infinity: h and dh are sums of
+ * three values, of which infinity times zero is one); one in its dy that row of db, through dh all
+ * of da, and the token's out.  Other adapters' gradients, and what of these is not named, keep
+ * their bits.
  */
 xshare_status xshare_adapters_backward(const xshare_adapters_args* args);
 
