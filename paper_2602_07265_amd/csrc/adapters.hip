@@ -205,7 +205,8 @@ struct ShrinkLds {
 template <int MT, int JT>
 __global__ __launch_bounds__(512) void shrink_kernel(Tokens o, Shrink first_a, Shrink second,
                                                      int groups) {
-  constexpr int kWaves = 8, kAhead = JT == 1 ? 4 : JT <= 4 ? 2 : 1;
+  static_assert(JT <= 2, "ranks past 32 are shrink_tile_kernel's");
+  constexpr int kWaves = 8, kAhead = JT == 1 ? 4 : 2;
   extern __shared__ floatx4 sums[];                    // [kWaves][MT JT][64]
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -377,6 +378,7 @@ __device__ __forceinline__ void copy_rest(const Expand& a, int T, int first) {
 // tokens without an adapter.
 template <int MT, int JT>
 __global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int groups) {
+  static_assert(JT <= 2, "ranks past 32 are expand_tile_kernel's");
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
@@ -402,9 +404,8 @@ __global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int gro
   const float scale = a.scales ? a.scales[e] : 1.0f;
   const uint16_t* const w = a.w + (size_t)e * a.N * o.r;
   const int end = min(c0 + a.columns, a.N);
-  // W's rows go with both parts of h: with 16 ranks the parts lie in one operand, else in two
-  constexpr int kSteps = JT == 1 ? 1 : JT / 2;
-  uint4 fw[2][kSteps], base[MT];
+  // W's rows go with both parts of h: with 16 ranks the parts lie in one operand, with 32 in two
+  uint4 fw[2], base[MT];
   auto fetch = [&](int c) {                            // under way while the columns before are stored
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
@@ -415,11 +416,8 @@ __global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int gro
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const int col = min(c + 8 * (n >> 2) + 4 * m + (n & 3), a.N - 1);
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const int j = (32 * s + 8 * g) % (16 * JT);
-        fw[m][s] = load8(w + (size_t)col * o.r, j, j < o.r);
-      }
+      const int j = 8 * g % (16 * JT);
+      fw[m] = load8(w + (size_t)col * o.r, j, j < o.r);
     }
   };
   if (c0 + 32 * wave < end) fetch(c0 + 32 * wave);
@@ -434,14 +432,10 @@ __global__ __launch_bounds__(256) void expand_kernel(Tokens o, Expand a, int gro
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
         acc[m][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          const bf16x8 v = __builtin_bit_cast(bf16x8, fw[m][s]);
-          acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, fh[t][s], acc[m][t], 0, 0, 0);
-          if constexpr (JT > 1)
-            acc[m][t] =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, fh[t][kSteps + s], acc[m][t], 0, 0, 0);
-        }
+        const bf16x8 v = __builtin_bit_cast(bf16x8, fw[m]);
+        acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, fh[t][0], acc[m][t], 0, 0, 0);
+        if constexpr (JT > 1)
+          acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, fh[t][1], acc[m][t], 0, 0, 0);
       }
     if (c + 128 < end) fetch(c + 128);
 #pragma unroll
