@@ -90,8 +90,8 @@ __global__ __launch_bounds__(256) void few_expand_kernel(AdaptersArgs a, const f
   a.out[(size_t)t * a.ld_out + c] = to_bf16(y);
 }
 
-// Both in one launch, for factors that every workgroup may read: workgroup (1024 columns, t) makes
-// token t's h for itself, a wave a value at a time, while the first values of B_e are under way.
+// Both in one launch (in_one_launch): workgroup (1024 columns, t) makes token t's h for itself, a wave a
+// value at a time, while the first values of B_e are under way.
 __global__ __launch_bounds__(1024) void few_kernel(AdaptersArgs a) {
   constexpr int kAhead = 4;                            // of eight values of a row of B_e
   __shared__ float hs[kMaxRank];
@@ -822,7 +822,7 @@ OrderArgs order_of(const AdaptersArgs& a) {
 
 hipError_t launch_adapters(const AdaptersArgs& a, hipStream_t stream) {
   if (few_tokens(a.T, a.r, a.n, a.d)) {
-    if ((long)a.T * ((a.n + 1023) / 1024) * a.r * a.d <= kAdapterOne) {
+    if (in_one_launch(a.T, a.r, a.n, a.d)) {
       few_kernel<<<dim3((a.n + 1023) / 1024, a.T), 1024, 0, stream>>>(a);
       return hipGetLastError();
     }

@@ -111,10 +111,20 @@ inline bool few_tokens(int T, int r, int n, int d) {
   const float in_order = 9.0f + d * (1.4f + r / 40.0f) * 1e-3f + float(r) * n / 2.5e6f;
   return T <= kAdapterFew && one_by_one <= in_order;
 }
-// In one launch where its workgroups read no more values of A than this (each a whole A_e: one token of
-// n = d = 4096, r = 16 in 4.9 us, 4.3 + 3.2 in two launches; 45 of n = 2048, d = 7168, r = 32 in 19.5,
-// 5.8 + 3.2 in two).
-constexpr int kAdapterOne = 1 << 20;
+// Such a call in one launch, whose workgroups (of 1024 columns of a token) each make the token's h for
+// themselves, or in two, whose first has a wave for each value.  A workgroup has 16 waves: up to 16
+// ranks are a row of A each, as in two launches; more rows come one after the other, which the launch
+// saved (1.4 us) pays for while rows are short; from 56 ranks on the rows of B that were not loaded ahead
+// cost more than it.  With more than a workgroup a compute unit A is read too often.  One launch and
+// two, us, of 840 sizes with 8 adapters.  One token, n = 4096: rank 16, d = 4096 4.8, 6.1, d = 8192
+// 6.7, 8.3; rank 24, d = 2048 4.2, 4.9, d = 4096 6.8, 6.3; rank 32, d = 1024 4.3, 4.6, d = 2048 5.2,
+// 4.9; rank 40, d = 2048 5.4, 5.0; rank 48, d = 512 4.3, 4.6; rank 64, d = 256 7.3, 5.1, d = 4096
+// 14.8, 6.8.  Rank 16, n = 4096: 32 tokens of d = 4096 5.0, 6.3; 128 of d = 2048 6.0, 6.6, of d = 8192
+// 12.2, 10.4.
+inline bool in_one_launch(int T, int r, int n, int d) {
+  const long groups = long(T) * ((n + 1023) / 1024), values = long(r) * d;   // of A, a workgroup
+  return (r <= 16 || (r <= 48 && values < 1 << 16)) && (groups <= 256 || groups * values <= 1 << 24);
+}
 // Values of a row of h: the ranks of the kernels' instances, which have 1, 2, 4 or 8 tiles of 16.
 inline int padded_rank(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
 

@@ -1,5 +1,6 @@
 """The ways that calls of adapters go at the sizes of the GPU tests, on the CPU: what these tests are
 for is what they run."""
+import test_gpu_adapter_few as few
 import test_gpu_adapter_loops as loops
 import test_gpu_adapter_order as order
 from adapter_grids import adapter_grids
@@ -52,3 +53,10 @@ def test_an_adapter_has_more_tokens_than_a_chunk():
         assert splits == 1 and int((ids == 5).sum()) > CHUNK and not (ids == 9).any(), s
         seen.add(name)
     assert seen == {f"factors_kernel<{j}>" for j in (1, 2, 4, 8)}
+
+
+def test_few_tokens_in_one_launch_or_two():
+    got = adapter_grids([(0, *s) for s in few.ONE + few.TWO])
+    names = [[name for name, _ in launched] for launched in got]
+    for s, launched in zip(few.ONE + few.TWO, names):
+        assert launched == (["few_kernel"] if s in few.ONE else ["few_shrink_kernel", "few_expand_kernel"]), s
