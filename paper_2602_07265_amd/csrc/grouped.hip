@@ -13,8 +13,9 @@
 // instruction's operands hit all banks; each load's buffer ends with the group's last value, so that
 // past it (another group's values, infinities too) zeros arrive.
 //
-// Few rows are bound by the weights' stream (8 rows of 8 (1536, 2048) experts: 50 MB in 11 us, 4.6
-// TB/s), many by the matrix cores (turns_kernel), dW of many small groups by its stores.
+// Few rows are bound by the weights' stream (8 rows of 8 (1536, 2048) experts, 50 MB: 10.8 us again and
+// again, out of the Infinity Cache, 14.3 us out of memory, where eight calls read 400 MB), many by the
+// matrix cores (turns_kernel), dW of many small groups by its stores.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -30,7 +31,10 @@ enum Kind { kForward, kGradX, kGradW };
 
 constexpr int kUnits = 256;             // compute units of the GPU
 constexpr int kTileQuads = 256 * 256 / 4;
-constexpr int kSplitRounds = 16;        // tiles a unit from which none is split
+// Tiles a unit from which none is split.  Rows of one group by (8192, 4096): 8448, 4.1 rounds, 426 us,
+// 460 where none is split from 4 on; 33024, 16.1 rounds, 1611, 1584 if they were; by (8192, 1024) 66000
+// rows, 32.3 rounds, 984, and 992.
+constexpr int kSplitRounds = 16;
 
 struct Product {
   const int32_t* offsets;
@@ -65,6 +69,8 @@ struct Shares {
   long whole;
   int rest, parts;
 };
+// With at least 4 blocks 8192 rows of 4 groups by (2312, 1032) take 72.9 us, 62.8 with 8; with 16 8192 rows
+// of one by (4104, 1032) 91.7, 89.7 with 8; 22 other products of 300 to 8192 rows take the same, within 1.2 %.
 constexpr int kLeastBlocks = 8;
 __host__ __device__ inline Shares shares_of(long tiles, int reduction) {
   Shares s{tiles, 0, 1};
@@ -163,7 +169,9 @@ __device__ __forceinline__ floatx4 multiply_add(const bf16x8& a, const bf16x8& b
 // columns 4 g .. 4 g + 3 of each tile in row n; kSpread: of the pairs that tile_kernel deals; kGradW:
 // rows 4 g .. 4 g + 3 of column n, so that 16 lanes store 64 neighbouring bytes and not 16 of each of 16
 // rows (dW of 128 groups of 256 rows by (1536, 2048): 471 us, 558 the other way, of which 273 are the
-// stores alone; 64 of 64 rows by (2048, 1536): 158 us, 191.  y and dx took no less time so).
+// stores alone; 64 of 64 rows by (2048, 1536): 158 us, 191.  y and dx took no less time so).  In bf16
+// the two take 482 and 176 us.  Added to dW they take 1546 and 766: a lane's values are read, added and
+// stored one after the other; one group of 8192 rows by (4096, 4096) 248, 226 if it is not added.
 template <Kind kKind, bool kSpread, int MA>
 __device__ __forceinline__ void store(const Product& a, const Tile& t, int r0, int c, int n, int g,
                                       const floatx4 (&v)[MA]) {

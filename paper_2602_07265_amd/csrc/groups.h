@@ -102,7 +102,8 @@ hipError_t launch_grouped_backward_w(const GroupedArgs& a, hipStream_t stream);
 
 // Whether an adapters call goes token by token, without an order: by what both ways take in microseconds,
 // each token's factors at 9 TB/s from the caches against an order and, for each tile, chains over d.
-// Measured with 8 adapters at 48 to 256 tokens.  n = d = 4096: rank 16 8.4 us of 128 tokens, 16.6 in
+// Measured with 8 adapters at 48 to 256 tokens; with 1 and with 64 of them, at 32 to 256 tokens, the choice was
+// the faster one of all 20 sizes too.  n = d = 4096: rank 16 8.4 us of 128 tokens, 16.6 in
 // order; rank 64 13.5 of 96, 24.8, and 29.4 of 256, 25.5; rank 128 12.9 of 48. n = 8192, d = 512, rank 64:
 // 16.9 of 96, 14.0.
 constexpr int kAdapterFew = 256;
