@@ -16,6 +16,9 @@ WIDE_BACK = [(3000, 2, 24, 264, 4104), (4000, 2, 8, 520, 3080)]
 # one adapter with most of the tokens
 HEAVY = [(9000, 64, r, 200, 232) for r in (8, 32, 64, 120)] + [(4700, 70, 16, 136, 264)]
 MOST = 0.6
+# as many adapters as there may be, about as many of which have tokens as not; the shortest rows
+MANY = [(300, 1024, 8, 64, 72), (300, 512, 8, 64, 72), (1500, 1024, 16, 136, 72), (5000, 1000, 40, 72, 136)]
+SHORT = [(300, 3, r, n, d) for r in (8, 32, 40, 128) for n, d in ((8, 8), (8, 16), (136, 8))]
 
 
 def _check(c, T, r, n, d, based):
@@ -61,3 +64,9 @@ def test_an_adapter_with_most_tokens(T, L, r, n, d):
     c = _case(T, L, r, n, d, T + r)
     c["ids"] = heavy_ids(T, L, r).to(DEV)
     _check(c, T, r, n, d, False)
+
+
+@pytest.mark.parametrize("T,L,r,n,d", MANY + SHORT)
+def test_many_adapters_and_short_rows(T, L, r, n, d):
+    say(f"adapters, many or of short rows: T={T} L={L} r={r} n={n} d={d}")
+    _check(_case(T, L, r, n, d, T + r, pad=8), T, r, n, d, True)
